@@ -8,7 +8,8 @@
  *
  * Conventions for every call
  *   - Every pointer named "device" is HIP device memory on the current device; "host" is host
- *     memory.  Dense matrices are fp32, row-major, with a leading dimension in elements.
+ *     memory.  Dense matrices are row-major, with a leading dimension in elements: fp32, and in the calls that take an
+ *     element type (gcn_linear_*, gcn_block_norm_*, gcn_distill) of that type.
  *   - Dense buffers are owned by the caller; the library neither frees nor keeps them after the
  *     work queued on `stream` has finished.  Only gcn_csr objects own device memory.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Compute calls only
@@ -22,8 +23,8 @@
  *     earlier stay valid.
  *   - A matrix that gcn_csr_create symmetrised and did not normalise by rows equals its transpose bit by bit: it is
  *     stored once, and gcn_csr_arrays gives the same arrays for both.
- *   - Library-owned scratch exists only for the stand-alone gcn_gemm (ta = 1), gcn_softmax_nll* and the gradients of
- *     gcn_layer_backward: a buffer per (device, stream), grown on demand by the first call that needs more (an
+ *   - Library-owned scratch exists only for the stand-alone gcn_gemm (ta = 1), gcn_softmax_nll*, the gradients of
+ *     gcn_layer_backward, gcn_linear_* , gcn_block_norm_backward and gcn_distill: a buffer per (device, stream), grown on demand by the first call that needs more (an
  *     allocation), never shared between streams, nor between calls that threads make on one stream at the same time: these get
  *     buffers of their own.  gcn_scratch_release frees all of them.  The epoch calls keep these partial sums in the caller's
  *     workspace instead.
@@ -70,6 +71,19 @@ extern "C" {
 
 #define GCN_ACT_NONE 0
 #define GCN_ACT_RELU 1
+#define GCN_ACT_GELU 2 /* z/2 (1 + erf(z / sqrt 2)); gcn_linear_* only, as the next */
+#define GCN_ACT_SILU 3 /* z / (1 + exp(-z)) */
+
+/* element types of gcn_linear_*, gcn_block_norm_* and gcn_distill; sums, statistics and vectors are fp32 with each of them */
+#define GCN_F32 0
+#define GCN_BF16 1
+#define GCN_F16 2
+
+/* norms of gcn_block_norm_* */
+#define GCN_NORM_RMS 0   /* x / sqrt(mean(x^2) + eps) */
+#define GCN_NORM_LAYER 1 /* (x - mean(x)) / sqrt(var(x) + eps), var the mean squared deviation */
+
+#define GCN_DISTILL_MOST 4096 /* entries of a teacher's list in gcn_distill */
 
 /* gcn_config / gcn_csr_config keys */
 #define GCN_CFG_SPMM_ALGO 1 /* 0 = automatic, 1 = one thread per output element, 2 = nonzero-split, 3 = column sweep, 4 = hub schedule (long rows x hot columns over a packed buffer, the rest as 2) */
@@ -243,6 +257,74 @@ int gcn_softmax_nll(int64_t n, int32_t C, const float* Z, int64_t ldz, const int
  * knows its split); the mean and the 1/n factor of G use it.  BADARG unless 1 <= n_labelled <= n. */
 int gcn_softmax_nll_masked(int64_t n, int32_t C, const float* Z, int64_t ldz, const int32_t* labels,
                            int64_t n_labelled, float* loss, float* G, int64_t ldg, void* stream);
+
+/* -------------------------------------------------------------------------------------------
+ * A linear layer over the rows of X, with what follows it in the product's epilogue:
+ *   Z = X W + 1 bias^T,   Y = rho R + act(Z)
+ * X: n x f_in, W: f_in x f_out, R, Z, Y: n x f_out, all of element type `type` (GCN_F32, GCN_BF16, GCN_F16); bias: fp32[f_out].  bias and R
+ * may be NULL; Z (the argument of act, which backward needs unless act is GCN_ACT_NONE) may be NULL.  Products are summed in
+ * fp32, and bias, activation and residual applied to the fp32 sum; Z and Y are rounded once.  fp32 elements are multiplied as
+ * fp32.  Y may be R (same address and leading dimension); no other output may overlap an input or another output.
+ * Sums have a fixed order: repeated calls give the same bits.  Rows and leading dimensions of any alignment are taken; rows at
+ * 16-byte addresses (and widths of whole 16 bytes) are faster.
+ * backward, with G = dL/dY given as dY:
+ *   dZ = dY (Hadamard) act'(Z),  dX = dZ W^T,  dW = X^T dZ,  dbias = column sums of dZ (before it is rounded),  dR = rho dY
+ * Any of dX, dW, dbias, dR may be NULL, and is then not computed; X is read for dW and W for dX only.  dZ (n x f_out) is workspace that the
+ * call fills, needed for dX and dW unless act is GCN_ACT_NONE (it is ignored then, and so is Z); it is rounded to the element type, which is what the matrix
+ * units take.  dZ may be Z or dY, and dR may be dY where dY is not needed any more (an activation, or neither dX nor dW).
+ * ReLU' is 1 for z > 0 and 0 for z <= 0; NaN stays NaN in both directions.
+ * ----------------------------------------------------------------------------------------- */
+int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W,
+                       int64_t ldw, const float* bias, int act, const void* R, int64_t ldr, float rho, void* Z,
+                       int64_t ldz, void* Y, int64_t ldy, void* stream);
+int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W,
+                        int64_t ldw, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho,
+                        void* dZ, int64_t lddz, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias, void* dR,
+                        int64_t lddr, void* stream);
+
+/* -------------------------------------------------------------------------------------------
+ * The norms around a block of a residual network, with the block's gate and residual scale, in one pass:
+ *   V = N(U; w_post, b_post),   X' = X + scale (Hadamard) sigmoid(A) (Hadamard) V,   H = N(X'; w_pre, b_pre)
+ * with N(x; w, b) = w (Hadamard) (x - mean) rstd + b over a row, `kind` GCN_NORM_RMS (mean = 0) or GCN_NORM_LAYER.
+ * X: the residual stream; U: what the block gave; A: the gate's argument, n x f (gate_cols = f) or one per row, n x 1 (gate_cols = 1); Xout = X';
+ * H: what the next block takes; X, U, A, Xout, H of element type `type`.  scale, w_*, b_*: fp32[f].  stats: fp32[n][4], receives
+ * mean and rstd of U's row and of that of X' (what backward needs; 0 where there is no such norm), or NULL.
+ * What may be left out (NULL): A (gate 1), scale (1), w_post with b_post (V = U), b_post, b_pre; U with all of these and Xout (X' = X: the norm in
+ * front of a first block); w_pre with H (behind a last one); Xout where only H is wanted.  The second norm is taken of X' before it is rounded.
+ * Xout and H may each be X, U or (n x f) A: same address and leading dimension; nothing else may overlap.
+ * backward: dXout and dH are the gradients of X' and H (either may be NULL: zero), Xout and stats what the forward call wrote.
+ *   dX = dXout + dN/dX'(dH);  dA, dscale, dw_post, db_post, dU from dX through the block's side; dw_pre, db_pre from dH.
+ * Each output may be NULL.  dA has the shape of A (with one gate per row a sum over it).  The vectors' gradients are fp32 sums over all
+ * rows in a fixed order.  dX, dU and dA may each be U, A, Xout, dXout or dH (same address, leading dimension and width).
+ * Widths up to 1024 times 16 bytes (forward: twice that) are held in registers; longer rows are read several times.
+ * ----------------------------------------------------------------------------------------- */
+int gcn_block_norm_forward(int64_t n, int32_t f, int type, int kind, float eps, const void* X, int64_t ldx, const void* U,
+                           int64_t ldu, const void* A, int32_t gate_cols, int64_t lda, const float* scale,
+                           const float* w_post, const float* b_post, const float* w_pre, const float* b_pre, void* Xout,
+                           int64_t ldxo, void* H, int64_t ldh, float* stats, void* stream);
+int gcn_block_norm_backward(int64_t n, int32_t f, int type, int kind, const void* U, int64_t ldu, const void* A,
+                            int32_t gate_cols, int64_t lda, const float* scale, const float* w_post, const float* b_post,
+                            const float* w_pre, const void* Xout, int64_t ldxo, const float* stats, const void* dXout,
+                            int64_t lddxo, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dU, int64_t lddu,
+                            void* dA, int64_t ldda, float* dscale, float* dw_post, float* db_post, float* dw_pre,
+                            float* db_pre, void* stream);
+
+/* -------------------------------------------------------------------------------------------
+ * Distillation: loss and gradient of the logits Z (n x C) against a teacher's k largest logits per row, mixed with the labels' loss:
+ *   p = softmax of t / T over the row's list,  q = softmax of z / T over all C,
+ *   loss = 1/m sum_i [ w_teacher T^2 sum_j p_j (log p_j - log q_top(j)) - w_label log softmax(z)_label ]
+ *   G = grad_scale dloss/dZ
+ * top: int32[n][k] (ld ldtop), the classes of the list; an index below 0 or from C on is no entry, and neither is one whose t is
+ * -inf (a list shorter than k, a row that the teacher never saw: a row without entries adds nothing to the teacher's part).  An index that comes twice counts as
+ * two entries.  t: n x k (ld ldt) and Z, G of element type `type`.  labels: int32[n] or NULL; a label outside [0, C) is none.  m: the divisor
+ * (host value, for instance the number of rows with a list or a label).  loss: fp32, written.  G: n x C or NULL; it may be Z.
+ * Logits of -inf are classes that cannot be (q = 0); a row of them alone has no softmax, and gives NaN if it has a list or a label.  Exponentials
+ * and row sums are fp32; the loss is added up in fp64 in a fixed order.  1 <= k <= min(C, GCN_DISTILL_MOST).  Rows up to
+ * 256 KB are read once.
+ * ----------------------------------------------------------------------------------------- */
+int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_t ldz, int32_t k, const int32_t* top, int64_t ldtop,
+                const void* t, int64_t ldt, const int32_t* labels, float temperature, float w_teacher, float w_label,
+                int64_t m, float grad_scale, float* loss, void* G, int64_t ldg, void* stream);
 
 /* -------------------------------------------------------------------------------------------
  * One layer forward -- "Forward Propagation": Z = A^T Hin W (+ bias), Hout = sigma(Z).

@@ -12,7 +12,9 @@ _HEADER = os.path.join(os.path.dirname(HERE), "include", "gcn.h")
 SYMMETRISE, ADD_SELF_LOOPS, NORM_SYM, BUILD_TRANSPOSE, NORM_ROW = 1, 2, 4, 8, 16
 EPI_NONE, EPI_RELU, EPI_MASK = 0, 1, 2
 ORDER_AUTO, ORDER_GEMM_FIRST, ORDER_SPMM_FIRST = 0, 1, 2
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
+F32, BF16, F16 = 0, 1, 2
+NORM_RMS, NORM_LAYER = 0, 1
 CFG_SPMM_ALGO, CFG_TIMING, CFG_SPMM_BLOCKS, CFG_SWEEP_HEAVY, CFG_SWEEP_WAVES, CFG_PATTERN_SPMM, CFG_HUB_MB, CFG_HUB_DMIN, CFG_HUB_BLOCK_COLS, CFG_SPLIT_LDS_KB, CFG_FUSED_LAST_LAYER = 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11
 
 _lib = None
@@ -66,8 +68,15 @@ def lib():
         L.gcn_epoch.argtypes = [p, i32, p, p, p, p, p, f32, p, p, sz, i, p]
         L.gcn_epoch_masked.argtypes = [p, i32, p, p, p, i64, p, p, f32, p, p, sz, i, p]
         L.gcn_epoch_preaggregated.argtypes = L.gcn_epoch_masked.argtypes
-        global _raw_stream, _device, _f32, _i32
+        L.gcn_linear_forward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i, p, i64, f32, p, i64, p, i64, p]
+        L.gcn_linear_backward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i64, p, i64, i, f32, p, i64, p, i64, p, i64, p, p, i64, p]
+        L.gcn_block_norm_forward.argtypes = [i64, i32, i, i, f32, p, i64, p, i64, p, i32, i64, p, p, p, p, p, p, i64, p, i64, p, p]
+        L.gcn_block_norm_backward.argtypes = [i64, i32, i, i, p, i64, p, i32, i64, p, p, p, p, p, i64, p, p, i64, p, i64, p, i64, p,
+                                              i64, p, i64, p, p, p, p, p, p]
+        L.gcn_distill.argtypes = [i64, i32, i, p, i64, i32, p, i64, p, i64, p, f32, f32, f32, i64, f32, p, p, i64, p]
+        global _raw_stream, _device, _f32, _i32, _types
         import torch
+        _types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
         _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _f32, _i32 = torch.float32, torch.int32
         _lib = L
@@ -309,6 +318,116 @@ def gcn_layer_backward(a: Csr, Hin, Zprev, W, G, T, S, Y, Gprev, order: int = OR
         assert t.is_contiguous()
     _check(L.gcn_layer_backward(a._h, f_in, f_out, _at(Hin), 0 if Hin is None else _ld(Hin), _at(Zprev), W.data_ptr(),
                                 G.data_ptr(), _at(T), S.data_ptr(), Y.data_ptr(), _at(dbias), _at(Gprev), int(order), _now()))
+
+
+def _elements(rows: int, cols: int, dtype, *tensors):
+    """Checks operands of rows x cols elements of one type (None: not there)."""
+    for t in tensors:
+        if t is not None:
+            assert t.is_cuda, "device tensor expected"
+            assert t.dtype is dtype and t.shape == (rows, cols), (t.dtype, tuple(t.shape), dtype, (rows, cols))
+
+
+def _vectors(size: int, *tensors):
+    """Checks fp32 vectors (None: not there)."""
+    for t in tensors:
+        if t is not None:
+            assert t.is_cuda, "device tensor expected"
+            assert t.dtype is _f32 and t.shape == (size,) and t.is_contiguous(), (t.dtype, tuple(t.shape), size)
+
+
+def _place(t):
+    """Address and leading dimension."""
+    return (0, 0) if t is None else (t.data_ptr(), _ld(t))
+
+
+def _type_of(t) -> int:
+    assert t.dtype in _types, f"elements are fp32, bf16 or fp16, not {t.dtype}"
+    return _types[t.dtype]
+
+
+def gcn_linear_forward(X, W, Y, bias=None, act: int = ACT_NONE, R=None, rho: float = 1.0, Z=None):
+    """Y = rho R + act(X W + 1 bias^T); Z receives the argument of act."""
+    L = _lib or lib()
+    n, f_in = X.shape
+    f_out = W.shape[1]
+    dt = X.dtype
+    _elements(n, f_in, dt, X), _elements(f_in, f_out, dt, W), _elements(n, f_out, dt, Y, R, Z), _vectors(f_out, bias)
+    rc = L.gcn_linear_forward(n, f_in, f_out, _type_of(X), *_place(X), *_place(W), _at(bias), act, *_place(R), rho, *_place(Z),
+                              *_place(Y), _now())
+    if rc:
+        _check(rc)
+    return Y
+
+
+def gcn_linear_backward(X, W, Z, dY, dZ=None, dX=None, dW=None, dbias=None, act: int = ACT_NONE, dR=None, rho: float = 1.0):
+    """The gradients that are given a place; dZ is workspace of the size of dY (none is needed without an activation).  X may be
+    None without dW, W without dX and Z without an activation."""
+    L = _lib or lib()
+    n, f_out = dY.shape
+    f_in = next(s for s in (X.shape[1] if X is not None else None, W.shape[0] if W is not None else None, 1) if s is not None)
+    dt = dY.dtype
+    _elements(n, f_out, dt, dY, Z, dZ, dR), _elements(n, f_in, dt, X, dX), _elements(f_in, f_out, dt, W, dW), _vectors(f_out, dbias)
+    rc = L.gcn_linear_backward(n, f_in, f_out, _type_of(dY), *_place(X), *_place(W), *_place(Z), *_place(dY), act, rho, *_place(dZ),
+                               *_place(dX), *_place(dW), _at(dbias), *_place(dR), _now())
+    if rc:
+        _check(rc)
+
+
+def gcn_block_norm_forward(X, U=None, Xout=None, H=None, w_pre=None, b_pre=None, A=None, scale=None, w_post=None, b_post=None,
+                           stats=None, kind: int = NORM_RMS, eps: float = 1e-5):
+    """Xout = X + scale sigmoid(A) N(U; w_post, b_post), H = N(Xout; w_pre, b_pre)."""
+    L = _lib or lib()
+    n, f = X.shape
+    _elements(n, f, X.dtype, X, U, Xout, H), _vectors(f, w_pre, b_pre, scale, w_post, b_post)
+    gate = 0 if A is None else A.shape[1]
+    _elements(n, gate, X.dtype, A)
+    if stats is not None:
+        _elements(n, 4, _f32, stats)
+        assert stats.is_contiguous()
+    rc = L.gcn_block_norm_forward(n, f, _type_of(X), kind, eps, *_place(X), *_place(U), _at(A), gate, 0 if A is None else _ld(A),
+                                  _at(scale), _at(w_post), _at(b_post), _at(w_pre), _at(b_pre), *_place(Xout), *_place(H), _at(stats),
+                                  _now())
+    if rc:
+        _check(rc)
+    return H
+
+
+def gcn_block_norm_backward(U, Xout, stats, dXout, dH, dX=None, dU=None, w_pre=None, A=None, dA=None, scale=None, w_post=None,
+                            b_post=None, dscale=None, dw_post=None, db_post=None, dw_pre=None, db_pre=None, kind: int = NORM_RMS):
+    """The gradients that are given a place, from dXout and dH (either may be None)."""
+    L = _lib or lib()
+    some = dH if dH is not None else dXout
+    n, f = some.shape
+    dt = some.dtype
+    _elements(n, f, dt, U, Xout, dXout, dH, dX, dU)
+    _vectors(f, w_pre, scale, w_post, b_post, dscale, dw_post, db_post, dw_pre, db_pre)
+    gate = 0 if A is None else A.shape[1]
+    _elements(n, gate, dt, A, dA)
+    _elements(n, 4, _f32, stats)
+    assert stats.is_contiguous()
+    rc = L.gcn_block_norm_backward(n, f, _type_of(some), kind, *_place(U), _at(A), gate, 0 if A is None else _ld(A), _at(scale),
+                                   _at(w_post), _at(b_post), _at(w_pre), *_place(Xout), _at(stats), *_place(dXout), *_place(dH),
+                                   *_place(dX), *_place(dU), *_place(dA), _at(dscale), _at(dw_post), _at(db_post), _at(dw_pre),
+                                   _at(db_pre), _now())
+    if rc:
+        _check(rc)
+
+
+def gcn_distill(Z, top, t, loss, G=None, labels=None, temperature: float = 1.0, w_teacher: float = 1.0, w_label: float = 0.0,
+                m: int | None = None, grad_scale: float = 1.0):
+    """Loss of the logits Z against the teacher's list (classes `top`, logits `t`) and the labels, and its gradient G.  m: the divisor
+    (None: the number of rows)."""
+    L = _lib or lib()
+    n, classes = Z.shape
+    k = top.shape[1]
+    _elements(n, classes, Z.dtype, Z, G), _elements(n, k, Z.dtype, t), _elements(n, k, _i32, top), _vectors(1, loss)
+    assert labels is None or (labels.is_cuda and labels.dtype is _i32 and labels.shape == (n,) and labels.is_contiguous())
+    rc = L.gcn_distill(n, classes, _type_of(Z), *_place(Z), k, *_place(top), *_place(t), _at(labels), temperature, w_teacher,
+                       w_label, n if m is None else m, grad_scale, loss.data_ptr(), *_place(G), _now())
+    if rc:
+        _check(rc)
+    return loss
 
 
 def _dims_array(dims):

@@ -1,0 +1,654 @@
+// The norms around a block, with the block's gate and its residual scale, in one pass over a row:
+//   V = N_post(U),  X' = X + scale * sigmoid(A) * V,  H = N_pre(X')
+// where N(x) = w (x - mean) rstd + b, mean = 0 for the root-mean-square norm, rstd = 1 / sqrt(mean((x - mean)^2) + eps); and its gradients.
+#include <initializer_list>
+#include <type_traits>
+
+#include "rows.h"
+#include "sum_parts.h"
+
+namespace gcn {
+
+struct NormArgs {
+    int64_t n = 0;
+    int32_t f = 0;
+    int layer = 0;                 // subtract the mean
+    float eps = 0;
+    int gate = 0;                  // columns of A: 0, 1 or f
+    int64_t ldx = 0, ldu = 0, lda = 0, ldxo = 0, ldh = 0;
+    const void *X = nullptr, *U = nullptr, *A = nullptr;
+    const float *scale = nullptr, *w_post = nullptr, *b_post = nullptr, *w_pre = nullptr, *b_pre = nullptr;
+    void *Xout = nullptr, *H = nullptr;
+    float* stats = nullptr;        // n x 4: mean and rstd of U, mean and rstd of X'
+    // backward
+    int64_t lddxo = 0, lddh = 0, lddx = 0, lddu = 0, ldda = 0;
+    const void *dXout = nullptr, *dH = nullptr;
+    void *dX = nullptr, *dU = nullptr, *dA = nullptr;
+    float* part = nullptr;         // partial sums: of each workgroup `sums` vectors of f
+    int sums = 0;
+    int at[4] = {-1, -1, -1, -1};  // which of them are sum dX' a u^, sum dX' a, sum dH x^, sum dH
+};
+
+__device__ __forceinline__ float gate_of(float a) { return 1.f / (1.f + expf(-a)); }
+
+template <typename T, int L, int P>
+__global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_block_norm(NormArgs g) {
+    using R = Rows<T, L, P>;
+    constexpr int E = R::E;
+    __shared__ float meet[2][16][4];
+    int turn = 0;
+    const int li = threadIdx.x % L;
+    const float inv_f = 1.f / (float)g.f;
+    for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < g.n; i += (int64_t)gridDim.x * R::ROWS) {
+        float x[P][E], u[P][E];
+        int count[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = R::column(p);
+            count[p] = R::there(c, g.f);
+            to_floats<T>(load_vec_part((const T*)g.X + i * g.ldx + c, count[p]), x[p]);
+            if (g.U) to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count[p]), u[p]);
+        }
+        float umean = 0.f, urstd = 0.f;
+        if (g.U) {
+            if (g.w_post) {
+                float s[1] = {0.f};
+                if (g.layer) {
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) s[0] += u[p][e];
+                    join_lanes<L>(s, meet, turn);
+                    umean = s[0] * inv_f;
+                }
+                s[0] = 0.f;
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float d = e < count[p] ? u[p][e] - umean : 0.f;
+                        s[0] = fmaf(d, d, s[0]);
+                    }
+                join_lanes<L>(s, meet, turn);
+                urstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
+            }
+            const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int c = R::column(p);
+                float w[E], b[E], sc[E], a[E];
+                load_floats<E>(g.scale, c, count[p], 1.f, sc);
+                if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count[p]), a);
+                if (g.w_post) {
+                    load_floats<E>(g.w_post, c, count[p], 1.f, w);
+                    load_floats<E>(g.b_post, c, count[p], 0.f, b);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float v = g.w_post ? fmaf((u[p][e] - umean) * urstd, w[e], b[e]) : u[p][e];
+                    x[p][e] = fmaf(sc[e] * (g.gate > 1 ? gate_of(a[e]) : row_gate), v, x[p][e]);
+                }
+                if (g.Xout) store_vec_part((T*)g.Xout + i * g.ldxo + c, from_floats<T>(x[p]), count[p]);
+            }
+        }
+        float xmean = 0.f, xrstd = 0.f;
+        if (g.H) {
+            float s[1] = {0.f};
+            if (g.layer) {
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s[0] += e < count[p] ? x[p][e] : 0.f;
+                join_lanes<L>(s, meet, turn);
+                xmean = s[0] * inv_f;
+            }
+            s[0] = 0.f;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float d = e < count[p] ? x[p][e] - xmean : 0.f;
+                    s[0] = fmaf(d, d, s[0]);
+                }
+            join_lanes<L>(s, meet, turn);
+            xrstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int c = R::column(p);
+                float w[E], b[E];
+                load_floats<E>(g.w_pre, c, count[p], 1.f, w);
+                load_floats<E>(g.b_pre, c, count[p], 0.f, b);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[p][e] = fmaf((x[p][e] - xmean) * xrstd, w[e], b[e]);
+                store_vec_part((T*)g.H + i * g.ldh + c, from_floats<T>(x[p]), count[p]);
+            }
+        }
+        if (g.stats && li == 0) *reinterpret_cast<f4u*>(g.stats + 4 * i) = f4u{umean, urstd, xmean, xrstd};
+    }
+}
+
+// The four sums over the rows are kept per column in registers and leave once per workgroup.
+template <typename T, int L, int P>
+__global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_block_norm_back(NormArgs g) {
+    using R = Rows<T, L, P>;
+    constexpr int E = R::E;
+    __shared__ float meet[2][16][4];
+    int turn = 0;
+    const int li = threadIdx.x % L;
+    const float inv_f = 1.f / (float)g.f;
+    float sum[4][P][E] = {};
+    for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < g.n; i += (int64_t)gridDim.x * R::ROWS) {
+        float dx[P][E];
+        int count[P];
+        const f4u st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = R::column(p);
+            count[p] = R::there(c, g.f);
+            if (g.dXout) to_floats<T>(load_vec_part((const T*)g.dXout + i * g.lddxo + c, count[p]), dx[p]);
+            else
+#pragma unroll
+                for (int e = 0; e < E; ++e) dx[p][e] = 0.f;
+        }
+        if (g.dH) {
+            float xh[P][E], gw[P][E];
+            float s[2] = {0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int c = R::column(p);
+                float w[E];
+                to_floats<T>(load_vec_part((const T*)g.Xout + i * g.ldxo + c, count[p]), xh[p]);
+                to_floats<T>(load_vec_part((const T*)g.dH + i * g.lddh + c, count[p]), gw[p]);
+                load_floats<E>(g.w_pre, c, count[p], 1.f, w);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    xh[p][e] = e < count[p] ? (xh[p][e] - st.z) * st.w : 0.f;
+                    sum[2][p][e] = fmaf(gw[p][e], xh[p][e], sum[2][p][e]);
+                    sum[3][p][e] += gw[p][e];
+                    gw[p][e] *= w[e];
+                    s[0] = fmaf(gw[p][e], xh[p][e], s[0]);
+                    s[1] += gw[p][e];
+                }
+            }
+            join_lanes<L>(s, meet, turn);
+            const float along = s[0] * inv_f, mean = g.layer ? s[1] * inv_f : 0.f;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < E; ++e) dx[p][e] = fmaf(st.w, gw[p][e] - fmaf(xh[p][e], along, mean), dx[p][e]);
+        }
+        auto store_dx = [&]() {                                  // behind the row's last load: dX may take the place of any of them
+            if (g.dX)
+#pragma unroll
+                for (int p = 0; p < P; ++p) store_vec_part((T*)g.dX + i * g.lddx + R::column(p), from_floats<T>(dx[p]), count[p]);
+        };
+        if (!g.U) {
+            store_dx();
+            continue;
+        }
+        const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
+        float uh[P][E], gv[P][E];
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = R::column(p);
+            float w[E], b[E], sc[E], a[E];
+            load_floats<E>(g.scale, c, count[p], 1.f, sc);
+            load_floats<E>(g.w_post, c, count[p], 1.f, w);
+            load_floats<E>(g.b_post, c, count[p], 0.f, b);
+            to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count[p]), uh[p]);
+            if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count[p]), a);
+            float da[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (g.w_post) uh[p][e] = e < count[p] ? (uh[p][e] - st.x) * st.y : 0.f;
+                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+                const float d = e < count[p] ? dx[p][e] * gate : 0.f;
+                const float v = fmaf(uh[p][e], w[e], b[e]);
+                sum[0][p][e] = fmaf(d, uh[p][e], sum[0][p][e]);
+                sum[1][p][e] += d;
+                da[e] = d * sc[e] * v * (1.f - gate);
+                s[2] += da[e];
+                gv[p][e] = d * sc[e] * w[e];
+                s[0] = fmaf(gv[p][e], uh[p][e], s[0]);
+                s[1] += gv[p][e];
+            }
+            if (g.dA && g.gate > 1) store_vec_part((T*)g.dA + i * g.ldda + c, from_floats<T>(da), count[p]);
+        }
+        store_dx();
+        if (!g.dU && g.gate != 1) continue;                      // (the same for all lanes)
+        if (g.w_post || g.gate == 1) join_lanes<L>(s, meet, turn);
+        if (g.dA && g.gate == 1 && li == 0) ((T*)g.dA)[i * g.ldda] = (T)s[2];
+        if (!g.dU) continue;
+        const float along = s[0] * inv_f, mean = g.layer ? s[1] * inv_f : 0.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (g.w_post)
+#pragma unroll
+                for (int e = 0; e < E; ++e) gv[p][e] = st.y * (gv[p][e] - fmaf(uh[p][e], along, mean));
+            store_vec_part((T*)g.dU + i * g.lddu + R::column(p), from_floats<T>(gv[p]), count[p]);
+        }
+    }
+    if (!g.part) return;
+    // the rows of the workgroup in order, one of the sums at a time
+    __shared__ float add[R::ROWS > 1 ? R::THREADS * E : 1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (g.at[k] < 0) continue;
+        float* const out = g.part + ((int64_t)blockIdx.x * g.sums + g.at[k]) * g.f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if constexpr (R::ROWS > 1) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < E; ++e) add[threadIdx.x * E + e] = sum[k][p][e];
+                __syncthreads();
+                if (threadIdx.x < L) {
+                    for (int r = 1; r < R::ROWS; ++r)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) sum[k][p][e] += add[(r * L + threadIdx.x) * E + e];
+                }
+            }
+            if (threadIdx.x < L) {
+                const int c = R::column(p);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (c + e < g.f) out[c + e] = sum[k][p][e];
+            }
+        }
+    }
+}
+
+// Rows longer than the registers hold: a workgroup reads its row again for every sum, from the caches.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_block_norm_long(NormArgs g) {
+    constexpr int E = Elem<T>::E, STEP = 1024 * E;
+    __shared__ float meet[2][16][4];
+    int turn = 0;
+    const float inv_f = 1.f / (float)g.f;
+    for (int64_t i = blockIdx.x; i < g.n; i += gridDim.x) {
+        const T* const X = (const T*)g.X + i * g.ldx;
+        const T* const U = g.U ? (const T*)g.U + i * g.ldu : nullptr;
+        const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
+        float umean = 0.f, urstd = 0.f, xmean = 0.f, xrstd = 0.f;
+        // each(value, column, elements there) for the thread's columns of U, then of X'
+        auto each_u = [&](auto f) {
+            for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
+                const int count = g.f - c < E ? (int)(g.f - c) : E;
+                float u[E];
+                to_floats<T>(load_vec_part(U + c, count), u);
+                f(u, c, count);
+            }
+        };
+        auto each_x = [&](auto f) {
+            for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
+                const int count = g.f - c < E ? (int)(g.f - c) : E;
+                float x[E];
+                to_floats<T>(load_vec_part(X + c, count), x);
+                if (U) {
+                    float u[E], w[E], b[E], sc[E], a[E];
+                    to_floats<T>(load_vec_part(U + c, count), u);
+                    load_floats<E>(g.scale, c, count, 1.f, sc);
+                    load_floats<E>(g.w_post, c, count, 1.f, w);
+                    load_floats<E>(g.b_post, c, count, 0.f, b);
+                    if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count), a);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float v = g.w_post ? fmaf((u[e] - umean) * urstd, w[e], b[e]) : u[e];
+                        x[e] = fmaf(sc[e] * (g.gate > 1 ? gate_of(a[e]) : row_gate), v, x[e]);
+                    }
+                }
+                f(x, c, count);
+            }
+        };
+        auto statistics = [&](auto each, float& mean, float& rstd) {
+            float s[1] = {0.f};
+            if (g.layer) {
+                each([&](float(&v)[E], int64_t, int count) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) s[0] += e < count ? v[e] : 0.f;
+                });
+                join_lanes<1024>(s, meet, turn);
+                mean = s[0] * inv_f;
+            }
+            s[0] = 0.f;
+            each([&](float(&v)[E], int64_t, int count) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float d = e < count ? v[e] - mean : 0.f;
+                    s[0] = fmaf(d, d, s[0]);
+                }
+            });
+            join_lanes<1024>(s, meet, turn);
+            rstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
+        };
+        if (U && g.w_post) statistics(each_u, umean, urstd);
+        if (g.H) statistics(each_x, xmean, xrstd);
+        each_x([&](float(&x)[E], int64_t c, int count) {          // what is written may take the place of what is read here
+            if (U && g.Xout) store_vec_part((T*)g.Xout + i * g.ldxo + c, from_floats<T>(x), count);
+            if (!g.H) return;
+            float w[E], b[E];
+            load_floats<E>(g.w_pre, c, count, 1.f, w);
+            load_floats<E>(g.b_pre, c, count, 0.f, b);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - xmean) * xrstd, w[e], b[e]);
+            store_vec_part((T*)g.H + i * g.ldh + c, from_floats<T>(x), count);
+        });
+        if (g.stats && threadIdx.x == 0) *reinterpret_cast<f4u*>(g.stats + 4 * i) = f4u{umean, urstd, xmean, xrstd};
+    }
+}
+
+// Likewise; a workgroup's sums over its rows grow in its partial results, where each thread has its own columns.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_block_norm_back_long(NormArgs g) {
+    constexpr int E = Elem<T>::E, STEP = 1024 * E;
+    __shared__ float meet[2][16][4];
+    int turn = 0;
+    const float inv_f = 1.f / (float)g.f;
+    for (int64_t i = blockIdx.x; i < g.n; i += gridDim.x) {
+        const bool first = i == (int64_t)blockIdx.x;
+        const f4u st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
+        const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
+        float along = 0.f, mean = 0.f;
+        auto grow = [&](int k, int64_t c, float v) {
+            if (g.at[k] < 0) return;
+            float* const p = g.part + ((int64_t)blockIdx.x * g.sums + g.at[k]) * g.f + c;
+            *p = first ? v : *p + v;
+        };
+        // dX of the thread's columns, and what goes into the sums over the row on the way
+        auto each = [&](auto f) {
+            for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
+                const int count = g.f - c < E ? (int)(g.f - c) : E;
+                float dx[E] = {}, xh[E] = {}, gh[E] = {}, w[E] = {};
+                if (g.dXout) to_floats<T>(load_vec_part((const T*)g.dXout + i * g.lddxo + c, count), dx);
+                if (g.dH) {
+                    to_floats<T>(load_vec_part((const T*)g.Xout + i * g.ldxo + c, count), xh);
+                    to_floats<T>(load_vec_part((const T*)g.dH + i * g.lddh + c, count), gh);
+                    load_floats<E>(g.w_pre, c, count, 1.f, w);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        xh[e] = e < count ? (xh[e] - st.z) * st.w : 0.f;
+                        dx[e] = fmaf(st.w, gh[e] * w[e] - fmaf(xh[e], along, mean), dx[e]);
+                    }
+                }
+                f(dx, xh, gh, w, c, count);
+            }
+        };
+        if (g.dH) {
+            float s[2] = {0.f, 0.f};
+            each([&](float(&)[E], float(&xh)[E], float(&gh)[E], float(&w)[E], int64_t, int count) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    s[0] = fmaf(gh[e] * w[e], xh[e], s[0]);
+                    s[1] += gh[e] * w[e];
+                }
+            });
+            join_lanes<1024>(s, meet, turn);
+            along = s[0] * inv_f;
+            mean = g.layer ? s[1] * inv_f : 0.f;
+        }
+        // the block's side, from dX of the same columns
+        auto block = [&](const float(&dx)[E], int64_t c, int count, float(&uh)[E], float(&d)[E], float(&da)[E], float(&gv)[E]) {
+            float w[E], b[E], sc[E], a[E];
+            load_floats<E>(g.scale, c, count, 1.f, sc);
+            load_floats<E>(g.w_post, c, count, 1.f, w);
+            load_floats<E>(g.b_post, c, count, 0.f, b);
+            to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count), uh);
+            if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count), a);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (g.w_post) uh[e] = e < count ? (uh[e] - st.x) * st.y : 0.f;
+                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+                d[e] = e < count ? dx[e] * gate : 0.f;
+                da[e] = d[e] * sc[e] * fmaf(uh[e], w[e], b[e]) * (1.f - gate);
+                gv[e] = d[e] * sc[e] * w[e];
+            }
+        };
+        float s[3] = {0.f, 0.f, 0.f};
+        if (g.U && (g.w_post || g.gate == 1)) {
+            each([&](float(&dx)[E], float(&)[E], float(&)[E], float(&)[E], int64_t c, int count) {
+                float uh[E], d[E], da[E], gv[E];
+                block(dx, c, count, uh, d, da, gv);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    s[0] = fmaf(gv[e], uh[e], s[0]);
+                    s[1] += gv[e];
+                    s[2] += da[e];
+                }
+            });
+            join_lanes<1024>(s, meet, turn);
+        }
+        const float ualong = s[0] * inv_f, umean = g.layer ? s[1] * inv_f : 0.f;
+        if (g.dA && g.gate == 1) {
+            __syncthreads();                                     // dA may take the place of A: all lanes have read the row's gate
+            if (threadIdx.x == 0) ((T*)g.dA)[i * g.ldda] = (T)s[2];
+        }
+        each([&](float(&dx)[E], float(&xh)[E], float(&gh)[E], float(&)[E], int64_t c, int count) {
+            float uh[E], d[E], da[E], gv[E];
+            if (g.U) block(dx, c, count, uh, d, da, gv);
+            for (int e = 0; e < count; ++e) {
+                grow(2, c + e, gh[e] * xh[e]);
+                grow(3, c + e, gh[e]);
+                if (!g.U) continue;
+                grow(0, c + e, d[e] * uh[e]);
+                grow(1, c + e, d[e]);
+            }
+            if (g.dX) store_vec_part((T*)g.dX + i * g.lddx + c, from_floats<T>(dx), count);
+            if (!g.U) return;
+            if (g.dA && g.gate > 1) store_vec_part((T*)g.dA + i * g.ldda + c, from_floats<T>(da), count);
+            if (!g.dU) return;
+            if (g.w_post)
+#pragma unroll
+                for (int e = 0; e < E; ++e) gv[e] = st.y * (gv[e] - fmaf(uh[e], ualong, umean));
+            store_vec_part((T*)g.dU + i * g.lddu + c, from_floats<T>(gv), count);
+        });
+    }
+}
+
+// The sums of the workgroups, added in order, and the vectors' gradients from them:
+//   dscale = w_post S0 + b_post S1, dw_post = scale S0, db_post = scale S1, dw_pre = S2, db_pre = S3
+struct NormVectors {
+    const float *scale, *w_post, *b_post;
+    float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
+};
+__global__ __launch_bounds__(1024) void k_block_norm_vectors(NormArgs g, int blocks, NormVectors v) {
+    __shared__ float s_sum[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float sum[4] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (g.at[k] < 0) continue;
+        __syncthreads();
+        if (c < g.f) s_sum[wave][lane] = strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, wave, 16, blocks);
+        __syncthreads();
+        if (wave == 0 && c < g.f)
+            for (int w = 0; w < 16; ++w) sum[k] += s_sum[w][lane];
+    }
+    if (wave != 0 || c >= g.f) return;
+    const float sc = v.scale ? v.scale[c] : 1.f;
+    if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], sum[0], v.b_post ? v.b_post[c] * sum[1] : 0.f) : sum[0];
+    if (v.dw_post) v.dw_post[c] = sc * sum[0];
+    if (v.db_post) v.db_post[c] = sc * sum[1];
+    if (v.dw_pre) v.dw_pre[c] = sum[2];
+    if (v.db_pre) v.db_pre[c] = sum[3];
+}
+
+__global__ __launch_bounds__(1024) void k_vector_sums(const float* __restrict__ part, int parts, int64_t count, float* __restrict__ out) {
+    __shared__ float s_sum[16][64];
+    sum_of_parts(blockIdx.x, 1, (int32_t)count, parts, 0, part, 16, s_sum, [&](int, int c, float s) { out[c] = s; });
+}
+
+int vector_sums_launch(const float* part, int parts, int64_t count, float* out, hipStream_t s) {
+    hipLaunchKernelGGL(k_vector_sums, dim3((unsigned)((count + 63) / 64)), dim3(1024), 0, s, part, parts, count, out);
+    GCN_LAUNCH_CHECK();
+    return GCN_OK;
+}
+
+// The fewest lanes that hold a row in one step, more steps where a workgroup's 1024 do not; f(lanes, steps), or f(0, 0) for longer rows than that.
+template <typename T, int MOST, typename F>
+static int by_row(int32_t f, const F& call) {
+    constexpr int E = Elem<T>::E;
+    const int64_t pieces = (f + E - 1) / E;
+#define GCN_LANES(L, P) if (pieces <= (int64_t)(L) * (P)) return call(std::integral_constant<int, L>(), std::integral_constant<int, P>())
+    GCN_LANES(4, 1); GCN_LANES(8, 1); GCN_LANES(16, 1); GCN_LANES(32, 1); GCN_LANES(64, 1); GCN_LANES(128, 1); GCN_LANES(256, 1);
+    GCN_LANES(512, 1); GCN_LANES(1024, 1);
+    if constexpr (MOST >= 2) GCN_LANES(1024, 2);
+#undef GCN_LANES
+    return call(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
+}
+
+template <typename T>
+static int norm_forward(const NormArgs& g, hipStream_t s) {
+    return by_row<T, 2>(g.f, [&](auto l, auto p) -> int {
+        constexpr int L = decltype(l)::value, P = decltype(p)::value;
+        const int64_t most = 16LL * device_info().cus;
+        if constexpr (L == 0) {
+            hipLaunchKernelGGL((k_block_norm_long<T>), dim3((unsigned)(g.n < most ? g.n : most)), dim3(1024), 0, s, g);
+        } else {
+            using R = Rows<T, L, P>;
+            const int64_t groups = (g.n + R::ROWS - 1) / R::ROWS;
+            hipLaunchKernelGGL((k_block_norm<T, L, P>), dim3((unsigned)(groups < most ? groups : most)), dim3(R::THREADS), 0, s, g);
+        }
+        GCN_LAUNCH_CHECK();
+        return GCN_OK;
+    });
+}
+
+template <typename T>
+static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
+    return by_row<T, 1>(g.f, [&](auto l, auto p) -> int {
+        constexpr int L = decltype(l)::value, P = decltype(p)::value;
+        int64_t groups = g.n, most = device_info().cus;
+        if constexpr (L != 0) {
+            using R = Rows<T, L, P>;
+            groups = (g.n + R::ROWS - 1) / R::ROWS;
+            most *= 2048 / R::THREADS;
+        }
+        const int blocks = (int)(groups < most ? groups : most);
+        ScratchLease lease;
+        if (g.sums) {
+            void* mem = nullptr;
+            GCN_TRY(lease.get(&mem, (size_t)blocks * g.sums * g.f * 4, s));
+            g.part = (float*)mem;
+        }
+        if constexpr (L == 0) hipLaunchKernelGGL((k_block_norm_back_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, g);
+        else hipLaunchKernelGGL((k_block_norm_back<T, L, P>), dim3((unsigned)blocks), dim3(Rows<T, L, P>::THREADS), 0, s, g);
+        GCN_LAUNCH_CHECK();
+        if (g.sums) {
+            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)((g.f + 63) / 64)), dim3(1024), 0, s, g, blocks, v);
+            GCN_LAUNCH_CHECK();
+        }
+        return GCN_OK;
+    });
+}
+
+}  // namespace gcn
+
+using namespace gcn;
+
+// Whether outputs overlap inputs or each other otherwise than element by element: an output of the rows' size may be an input of that size
+// (same address and leading dimension).
+struct Place {
+    const void* p;
+    int64_t cols, ld;
+};
+static bool misplaced(int64_t n, int32_t f, size_t b, std::initializer_list<Place> in, std::initializer_list<Place> out,
+                      std::initializer_list<const void*> vectors_in, std::initializer_list<const void*> vectors_out, const void* stats, bool stats_out) {
+    auto span = [&](const Place& x) { return Span(x.p, n, x.cols, x.ld, b); };
+    const Span st(stats, n, 4, 4, 4);
+    for (const Place* o = out.begin(); o != out.end(); ++o) {
+        for (const Place& i : in)
+            if (span(*o).meets(span(i)) && !(o->p == i.p && o->ld == i.ld && o->cols == i.cols)) return true;
+        for (const Place* q = out.begin(); q != o; ++q)
+            if (span(*o).meets(span(*q))) return true;
+        for (const void* v : vectors_in)
+            if (span(*o).meets(Span(v, 1, f, f, 4))) return true;
+        for (const void* v : vectors_out)
+            if (span(*o).meets(Span(v, 1, f, f, 4))) return true;
+        if (span(*o).meets(st)) return true;
+    }
+    for (const void* const* o = vectors_out.begin(); o != vectors_out.end(); ++o) {
+        const Span v(*o, 1, f, f, 4);
+        for (const Place& i : in)
+            if (v.meets(span(i))) return true;
+        for (const void* x : vectors_in)
+            if (v.meets(Span(x, 1, f, f, 4))) return true;
+        for (const void* const* q = vectors_out.begin(); q != o; ++q)
+            if (v.meets(Span(*q, 1, f, f, 4))) return true;
+        if (v.meets(st)) return true;
+    }
+    if (stats_out) {
+        for (const Place& i : in)
+            if (st.meets(span(i))) return true;
+        for (const void* v : vectors_in)
+            if (st.meets(Span(v, 1, f, f, 4))) return true;
+    }
+    return false;
+}
+
+static int norm_checks(const char* who, int64_t n, int32_t f, int type, int kind, int32_t gate_cols, const void* A, int64_t lda) {
+    if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
+    if (kind != GCN_NORM_RMS && kind != GCN_NORM_LAYER) return fail(GCN_ERR_BADARG, "%s: unknown norm %d", who, kind);
+    if (n <= 0 || f <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (A && gate_cols != 1 && gate_cols != f) return fail(GCN_ERR_BADARG, "%s: the gate has 1 or f columns", who);
+    if (A && lda < gate_cols) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    return GCN_OK;
+}
+
+extern "C" int gcn_block_norm_forward(int64_t n, int32_t f, int type, int kind, float eps, const void* X, int64_t ldx, const void* U,
+                                      int64_t ldu, const void* A, int32_t gate_cols, int64_t lda, const float* scale, const float* w_post,
+                                      const float* b_post, const float* w_pre, const float* b_pre, void* Xout, int64_t ldxo, void* H,
+                                      int64_t ldh, float* stats, void* stream) {
+    static const char* const who = "gcn_block_norm_forward";
+    GCN_TRY(norm_checks(who, n, f, type, kind, gate_cols, A, lda));
+    if (!X || (!H && !(U && Xout))) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!U && (A || scale || w_post || b_post || Xout)) return fail(GCN_ERR_BADARG, "%s: a gate, a scale, a post-norm and X' need U", who);
+    if (b_post && !w_post) return fail(GCN_ERR_BADARG, "%s: b_post without w_post", who);
+    if ((H && !w_pre) || (!H && (w_pre || b_pre))) return fail(GCN_ERR_BADARG, "%s: H and w_pre go together", who);
+    if (!(eps >= 0.f)) return fail(GCN_ERR_BADARG, "%s: eps must not be negative", who);
+    if (ldx < f || (U && ldu < f) || (Xout && ldxo < f) || (H && ldh < f))
+        return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    if (misplaced(n, f, elem_bytes(type), {{X, f, ldx}, {U, f, ldu}, {A, gate_cols, lda}}, {{Xout, f, ldxo}, {H, f, ldh}},
+                  {scale, w_post, b_post, w_pre, b_pre}, {}, stats, true))
+        return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    NormArgs g;
+    g.n = n; g.f = f; g.layer = kind == GCN_NORM_LAYER; g.eps = eps; g.gate = A ? (gate_cols == f && f > 1 ? f : 1) : 0;
+    g.X = X; g.ldx = ldx; g.U = U; g.ldu = ldu; g.A = A; g.lda = lda; g.scale = scale; g.w_post = w_post; g.b_post = b_post;
+    g.w_pre = w_pre; g.b_pre = b_pre; g.Xout = Xout; g.ldxo = ldxo; g.H = H; g.ldh = ldh; g.stats = stats;
+    return by_type(type, [&](auto t) { return norm_forward<decltype(t)>(g, (hipStream_t)stream); });
+}
+
+extern "C" int gcn_block_norm_backward(int64_t n, int32_t f, int type, int kind, const void* U, int64_t ldu, const void* A,
+                                       int32_t gate_cols, int64_t lda, const float* scale, const float* w_post, const float* b_post,
+                                       const float* w_pre, const void* Xout, int64_t ldxo, const float* stats, const void* dXout,
+                                       int64_t lddxo, const void* dH, int64_t lddh, void* dX, int64_t lddx, void* dU, int64_t lddu,
+                                       void* dA, int64_t ldda, float* dscale, float* dw_post, float* db_post, float* dw_pre, float* db_pre,
+                                       void* stream) {
+    static const char* const who = "gcn_block_norm_backward";
+    GCN_TRY(norm_checks(who, n, f, type, kind, gate_cols, A, lda));
+    if ((!dXout && !dH) || !stats) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!U && (A || scale || w_post || b_post || dU || dA || dscale || dw_post || db_post))
+        return fail(GCN_ERR_BADARG, "%s: a gate, a scale, a post-norm and their gradients need U", who);
+    if (b_post && !w_post) return fail(GCN_ERR_BADARG, "%s: b_post without w_post", who);
+    if (dH && (!w_pre || !Xout)) return fail(GCN_ERR_BADARG, "%s: dH needs w_pre and X'", who);
+    if (!dH && (dw_pre || db_pre)) return fail(GCN_ERR_BADARG, "%s: the pre-norm's gradients need dH", who);
+    if ((dA && !A) || (dw_post && !w_post) || (db_post && !w_post))
+        return fail(GCN_ERR_BADARG, "%s: the gradient of an operand that is not there", who);
+    if ((U && ldu < f) || (dH && (ldxo < f || lddh < f)) || (dXout && lddxo < f) || (dX && lddx < f) || (dU && lddu < f) || (dA && ldda < gate_cols))
+        return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    if (misplaced(n, f, elem_bytes(type), {{U, f, ldu}, {A, gate_cols, lda}, {dH ? Xout : nullptr, f, ldxo}, {dXout, f, lddxo}, {dH, f, lddh}},
+                  {{dX, f, lddx}, {dU, f, lddu}, {dA, gate_cols, ldda}}, {scale, w_post, b_post, w_pre},
+                  {dscale, dw_post, db_post, dw_pre, db_pre}, stats, false))
+        return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    NormArgs g;
+    g.n = n; g.f = f; g.layer = kind == GCN_NORM_LAYER; g.gate = A ? (gate_cols == f && f > 1 ? f : 1) : 0;
+    g.U = U; g.ldu = ldu; g.A = A; g.lda = lda; g.scale = scale; g.w_post = w_post; g.b_post = b_post; g.w_pre = w_pre;
+    g.Xout = const_cast<void*>(Xout); g.ldxo = ldxo; g.stats = const_cast<float*>(stats); g.dXout = dXout; g.lddxo = lddxo; g.dH = dH; g.lddh = lddh;
+    g.dX = dX; g.lddx = lddx; g.dU = dU; g.lddu = lddu; g.dA = dA; g.ldda = ldda;
+    const bool want[4] = {dscale || dw_post, (dscale && b_post) || db_post, dw_pre != nullptr, db_pre != nullptr};
+    for (int k = 0; k < 4; ++k)
+        if (want[k]) g.at[k] = g.sums++;
+    const NormVectors v{scale, w_post, b_post, dscale, dw_post, db_post, dw_pre, db_pre};
+    return by_type(type, [&](auto t) { return norm_backward<decltype(t)>(g, v, (hipStream_t)stream); });
+}

@@ -1,0 +1,238 @@
+// Distillation from a teacher's largest logits: with S the entries of a row's list (index >= 0, logit above -inf), p = softmax over S of t / T and
+// q = softmax over all classes of z / T,
+//   loss = 1/m sum over rows [ wt T^2 sum over S of p (log p - log q) - wl log softmax(z)_y ]
+//   G    = 1/m [ wt T (q - p) where S is not empty, + wl (softmax(z) - onehot(y)) where y >= 0 ]
+// A row is read once, held in registers in its own type, and its gradient written once.
+#include <type_traits>
+
+#include "rows.h"
+#include "sum_parts.h"
+
+namespace gcn {
+
+struct DistillArgs {
+    int64_t n = 0;
+    int32_t C = 0, k = 0;
+    const void* Z = nullptr;
+    void* G = nullptr;
+    int64_t ldz = 0, ldg = 0, ldtop = 0, ldt = 0;
+    const int32_t* top = nullptr;
+    const void* t = nullptr;
+    const int32_t* labels = nullptr;
+    float inv_T = 1, wt = 0, wl = 0;          // wt, wl: of the loss
+    float gt = 0, gl = 0;                     // of the gradient: grad_scale / m times wt T and wl
+    double* part = nullptr;
+};
+
+// exp of 32-bit elements by the function, of 16-bit ones by the instruction that raises 2 to a power: its error, 2^-22 of the result times the argument,
+// is far below the rounding of such a gradient.
+template <typename T>
+__device__ __forceinline__ float exp_of(float x) {
+    return sizeof(T) == 4 ? expf(x) : __expf(x);
+}
+// e^(z - high) from et = e^((z - high) / T): powers of it at the temperatures 1, 2 and 4 (POWER), else a second exponential.
+template <typename T, int POWER>
+__device__ __forceinline__ float plain_exp(float et, float z, float high) {
+    if (POWER == 1) return et;
+    if (POWER == 2) return et * et;
+    if (POWER == 4) return (et * et) * (et * et);
+    return exp_of<T>(z - high);
+}
+
+// P = 0: rows longer than the registers hold are read again for each step, from the caches.
+template <typename T, int L, int P, int POWER>
+__global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_distill(DistillArgs a) {
+    using R = Rows<T, L, P>;
+    constexpr int E = R::E;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    __shared__ float meet[2][16][4];
+    __shared__ double s_w[16];
+    int turn = 0;
+    const int li = threadIdx.x % L;
+    // the row's list: index (-1: none), logit of the student, p
+    int32_t* const l_at = (int32_t*)lds + (int64_t)(threadIdx.x / L) * 3 * a.k;
+    float* const l_z = (float*)(l_at + a.k);
+    float* const l_p = l_z + a.k;
+    double mine = 0.0;
+    auto lanes_meet = [&]() {                                    // what the row's lanes have written, to LDS or to G, comes before what follows
+        if constexpr (L > 64) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < a.n; i += (int64_t)gridDim.x * R::ROWS) {
+        const T* const z = (const T*)a.Z + i * a.ldz;
+        Vec<T> held[P ? P : 1];
+        int count[P ? P : 1];
+        // f(elements, column, elements there) for the lane's pieces of the row
+        auto each = [&](auto f) {
+            if constexpr (P != 0) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) f(held[p], R::column(p), count[p]);
+            } else {
+                for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) {
+                    const int there = a.C - c < E ? (int)(a.C - c) : E;
+                    f(load_vec_part(z + c, there), (int)c, there);
+                }
+            }
+        };
+        if constexpr (P != 0) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                count[p] = R::there(R::column(p), a.C);
+                held[p] = load_vec_part(z + R::column(p), count[p]);
+            }
+        }
+        const int32_t y = a.labels ? a.labels[i] : -1;
+        const bool labelled = y >= 0 && y < a.C;
+        // the list, and the maxima of both sides
+        float high[3] = {-INFINITY, -INFINITY, 0.f};             // of z, of t, whether there is an entry
+        for (int j = li; j < a.k; j += L) {
+            int32_t at = a.top[i * a.ldtop + j];
+            const float t = (float)((const T*)a.t)[i * a.ldt + j];
+            if (at >= a.C || t == -INFINITY) at = -1;
+            l_at[j] = at;
+            l_p[j] = t;
+            if (at < 0) continue;
+            l_z[j] = (float)z[at];
+            high[1] = fmaxf(high[1], t);
+            high[2] = 1.f;
+        }
+        each([&](Vec<T> v, int, int there) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) high[0] = e < there ? fmaxf(high[0], (float)v[e]) : high[0];
+        });
+        join_lanes<L, 3, 3>(high, meet, turn);
+        const bool taught = high[2] > 0.f;
+        const float zh = high[0], th = high[1];
+        float sum[3] = {0.f, 0.f, 0.f};                          // of e^((z - zh) / T), of e^(z - zh), of the list's e^((t - th) / T)
+        each([&](Vec<T> v, int, int there) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float x = (float)v[e];
+                const float et = exp_of<T>((x - zh) * a.inv_T);
+                sum[0] += e < there ? et : 0.f;
+                if (POWER != 1 && labelled) sum[1] += e < there ? plain_exp<T, POWER>(et, x, zh) : 0.f;
+            }
+        });
+        for (int j = li; j < a.k; j += L)
+            if (l_at[j] >= 0) sum[2] += expf((l_p[j] - th) * a.inv_T);
+        join_lanes<L, 3>(sum, meet, turn);
+        if (POWER == 1) sum[1] = sum[0];
+        const float logt = logf(sum[0]), logl = logf(sum[2]);
+        for (int j = li; j < a.k; j += L) {
+            if (l_at[j] < 0) continue;
+            const float x = (l_p[j] - th) * a.inv_T, p = expf(x) / sum[2];
+            const float logq = (l_z[j] - zh) * a.inv_T - logt;
+            if (p != 0.f) mine += (double)(a.wt * p) * (double)((x - logl) - logq);
+            l_p[j] = p;
+        }
+        if (labelled && li == 0) mine -= (double)a.wl * (double)(((float)z[y] - zh) - logf(sum[1]));
+        if (!a.G) {
+            lanes_meet();                                        // the list is written anew
+            continue;
+        }
+        lanes_meet();                                            // all of the list is there, and z[y] read where G takes the place of Z
+        T* const G = (T*)a.G + i * a.ldg;
+        const float ct = taught ? a.gt / sum[0] : 0.f, cl = labelled ? a.gl / sum[1] : 0.f;
+        // `et` and `el` may be NaN where a row is neither taught nor labelled: chosen, not multiplied away
+        auto gradient = [&](float x, int c) {
+            const float et = exp_of<T>((x - zh) * a.inv_T);
+            float g = taught ? ct * et : 0.f;
+            if (labelled) g += cl * plain_exp<T, POWER>(et, x, zh) - (c == y ? a.gl : 0.f);
+            return g;
+        };
+        each([&](Vec<T> v, int c, int there) {
+            Vec<T> out;
+#pragma unroll
+            for (int e = 0; e < E; ++e) out[e] = (T)gradient((float)v[e], c + e);
+            store_vec_part(G + c, out, there);
+        });
+        lanes_meet();                                            // the list's columns are written again, by other lanes
+        for (int j = li; j < a.k; j += L) {
+            const int32_t at = l_at[j];
+            if (at < 0) continue;
+            float p = 0.f;                                       // of all entries that name this column
+            for (int o = 0; o < a.k; ++o) p += l_at[o] == at ? l_p[o] : 0.f;
+            G[at] = (T)(gradient(l_z[j], at) - a.gt * p);
+        }
+        lanes_meet();
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) mine += __shfl_xor(mine, d, 64);
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double total = s_w[0];
+        for (int w = 1; w < R::THREADS / 64; ++w) total += s_w[w];
+        a.part[blockIdx.x] = total;
+    }
+}
+
+__global__ __launch_bounds__(256) void k_distill_loss(int64_t parts, const double* __restrict__ part, double inv_m, float* __restrict__ loss) {
+    __shared__ double s[256];
+    sum_of_losses(part, parts, inv_m, loss, s);
+}
+
+template <typename T>
+static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream_t s) {
+    auto launch = [&](auto l, auto p, auto power) -> int {
+        constexpr int L = decltype(l)::value, P = decltype(p)::value;
+        using R = Rows<T, L, P>;
+        const int64_t groups = (a.n + R::ROWS - 1) / R::ROWS, most = (int64_t)device_info().cus * (2048 / R::THREADS);
+        const int blocks = (int)(groups < most ? groups : most);
+        ScratchLease lease;
+        void* part = nullptr;
+        GCN_TRY(lease.get(&part, (size_t)blocks * 8, s));
+        a.part = (double*)part;
+        launch_lds<k_distill<T, L, P, decltype(power)::value>>(dim3((unsigned)blocks), R::THREADS, (size_t)R::ROWS * a.k * 12, s, a);
+        GCN_LAUNCH_CHECK();
+        hipLaunchKernelGGL(k_distill_loss, dim3(1), dim3(256), 0, s, (int64_t)blocks, (const double*)part, 1.0 / (double)m, loss);
+        GCN_LAUNCH_CHECK();
+        return GCN_OK;
+    };
+    auto with = [&](auto l, auto p) -> int {
+        if (T_ == 1.f) return launch(l, p, std::integral_constant<int, 1>());
+        if (T_ == 2.f) return launch(l, p, std::integral_constant<int, 2>());
+        if (T_ == 4.f) return launch(l, p, std::integral_constant<int, 4>());
+        return launch(l, p, std::integral_constant<int, 0>());
+    };
+    const int64_t pieces = (a.C + Elem<T>::E - 1) / Elem<T>::E;
+#define GCN_LANES(L, P) if (pieces <= (int64_t)(L) * (P)) return with(std::integral_constant<int, L>(), std::integral_constant<int, P>())
+    GCN_LANES(4, 1); GCN_LANES(16, 1); GCN_LANES(64, 1); GCN_LANES(64, 4); GCN_LANES(256, 4); GCN_LANES(1024, 4); GCN_LANES(1024, 16);
+#undef GCN_LANES
+    return with(std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
+}
+
+}  // namespace gcn
+
+using namespace gcn;
+
+extern "C" int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_t ldz, int32_t k, const int32_t* top, int64_t ldtop,
+                           const void* t, int64_t ldt, const int32_t* labels, float temperature, float w_teacher, float w_label,
+                           int64_t m, float grad_scale, float* loss, void* G, int64_t ldg, void* stream) {
+    static const char* const who = "gcn_distill";
+    if (!Z || !top || !t || !loss) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
+    if (n <= 0 || C <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (k <= 0 || k > C || k > GCN_DISTILL_MOST) return fail(GCN_ERR_BADARG, "%s: a list has 1 to %d entries, and no more than there are classes", who, GCN_DISTILL_MOST);
+    if (ldz < C || ldtop < k || ldt < k || (G && ldg < C)) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(GCN_ERR_BADARG, "%s: the temperature must be positive", who);
+    if (m <= 0) return fail(GCN_ERR_BADARG, "%s: m must be positive", who);
+    const size_t b = elem_bytes(type);
+    const Span z(Z, n, C, ldz, b), g(G, n, C, ldg, b), at(top, n, k, ldtop, 4), tt(t, n, k, ldt, b), y(labels, 1, n, n, 4), l(loss, 1, 1, 1, 4);
+    if ((g.meets(z) && (G != Z || ldg != ldz)) || g.meets(at) || g.meets(tt) || g.meets(y) || l.meets(z) || l.meets(g) || l.meets(at) || l.meets(tt) || l.meets(y))
+        return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    DistillArgs a;
+    a.n = n; a.C = C; a.k = k; a.Z = Z; a.ldz = ldz; a.G = G; a.ldg = ldg; a.top = top; a.ldtop = ldtop; a.t = t; a.ldt = ldt;
+    a.labels = w_label != 0.f ? labels : nullptr;
+    a.inv_T = 1.f / temperature;
+    a.wt = w_teacher * temperature * temperature;
+    a.wl = w_label;
+    const double scale = (double)grad_scale / (double)m;
+    a.gt = (float)(scale * w_teacher * temperature);
+    a.gl = (float)(scale * w_label);
+    return by_type(type, [&](auto e) { return distill_of<decltype(e)>(a, m, temperature, loss, (hipStream_t)stream); });
+}

@@ -1,0 +1,92 @@
+// Elements of 32 and 16 bits: 16 bytes of them at a time, at any address that the type itself is aligned for, and as floats.
+#pragma once
+#include "common.h"
+
+namespace gcn {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+    static constexpr int TYPE = GCN_F32, E = 4;                  // E: elements of 16 bytes
+    typedef float V __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(4))) Loose { uint32_t w[4]; };
+    struct __attribute__((packed, aligned(4))) Loose4 { uint32_t w[4]; };   // four elements
+};
+template <> struct Elem<__bf16> {
+    static constexpr int TYPE = GCN_BF16, E = 8;
+    typedef __bf16 V __attribute__((ext_vector_type(8)));
+    struct __attribute__((packed, aligned(2))) Loose { uint32_t w[4]; };
+    struct __attribute__((packed, aligned(2))) Loose4 { uint32_t w[2]; };
+};
+template <> struct Elem<_Float16> {
+    static constexpr int TYPE = GCN_F16, E = 8;
+    typedef _Float16 V __attribute__((ext_vector_type(8)));
+    struct __attribute__((packed, aligned(2))) Loose { uint32_t w[4]; };
+    struct __attribute__((packed, aligned(2))) Loose4 { uint32_t w[2]; };
+};
+template <typename T> using Vec = typename Elem<T>::V;
+template <typename T> using Vec4 = T __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ Vec<T> load_vec(const T* p) {
+    return __builtin_bit_cast(Vec<T>, *reinterpret_cast<const typename Elem<T>::Loose*>(p));
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(T* p, Vec<T> v) {
+    *reinterpret_cast<typename Elem<T>::Loose*>(p) = __builtin_bit_cast(typename Elem<T>::Loose, v);
+}
+template <typename T>
+__device__ __forceinline__ v4f load4(const T* p) {
+    return __builtin_convertvector(__builtin_bit_cast(Vec4<T>, *reinterpret_cast<const typename Elem<T>::Loose4*>(p)), v4f);
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, v4f v) {             // rounds to nearest, ties to even
+    *reinterpret_cast<typename Elem<T>::Loose4*>(p) = __builtin_bit_cast(typename Elem<T>::Loose4, __builtin_convertvector(v, Vec4<T>));
+}
+// The first `count` elements of 16 bytes; the others are zero.
+template <typename T>
+__device__ __forceinline__ Vec<T> load_vec_part(const T* p, int count) {
+    if (count >= Elem<T>::E) return load_vec(p);
+    Vec<T> v = {};
+#pragma unroll
+    for (int e = 0; e < Elem<T>::E; ++e)
+        if (e < count) v[e] = p[e];
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_vec_part(T* p, Vec<T> v, int count) {
+    if (count >= Elem<T>::E) {
+        store_vec(p, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < Elem<T>::E; ++e)
+        if (e < count) p[e] = v[e];
+}
+
+inline size_t elem_bytes(int type) { return type == GCN_F32 ? 4 : 2; }
+// Calls f with a value of the element type.
+template <typename F>
+int by_type(int type, const F& f) {
+    if (type == GCN_F32) return f(float());
+    if (type == GCN_BF16) return f(__bf16());
+    return f(_Float16());
+}
+inline bool known_type(int type) { return type == GCN_F32 || type == GCN_BF16 || type == GCN_F16; }
+
+// Rows of `cols` elements of `bytes` each, `ld` apart, as a range of addresses.
+struct Span {
+    uintptr_t from = 0, to = 0;
+    Span(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t bytes) {
+        if (!p || rows <= 0) return;
+        from = (uintptr_t)p;
+        to = from + ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * bytes;
+    }
+    bool meets(const Span& o) const { return from < o.to && o.from < to; }
+};
+
+// `group`s of 64 results, each the sum of `parts` partial results in a fixed order (see sum_of_parts).
+int vector_sums_launch(const float* part, int parts, int64_t count, float* out, hipStream_t s);
+
+}  // namespace gcn

@@ -1,0 +1,146 @@
+// A linear layer with what follows it: Y = rho R + act(X W + 1 bias^T), and its gradients, on 32- and 16-bit elements.
+#include "linear_tile.h"
+
+namespace gcn {
+
+// dZ = dY * act'(Z), dR = rho dY, and the column sums of dZ (the bias gradient, of the unrounded products): one pass over the matrices for the elementwise
+// part.  A workgroup has 64 lanes of four columns by four rows at a time, and a share of the rows; the four row sets are added in order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int64_t rows_per_block, const T* Z, int64_t ldz,
+                                                      const T* dY, int64_t lddy, int act, float rho, T* dZ, int64_t lddz, T* dR,
+                                                      int64_t lddr, float* __restrict__ part) {
+    __shared__ v4f sums[4][64];
+    const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.y * 64 + lane) * 4;
+    const int64_t rb = (int64_t)blockIdx.x * rows_per_block, re = rb + rows_per_block < n ? rb + rows_per_block : n;
+    const int64_t count = N - c;
+    v4f sum = {};
+    if (count >= 4) {
+        for (int64_t i = rb + set; i < re; i += 4) {
+            const v4f g = load4(dY + i * lddy + c);
+            v4f d = g;
+            if (act != GCN_ACT_NONE) {
+                const v4f z = load4(Z + i * ldz + c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] *= slope_of(z[e], act);
+                if (dZ) store4(dZ + i * lddz + c, d);
+            }
+            if (dR) store4(dR + i * lddr + c, g * rho);
+            sum += d;
+        }
+    } else if (count > 0) {
+        for (int64_t i = rb + set; i < re; i += 4)
+            for (int e = 0; e < count; ++e) {
+                const float g = (float)dY[i * lddy + c + e];
+                float d = g;
+                if (act != GCN_ACT_NONE) {
+                    d *= slope_of((float)Z[i * ldz + c + e], act);
+                    if (dZ) dZ[i * lddz + c + e] = (T)d;
+                }
+                if (dR) dR[i * lddr + c + e] = (T)(g * rho);
+                sum[e] += d;
+            }
+    }
+    if (!part) return;
+    sums[set][lane] = sum;
+    __syncthreads();
+    if (set) return;
+    for (int w = 1; w < 4; ++w) sum += sums[w][lane];
+    for (int e = 0; e < 4 && e < count; ++e) part[(int64_t)blockIdx.x * N + c + e] = sum[e];
+}
+
+template <typename T>
+static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho, void* dZ,
+                        int64_t lddz, void* dR, int64_t lddr, float* dbias, hipStream_t s) {
+    const int64_t across = ((int64_t)N + 255) / 256;
+    int64_t blocks = (8LL * device_info().cus + across - 1) / across;
+    if (blocks > (n + 15) / 16) blocks = (n + 15) / 16;
+    if (blocks > 1024) blocks = 1024;
+    const int64_t per = ((n + blocks - 1) / blocks + 3) / 4 * 4;
+    blocks = (n + per - 1) / per;
+    ScratchLease lease;
+    void* part = nullptr;
+    if (dbias) GCN_TRY(lease.get(&part, (size_t)blocks * N * 4, s));
+    hipLaunchKernelGGL(k_linear_slope<T>, dim3((unsigned)blocks, (unsigned)across), dim3(256), 0, s, n, N, per, (const T*)Z, ldz,
+                       (const T*)dY, lddy, act, rho, (T*)dZ, lddz, (T*)dR, lddr, (float*)part);
+    GCN_LAUNCH_CHECK();
+    if (dbias) return vector_sums_launch((const float*)part, (int)blocks, N, dbias, s);
+    return GCN_OK;
+}
+
+}  // namespace gcn
+
+using namespace gcn;
+
+static bool known_act(int act) { return act >= GCN_ACT_NONE && act <= GCN_ACT_SILU; }
+
+extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W,
+                                  int64_t ldw, const float* bias, int act, const void* R, int64_t ldr, float rho, void* Z,
+                                  int64_t ldz, void* Y, int64_t ldy, void* stream) {
+    static const char* const who = "gcn_linear_forward";
+    if (!X || !W || !Y) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
+    if (!known_act(act)) return fail(GCN_ERR_BADARG, "%s: unknown activation %d", who, act);
+    if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (ldx < f_in || ldw < f_out || ldy < f_out || (R && ldr < f_out) || (Z && ldz < f_out))
+        return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    const size_t b = elem_bytes(type);
+    const Span x(X, n, f_in, ldx, b), w(W, f_in, f_out, ldw, b), y(Y, n, f_out, ldy, b), z(Z, n, f_out, ldz, b), r(R, n, f_out, ldr, b);
+    const Span v(bias, 1, f_out, f_out, 4);
+    if (y.meets(x) || y.meets(w) || z.meets(x) || z.meets(w) || z.meets(y) || z.meets(r) || y.meets(v) || z.meets(v) || (y.meets(r) && (R != Y || ldr != ldy)))
+        return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    TileArgs a;
+    a.A = X; a.lda = ldx; a.B = W; a.ldb = ldw; a.M = n; a.N = f_out; a.K = f_in;
+    a.bias = bias; a.act = act; a.R = R; a.ldr = ldr; a.rho = rho; a.Z = Z; a.ldz = ldz; a.Y = Y; a.ldy = ldy;
+    return by_type(type, [&](auto t) { return linear_forward_of<decltype(t)>(a, (hipStream_t)stream); });
+}
+
+extern "C" int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W,
+                                   int64_t ldw, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho, void* dZ,
+                                   int64_t lddz, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias, void* dR, int64_t lddr,
+                                   void* stream) {
+    static const char* const who = "gcn_linear_backward";
+    const hipStream_t s = (hipStream_t)stream;
+    if (!dY || (dW && !X) || (dX && !W)) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
+    if (!known_act(act)) return fail(GCN_ERR_BADARG, "%s: unknown activation %d", who, act);
+    const bool curved = act != GCN_ACT_NONE, products = dX || dW;
+    if (curved && (products || dbias || dZ) && !Z) return fail(GCN_ERR_BADARG, "%s: the activation's derivative needs Z", who);
+    if (curved && products && !dZ) return fail(GCN_ERR_BADARG, "%s: the products need dZ as workspace", who);
+    if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (lddy < f_out || (X && ldx < f_in) || (W && ldw < f_out) || (Z && ldz < f_out) || (dZ && lddz < f_out) || (dX && lddx < f_in) ||
+        (dW && lddw < f_out) || (dR && lddr < f_out))
+        return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    const size_t b = elem_bytes(type);
+    if (!curved) dZ = nullptr;
+    const Span in[] = {Span(X, n, f_in, ldx, b), Span(W, f_in, f_out, ldw, b), Span(curved ? Z : nullptr, n, f_out, ldz, b), Span(dY, n, f_out, lddy, b)};
+    const Span out[] = {Span(dZ, n, f_out, lddz, b), Span(dR, n, f_out, lddr, b), Span(dX, n, f_in, lddx, b), Span(dW, f_in, f_out, lddw, b), Span(dbias, 1, f_out, f_out, 4)};
+    bool bad = false;
+    for (int o = 0; o < 5; ++o) {
+        for (int i = 0; i < 4; ++i) {
+            // an element of dZ may take the place of the one of Z or dY that it is made of, one of dR that of dY
+            const bool same = (o == 0 && i == 2 && dZ == Z && lddz == ldz) || (o == 0 && i == 3 && dZ == dY && lddz == lddy) ||
+                              (o == 1 && i == 3 && dR == dY && lddr == lddy && (curved || !products));
+            bad |= out[o].meets(in[i]) && !same;
+        }
+        for (int i = 0; i < o; ++i) bad |= out[o].meets(out[i]);
+    }
+    if (bad) return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    return by_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        if (dbias || dR || dZ)
+            GCN_TRY(slope_launch<T>(n, f_out, Z, ldz, dY, lddy, dbias || dZ ? act : GCN_ACT_NONE, rho, dZ, lddz, dR, lddr, dbias, s));
+        const void* const G = curved ? dZ : dY;
+        const int64_t ldg = curved ? lddz : lddy;
+        TileArgs a;
+        if (dX) {
+            a.A = G; a.lda = ldg; a.B = W; a.ldb = ldw; a.M = n; a.N = f_in; a.K = f_out; a.Y = dX; a.ldy = lddx;
+            GCN_TRY(linear_dx_of<T>(a, s));
+        }
+        if (dW) {
+            a.A = X; a.lda = ldx; a.B = G; a.ldb = ldg; a.M = f_in; a.N = f_out; a.K = n; a.Y = dW; a.ldy = lddw;
+            GCN_TRY(linear_dw_of<T>(a, s));
+        }
+        return GCN_OK;
+    });
+}

@@ -1,0 +1,330 @@
+// Tiles of a matrix product for the matrix units: D (M x N) = A (M x K) B (K x N), of 32- or 16-bit elements, sums in 32 bits, with what a linear
+// layer does to its result where a tile leaves.  One kernel serves the three products of a layer and its backward pass, which differ in which of
+// their dimensions lies contiguous in memory:
+//   forward  X W      A by k, B by n
+//   dX       dZ W^T   A by k, B by k   (the stored W is N x K)
+//   dW       X^T dZ   A by m, B by n   (the stored X is K x M)
+#pragma once
+#include "elem.h"
+
+namespace gcn {
+
+enum Lies { BY_K = 0, BY_MN = 1 };
+
+struct TileArgs {
+    const void* A = nullptr;
+    const void* B = nullptr;
+    int64_t lda = 0, ldb = 0;
+    int64_t M = 0, K = 0;
+    int64_t k_share = 0;          // of one split: a multiple of the tile's depth
+    int32_t N = 0;
+    int32_t tiles_m = 0, tiles_n = 0;
+    float* part = nullptr;        // partial results, one M x N each split; NULL: the epilogue runs here
+    // D' = rho R + act(D + 1 bias^T); the argument of act is Z
+    const float* bias = nullptr;
+    const void* R = nullptr;
+    void* Z = nullptr;
+    void* Y = nullptr;
+    int64_t ldr = 0, ldz = 0, ldy = 0;
+    float rho = 0;
+    int act = GCN_ACT_NONE;
+};
+
+// act and its derivative.  NaN stays NaN.
+__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+__device__ __forceinline__ float act_of(float z, int act) {
+    if (act == GCN_ACT_RELU) return z < 0.f ? 0.f : z;
+    if (act == GCN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if (act == GCN_ACT_SILU) return z / (1.f + expf(-z));
+    return z;
+}
+__device__ __forceinline__ float slope_of(float z, int act) {
+    if (act == GCN_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+    if (act == GCN_ACT_GELU)
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    if (act == GCN_ACT_SILU) {
+        const float s = sigmoid(z);
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+// What becomes of four results of row m, columns n to n + 3, of which `count` are there.
+template <typename T>
+__device__ __forceinline__ void finish4(const TileArgs& a, int64_t m, int n, int count, v4f d) {
+    T* const Y = (T*)a.Y + m * a.ldy + n;
+    T* const Z = a.Z ? (T*)a.Z + m * a.ldz + n : nullptr;
+    const T* const R = a.R ? (const T*)a.R + m * a.ldr + n : nullptr;
+    if (count >= 4) {
+        if (a.bias) d += __builtin_bit_cast(v4f, *reinterpret_cast<const f4u*>(a.bias + n));
+        if (Z) store4(Z, d);
+        if (a.act != GCN_ACT_NONE)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[e] = act_of(d[e], a.act);
+        if (R) {
+            const v4f r = load4(R);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) d[e] = fmaf(a.rho, r[e], d[e]);
+        }
+        store4(Y, d);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (e >= count) break;
+        float v = d[e];
+        if (a.bias) v += a.bias[n + e];
+        if (Z) Z[e] = (T)v;
+        v = act_of(v, a.act);
+        if (R) v = fmaf(a.rho, (float)R[e], v);
+        Y[e] = (T)v;
+    }
+}
+
+#if defined(__HIP_DEVICE_COMPILE__)
+#define GCN_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
+#endif
+
+// One operand of a tile in LDS: R rows (of A) or columns (of B) by 128 bytes of k, as 16-byte pieces.
+//   BY_K   R rows of 8 pieces; piece c of row r lies at c ^ (r & 7), so that the 16 rows that a fragment takes one piece of each
+//          come from all banks.
+//   BY_MN  one row per k of R elements; blocks of 16 elements are moved about within a row by a few bits of k, so that the rows that
+//          a fragment takes together (four, or four of eight) lie in different banks.
+// The place is the same whether pieces come straight from memory or through registers.
+template <typename T, int R, int LIES, int THREADS>
+struct Operand {
+    static constexpr int E = Elem<T>::E, BK = 8 * E, PIECES = R * 8, PER = PIECES / THREADS, ROW = R / E;   // ROW: pieces of a row, BY_MN
+    static constexpr int BLOCKS = R / 16 < 8 ? R / 16 : 8;
+    static_assert(PIECES % THREADS == 0, "whole pieces for every thread");
+    __device__ static int twist(int k) {                          // which block a row's first lies at
+        return (sizeof(T) == 2 ? (k & 3) | ((k >> 3 & 1) << 2) : (k >> 2) & 3) & (BLOCKS - 1);
+    }
+    // piece `slot` of LDS: its row (of r or k) and which piece of that row in memory
+    __device__ static void at(int slot, int& row, int& piece) {
+        if (LIES == BY_K) {
+            row = slot >> 3;
+            piece = (slot & 7) ^ (row & 7);
+        } else {
+            row = slot / ROW;
+            piece = (slot % ROW) ^ (twist(row) * (16 / E));
+        }
+    }
+    // All of a tile's k are there, and rows lie in whole pieces at 16-byte addresses: memory to LDS without registers.  What lies beyond the
+    // matrix along the other dimension is a copy of its last row or piece; its results are not stored.
+    __device__ static void direct(const T* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, char* lds, int tid) {
+        const int wave = tid & ~63;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            int row, piece;
+            at(i * THREADS + tid, row, piece);
+            const T* src;
+            if (LIES == BY_K) {
+                int64_t r = r0 + row;
+                r = r < rows ? r : rows - 1;
+                src = p + r * ld + k0 + piece * E;
+            } else {
+                int64_t r = r0 + piece * E;
+                r = r < rows ? r : rows - E;
+                src = p + (k0 + row) * ld + r;
+            }
+#if defined(__HIP_DEVICE_COMPILE__)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             GCN_LDS(void, lds + (i * THREADS + wave) * 16), 16, 0, 0);
+#endif
+        }
+    }
+    // Any alignment and any k: through registers, zeros for what is not there.
+    __device__ static void fetch(const T* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int64_t K, Vec<T> (&v)[PER], int tid) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            int row, piece;
+            at(i * THREADS + tid, row, piece);
+            const int64_t along = (LIES == BY_K ? k0 : r0) + piece * E, across = (LIES == BY_K ? r0 : k0) + row;
+            const int64_t left = (LIES == BY_K ? K : rows) - along;
+            const bool there = across < (LIES == BY_K ? rows : K) && left > 0;
+            v[i] = Vec<T>{};
+            if (there) v[i] = load_vec_part(p + across * ld + along, left < E ? (int)left : E);
+        }
+    }
+    __device__ static void put(const Vec<T> (&v)[PER], char* lds, int tid) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) *reinterpret_cast<Vec<T>*>(lds + (i * THREADS + tid) * 16) = v[i];
+    }
+    // The fragment of 16 rows (from r on) and the `step`th 64 bytes of k: lane l has row l % 16 and the E values of k that its quarter l / 16 stands for.
+    __device__ static Vec<T> fragment(const char* lds, int r, int step, int lane) {
+        if (LIES == BY_K) {
+            const int row = r + (lane & 15);
+            return *reinterpret_cast<const Vec<T>*>(lds + row * 128 + (((step * 4 + (lane >> 4)) ^ (row & 7)) << 4));
+        }
+#if defined(__HIP_DEVICE_COMPILE__)
+        if constexpr (sizeof(T) == 2) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            typedef short s8 __attribute__((ext_vector_type(8)));
+            // Sixteen lanes read four rows of k by 16 columns, 8 bytes each, and receive a column each.
+            const int k = step * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2), c = (lane & 3) * 8;
+            const char* const p0 = lds + (int64_t)k * (R * 2) + ((((r >> 4) ^ twist(k)) << 5) + c);
+            const char* const p1 = lds + (int64_t)(k + 4) * (R * 2) + ((((r >> 4) ^ twist(k + 4)) << 5) + c);
+            const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(GCN_LDS(s4, p0));
+            const s4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(GCN_LDS(s4, p1));
+            return __builtin_bit_cast(Vec<T>, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+#endif
+        Vec<T> v = {};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int k = step * (4 * E) + (lane >> 4) * E + e;
+            v[e] = *reinterpret_cast<const T*>(lds + (int64_t)k * (R * sizeof(T)) + ((((r >> 4) ^ twist(k)) * 16 + (lane & 15)) * sizeof(T)));
+        }
+        return v;
+    }
+};
+
+// acc += P Q over 64 bytes of k: P 16 rows, Q 16 columns.  With f32 elements four products of four k each; the k of a lane's quarter are consecutive,
+// which orders the sum's terms differently and needs one 16-byte read.
+__device__ __forceinline__ v4f mma(Vec<__bf16> p, Vec<__bf16> q, v4f acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(p, q, acc, 0, 0, 0);
+#else
+    return acc;
+#endif
+}
+__device__ __forceinline__ v4f mma(Vec<_Float16> p, Vec<_Float16> q, v4f acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(p, q, acc, 0, 0, 0);
+#else
+    return acc;
+#endif
+}
+__device__ __forceinline__ v4f mma(Vec<float> p, Vec<float> q, v4f acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(p[e], q[e], acc, 0, 0, 0);
+#endif
+    return acc;
+}
+
+// BM x BN results of a workgroup of WM x WN wavefronts, 128 bytes of k at a time (64 values of 16 bits, 32 of 32), two such stages in LDS: one is
+// fetched while the other is multiplied.  A wavefront's results are the transpose of what the matrix unit is given (B's columns as its rows), so that a lane
+// holds four neighbouring columns of one row.
+// DIRECT: rows of both operands at 16-byte addresses in whole pieces.
+template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT>
+__global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
+    constexpr int THREADS = WM * WN * 64, E = Elem<T>::E, BK = 8 * E;
+    constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+    constexpr int STAGE = (BM + BN) * 128;
+    using OpA = Operand<T, BM, LA, THREADS>;
+    using OpB = Operand<T, BN, LB, THREADS>;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // Neighbouring workgroups run on different XCDs, each with an L2 of its own: every XCD gets a contiguous share of the tiles, and walks it in
+    // groups of eight rows of tiles, column by column, so that what runs at one time shares operands.
+    int tm, tn;
+    {
+        const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, b = blockIdx.x, x = b & 7, q = tiles >> 3, r = tiles & 7;
+        const int64_t t = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + (b >> 3);
+        const int64_t per = (int64_t)8 * a.tiles_n, g = t / per;
+        const int first = (int)(g * 8), rows = a.tiles_m - first < 8 ? a.tiles_m - first : 8, in = (int)(t % per);
+        tm = first + in % rows;
+        tn = in / rows;
+    }
+    const int64_t m0 = (int64_t)tm * BM;
+    const int n0 = tn * BN;
+    const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
+    const T* const A = (const T*)a.A;
+    const T* const B = (const T*)a.B;
+    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+    v4f acc[FM][FN] = {};
+
+    auto multiply = [&](const char* stage) {
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            Vec<T> p[FN], q[FM];
+#pragma unroll
+            for (int j = 0; j < FN; ++j) p[j] = OpB::fragment(stage + BM * 128, wn + j * 16, step, lane);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) q[i] = OpA::fragment(stage, wm + i * 16, step, lane);
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = mma(p[j], q[i], acc[i][j]);
+        }
+    };
+    const int64_t whole = DIRECT ? (ke - kb) / BK : 0;
+    if (DIRECT && whole > 0) {
+        OpA::direct(A, a.lda, m0, a.M, kb, lds, tid);
+        OpB::direct(B, a.ldb, n0, a.N, kb, lds + BM * 128, tid);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        for (int64_t t = 0; t < whole; ++t) {
+            char* const now = lds + (t & 1) * STAGE;
+            char* const next = lds + ((t + 1) & 1) * STAGE;
+            if (t + 1 < whole) {
+                OpA::direct(A, a.lda, m0, a.M, kb + (t + 1) * BK, next, tid);
+                OpB::direct(B, a.ldb, n0, a.N, kb + (t + 1) * BK, next + BM * 128, tid);
+            }
+            multiply(now);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+        }
+    }
+    int64_t k = kb + whole * BK;
+    if (k < ke) {
+        Vec<T> va[OpA::PER], vb[OpB::PER];
+        OpA::fetch(A, a.lda, m0, a.M, k, ke, va, tid);
+        OpB::fetch(B, a.ldb, n0, a.N, k, ke, vb, tid);
+        for (int t = 0; k < ke; k += BK, t ^= 1) {
+            char* const now = lds + t * STAGE;
+            OpA::put(va, now, tid);
+            OpB::put(vb, now + BM * 128, tid);
+            __syncthreads();
+            if (!DIRECT && k + BK < ke) {
+                OpA::fetch(A, a.lda, m0, a.M, k + BK, ke, va, tid);
+                OpB::fetch(B, a.ldb, n0, a.N, k + BK, ke, vb, tid);
+            }
+            multiply(now);
+        }
+    }
+    float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N : nullptr;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int64_t m = m0 + wm + i * 16 + (lane & 15);
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            const int n = n0 + wn + j * 16 + (lane >> 4) * 4;
+            const int count = a.N - n;
+            if (count <= 0) continue;
+            if (part) {
+                float* const p = part + m * a.N + n;
+                if (count >= 4) store4(p, acc[i][j]);
+                else
+                    for (int e = 0; e < count; ++e) p[e] = acc[i][j][e];
+            } else {
+                finish4<T>(a, m, n, count, acc[i][j]);
+            }
+        }
+    }
+}
+
+// The partial results of the splits, added in order, and what the layer does with the sum: four columns per thread.
+template <typename T>
+__global__ __launch_bounds__(256) void k_linear_join(TileArgs a, int splits) {
+    const int64_t per = (a.N + 3) / 4, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t m = t / per;
+    if (m >= a.M) return;
+    const int n = (int)(t % per) * 4, count = a.N - n;
+    const float* p = a.part + m * a.N + n;
+    v4f d = {};
+    for (int s = 0; s < splits; ++s, p += a.M * a.N) {
+        if (count >= 4) d += load4(p);
+        else
+            for (int e = 0; e < count; ++e) d[e] += p[e];
+    }
+    finish4<T>(a, m, n, count, d);
+}
+
+template <typename T> int linear_forward_of(const TileArgs& a, hipStream_t s);          // A by k, B by n, with the epilogue
+template <typename T> int linear_dx_of(const TileArgs& a, hipStream_t s);               // A by k, B by k
+template <typename T> int linear_dw_of(const TileArgs& a, hipStream_t s);               // A by m, B by n
+
+}  // namespace gcn
