@@ -244,6 +244,7 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_block_norm_back(No
                 for (int e = 0; e < E; ++e) add[threadIdx.x * E + e] = sum[k][p][e];
                 __syncthreads();
                 if (threadIdx.x < L) {
+#pragma nounroll
                     for (int r = 1; r < R::ROWS; ++r)
 #pragma unroll
                         for (int e = 0; e < E; ++e) sum[k][p][e] += add[(r * L + threadIdx.x) * E + e];

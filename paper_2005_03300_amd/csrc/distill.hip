@@ -24,35 +24,42 @@ struct DistillArgs {
     double* part = nullptr;
 };
 
-// exp of 32-bit elements by the function, of 16-bit ones by the instruction that raises 2 to a power: its error, 2^-22 of the result times the argument,
-// is far below the rounding of such a gradient.
-template <typename T>
-__device__ __forceinline__ float exp_of(float x) {
-    return sizeof(T) == 4 ? expf(x) : __expf(x);
+// e^((x - high) / T) by the instruction that raises 2 to a power, c = log2(e) / T: the argument is rounded twice, so the result is off by 2^-23 of
+// itself for each unit of the exponent, and the exponents of what counts in a row's sum are small.
+__device__ __forceinline__ float power(float x, float high, float c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f((x - high) * c);
+#else
+    return 0.f;
+#endif
 }
-// e^(z - high) from et = e^((z - high) / T): powers of it at the temperatures 1, 2 and 4 (POWER), else a second exponential.
-template <typename T, int POWER>
-__device__ __forceinline__ float plain_exp(float et, float z, float high) {
+constexpr float LOG2E = 1.4426950408889634f;
+// e^(x - high) from et = e^((x - high) / T): powers of it at the temperatures 1, 2 and 4 (POWER), else a second exponential.
+template <int POWER>
+__device__ __forceinline__ float plain_power(float et, float x, float high) {
     if (POWER == 1) return et;
     if (POWER == 2) return et * et;
     if (POWER == 4) return (et * et) * (et * et);
-    return exp_of<T>(z - high);
+    return power(x, high, LOG2E);
 }
 
-// P = 0: rows longer than the registers hold are read again for each step, from the caches.
+// P = 0: rows longer than the registers hold are read twice, for the sums and for the gradient; what a thread has of a row is summed as it comes, with
+// its running maximum.
+// Elements that are not there count as -inf, so that only loads and stores look at a row's end.
 template <typename T, int L, int P, int POWER>
-__global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_distill(DistillArgs a) {
+__global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_distill(DistillArgs a) {
     using R = Rows<T, L, P>;
     constexpr int E = R::E;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     __shared__ float meet[2][16][4];
     __shared__ double s_w[16];
     int turn = 0;
-    const int li = threadIdx.x % L;
-    // the row's list: index (-1: none), logit of the student, p
-    int32_t* const l_at = (int32_t*)lds + (int64_t)(threadIdx.x / L) * 3 * a.k;
-    float* const l_z = (float*)(l_at + a.k);
-    float* const l_p = l_z + a.k;
+    const int li = threadIdx.x % L, entries = a.k + 1;
+    // the row's list: index (-1: none), logit of the student, p; the label is its last entry, with p = 0
+    int32_t* const l_at = (int32_t*)lds + (int64_t)(threadIdx.x / L) * 3 * entries;
+    float* const l_z = (float*)(l_at + entries);
+    float* const l_p = l_z + entries;
+    const float cT = LOG2E * a.inv_T;
     double mine = 0.0;
     auto lanes_meet = [&]() {                                    // what the row's lanes have written, to LDS or to G, comes before what follows
         if constexpr (L > 64) {
@@ -62,101 +69,138 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_distill(DistillArg
             __builtin_amdgcn_wave_barrier();
         }
     };
+    auto load = [&](const T* z, int64_t c) {
+        const int64_t left = a.C - c;
+        if (left >= E) return load_vec(z + c);
+        Vec<T> v;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = (T)-INFINITY;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < left) v[e] = z[c + e];
+        return v;
+    };
+    auto highest = [](Vec<T> v, float m) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) m = fmaxf(m, (float)v[e]);
+        return m;
+    };
     for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < a.n; i += (int64_t)gridDim.x * R::ROWS) {
         const T* const z = (const T*)a.Z + i * a.ldz;
         Vec<T> held[P ? P : 1];
-        int count[P ? P : 1];
-        // f(elements, column, elements there) for the lane's pieces of the row
-        auto each = [&](auto f) {
-            if constexpr (P != 0) {
+        if constexpr (P != 0)
 #pragma unroll
-                for (int p = 0; p < P; ++p) f(held[p], R::column(p), count[p]);
-            } else {
-                for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) {
-                    const int there = a.C - c < E ? (int)(a.C - c) : E;
-                    f(load_vec_part(z + c, there), (int)c, there);
-                }
-            }
-        };
-        if constexpr (P != 0) {
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                count[p] = R::there(R::column(p), a.C);
-                held[p] = load_vec_part(z + R::column(p), count[p]);
-            }
-        }
+            for (int p = 0; p < P; ++p) held[p] = load(z, R::column(p));
         const int32_t y = a.labels ? a.labels[i] : -1;
         const bool labelled = y >= 0 && y < a.C;
         // the list, and the maxima of both sides
         float high[3] = {-INFINITY, -INFINITY, 0.f};             // of z, of t, whether there is an entry
-        for (int j = li; j < a.k; j += L) {
-            int32_t at = a.top[i * a.ldtop + j];
-            const float t = (float)((const T*)a.t)[i * a.ldt + j];
-            if (at >= a.C || t == -INFINITY) at = -1;
+        for (int j = li; j < entries; j += L) {
+            int32_t at = labelled ? y : -1;
+            float t = 0.f;
+            if (j < a.k) {
+                at = a.top[i * a.ldtop + j];
+                t = (float)((const T*)a.t)[i * a.ldt + j];
+                if (at >= a.C || t == -INFINITY) at = -1;
+                if (at >= 0) {
+                    high[1] = fmaxf(high[1], t);
+                    high[2] = 1.f;
+                }
+            }
             l_at[j] = at;
             l_p[j] = t;
-            if (at < 0) continue;
-            l_z[j] = (float)z[at];
-            high[1] = fmaxf(high[1], t);
-            high[2] = 1.f;
+            if (at >= 0) l_z[j] = (float)z[at];
         }
-        each([&](Vec<T> v, int, int there) {
+        float sum[3] = {0.f, 0.f, 0.f};                          // of e^((z - zh) / T), of e^(z - zh), of the list's e^((t - th) / T)
+        float m = -INFINITY;                                     // P = 0: what the thread's sums are relative to
+        if constexpr (P != 0) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) high[0] = e < there ? fmaxf(high[0], (float)v[e]) : high[0];
-        });
+            for (int p = 0; p < P; ++p) m = highest(held[p], m);
+        } else {
+            for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) {
+                const Vec<T> v = load(z, c);
+                const float now = highest(v, m);
+                if (now > m) {
+                    const float by = power(m, now, cT);          // (nothing before: 0)
+                    sum[0] *= by;
+                    if (POWER != 1) sum[1] *= plain_power<POWER>(by, m, now);
+                    m = now;
+                }
+                if (m == -INFINITY) continue;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float et = power((float)v[e], m, cT);
+                    sum[0] += et;
+                    if (POWER != 1) sum[1] += plain_power<POWER>(et, (float)v[e], m);
+                }
+            }
+        }
+        high[0] = m;
         join_lanes<L, 3, 3>(high, meet, turn);
         const bool taught = high[2] > 0.f;
         const float zh = high[0], th = high[1];
-        float sum[3] = {0.f, 0.f, 0.f};                          // of e^((z - zh) / T), of e^(z - zh), of the list's e^((t - th) / T)
-        each([&](Vec<T> v, int, int there) {
+        if constexpr (P != 0) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float x = (float)v[e];
-                const float et = exp_of<T>((x - zh) * a.inv_T);
-                sum[0] += e < there ? et : 0.f;
-                if (POWER != 1 && labelled) sum[1] += e < there ? plain_exp<T, POWER>(et, x, zh) : 0.f;
-            }
-        });
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float et = power((float)held[p][e], zh, cT);
+                    sum[0] += et;
+                    if (POWER != 1) sum[1] += plain_power<POWER>(et, (float)held[p][e], zh);
+                }
+        } else if (m == -INFINITY) {                             // nothing in it: 0, and NaN where the whole row is so
+            sum[0] = sum[1] = zh == -INFINITY ? NAN : 0.f;
+        } else {
+            const float by = power(m, zh, cT);
+            sum[0] *= by;
+            if (POWER != 1) sum[1] *= plain_power<POWER>(by, m, zh);
+        }
         for (int j = li; j < a.k; j += L)
             if (l_at[j] >= 0) sum[2] += expf((l_p[j] - th) * a.inv_T);
         join_lanes<L, 3>(sum, meet, turn);
         if (POWER == 1) sum[1] = sum[0];
         const float logt = logf(sum[0]), logl = logf(sum[2]);
-        for (int j = li; j < a.k; j += L) {
-            if (l_at[j] < 0) continue;
-            const float x = (l_p[j] - th) * a.inv_T, p = expf(x) / sum[2];
-            const float logq = (l_z[j] - zh) * a.inv_T - logt;
-            if (p != 0.f) mine += (double)(a.wt * p) * (double)((x - logl) - logq);
-            l_p[j] = p;
+        for (int j = li; j < entries; j += L) {
+            if (j == a.k) {
+                if (labelled) mine -= (double)a.wl * (double)((l_z[j] - zh) - logf(sum[1]));
+            } else if (l_at[j] >= 0) {
+                const float x = (l_p[j] - th) * a.inv_T, p = expf(x) / sum[2];
+                const float logq = (l_z[j] - zh) * a.inv_T - logt;
+                if (p != 0.f) mine += (double)(a.wt * p) * (double)((x - logl) - logq);
+                l_p[j] = p;
+            }
         }
-        if (labelled && li == 0) mine -= (double)a.wl * (double)(((float)z[y] - zh) - logf(sum[1]));
-        if (!a.G) {
-            lanes_meet();                                        // the list is written anew
-            continue;
-        }
-        lanes_meet();                                            // all of the list is there, and z[y] read where G takes the place of Z
+        lanes_meet();                                            // all of the list is there; the next row writes it anew
+        if (!a.G) continue;
         T* const G = (T*)a.G + i * a.ldg;
         const float ct = taught ? a.gt / sum[0] : 0.f, cl = labelled ? a.gl / sum[1] : 0.f;
-        // `et` and `el` may be NaN where a row is neither taught nor labelled: chosen, not multiplied away
-        auto gradient = [&](float x, int c) {
-            const float et = exp_of<T>((x - zh) * a.inv_T);
-            float g = taught ? ct * et : 0.f;
-            if (labelled) g += cl * plain_exp<T, POWER>(et, x, zh) - (c == y ? a.gl : 0.f);
-            return g;
+        const bool any = taught || labelled;                     // the row's powers may be NaN where it is neither: not multiplied away
+        auto smooth = [&](float x) {                             // the gradient where the list and the label are not
+            const float et = power(x, zh, cT);
+            const float g = POWER == 1 ? (ct + cl) * et : fmaf(cl, plain_power<POWER>(et, x, zh), ct * et);
+            return any ? g : 0.f;
         };
-        each([&](Vec<T> v, int c, int there) {
+        auto put = [&](Vec<T> v, int64_t c) {
             Vec<T> out;
 #pragma unroll
-            for (int e = 0; e < E; ++e) out[e] = (T)gradient((float)v[e], c + e);
-            store_vec_part(G + c, out, there);
-        });
+            for (int e = 0; e < E; ++e) out[e] = (T)smooth((float)v[e]);
+            const int64_t left = a.C - c;
+            if (left >= E) store_vec(G + c, out);
+            else if (left > 0) store_vec_part(G + c, out, (int)left);
+        };
+        if constexpr (P != 0) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) put(held[p], R::column(p));
+        } else {
+            for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) put(load(z, c), c);
+        }
         lanes_meet();                                            // the list's columns are written again, by other lanes
-        for (int j = li; j < a.k; j += L) {
+        for (int j = li; j < entries; j += L) {
             const int32_t at = l_at[j];
             if (at < 0) continue;
             float p = 0.f;                                       // of all entries that name this column
             for (int o = 0; o < a.k; ++o) p += l_at[o] == at ? l_p[o] : 0.f;
-            G[at] = (T)(gradient(l_z[j], at) - a.gt * p);
+            G[at] = (T)(smooth(l_z[j]) - fmaf(a.gt, p, labelled && at == y ? a.gl : 0.f));
         }
         lanes_meet();
     }
@@ -187,7 +231,7 @@ static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream
         void* part = nullptr;
         GCN_TRY(lease.get(&part, (size_t)blocks * 8, s));
         a.part = (double*)part;
-        launch_lds<k_distill<T, L, P, decltype(power)::value>>(dim3((unsigned)blocks), R::THREADS, (size_t)R::ROWS * a.k * 12, s, a);
+        launch_lds<k_distill<T, L, P, decltype(power)::value>>(dim3((unsigned)blocks), R::THREADS, (size_t)R::ROWS * (a.k + 1) * 12, s, a);
         GCN_LAUNCH_CHECK();
         hipLaunchKernelGGL(k_distill_loss, dim3(1), dim3(256), 0, s, (int64_t)blocks, (const double*)part, 1.0 / (double)m, loss);
         GCN_LAUNCH_CHECK();
@@ -201,7 +245,7 @@ static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream
     };
     const int64_t pieces = (a.C + Elem<T>::E - 1) / Elem<T>::E;
 #define GCN_LANES(L, P) if (pieces <= (int64_t)(L) * (P)) return with(std::integral_constant<int, L>(), std::integral_constant<int, P>())
-    GCN_LANES(4, 1); GCN_LANES(16, 1); GCN_LANES(64, 1); GCN_LANES(64, 4); GCN_LANES(256, 4); GCN_LANES(1024, 4); GCN_LANES(1024, 16);
+    GCN_LANES(4, 1); GCN_LANES(16, 1); GCN_LANES(64, 1); GCN_LANES(64, 4); GCN_LANES(256, 4); GCN_LANES(1024, 4);
 #undef GCN_LANES
     return with(std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
 }

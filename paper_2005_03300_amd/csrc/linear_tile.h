@@ -5,7 +5,7 @@
 //   dX       dZ W^T   A by k, B by k   (the stored W is N x K)
 //   dW       X^T dZ   A by m, B by n   (the stored X is K x M)
 #pragma once
-#include "elem.h"
+#include "rows.h"
 
 namespace gcn {
 
@@ -49,36 +49,27 @@ __device__ __forceinline__ float slope_of(float z, int act) {
     return 1.f;
 }
 
-// What becomes of four results of row m, columns n to n + 3, of which `count` are there.
+// What becomes of the results of row m, columns n to n + E - 1, of which `count` are there.
 template <typename T>
-__device__ __forceinline__ void finish4(const TileArgs& a, int64_t m, int n, int count, v4f d) {
-    T* const Y = (T*)a.Y + m * a.ldy + n;
-    T* const Z = a.Z ? (T*)a.Z + m * a.ldz + n : nullptr;
-    const T* const R = a.R ? (const T*)a.R + m * a.ldr + n : nullptr;
-    if (count >= 4) {
-        if (a.bias) d += __builtin_bit_cast(v4f, *reinterpret_cast<const f4u*>(a.bias + n));
-        if (Z) store4(Z, d);
-        if (a.act != GCN_ACT_NONE)
+__device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int count, float (&d)[Elem<T>::E]) {
+    constexpr int E = Elem<T>::E;
+    if (a.bias) {
+        float b[E];
+        load_floats<E>(a.bias, n, count, 0.f, b);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d[e] = act_of(d[e], a.act);
-        if (R) {
-            const v4f r = load4(R);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[e] = fmaf(a.rho, r[e], d[e]);
-        }
-        store4(Y, d);
-        return;
+        for (int e = 0; e < E; ++e) d[e] += b[e];
     }
+    if (a.Z) store_vec_part((T*)a.Z + m * a.ldz + n, from_floats<T>(d), count);
+    if (a.act != GCN_ACT_NONE)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (e >= count) break;
-        float v = d[e];
-        if (a.bias) v += a.bias[n + e];
-        if (Z) Z[e] = (T)v;
-        v = act_of(v, a.act);
-        if (R) v = fmaf(a.rho, (float)R[e], v);
-        Y[e] = (T)v;
+        for (int e = 0; e < E; ++e) d[e] = act_of(d[e], a.act);
+    if (a.R) {
+        float r[E];
+        to_floats<T>(load_vec_part((const T*)a.R + m * a.ldr + n, count), r);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] = fmaf(a.rho, r[e], d[e]);
     }
+    store_vec_part((T*)a.Y + m * a.ldy + n, from_floats<T>(d), count);
 }
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -284,43 +275,71 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
             multiply(now);
         }
     }
+    // Results leave through LDS, a wavefront's own part of it: what the matrix unit leaves with a lane are four columns of a row, and whole rows of the
+    // wavefront's tile go out together, 16 bytes per lane.  The pieces of a row are moved about by the row, so that the lanes' writes meet all banks.
+    constexpr int PHASES = BM * BN * 4 > 2 * STAGE ? BM * BN * 4 / (2 * STAGE) : 1, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
+    static_assert(FM % PHASES == 0, "whole phases");
+    char* const mine = lds + wave * (ROWS * PIECES * 16);
     float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N : nullptr;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int64_t m = m0 + wm + i * 16 + (lane & 15);
-        if (m >= a.M) continue;
+    for (int ph = 0; ph < PHASES; ++ph) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int n = n0 + wn + j * 16 + (lane >> 4) * 4;
-            const int count = a.N - n;
-            if (count <= 0) continue;
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int row = i * 16 + (lane & 15);
+                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[ph * FP + i][j];
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        constexpr int LANES = FN * 16 / E, STEP = 64 / LANES;     // lanes of a row, rows at a time
+        const int c = (lane % LANES) * E;
+        const int n = n0 + wn + c, count = a.N - n;
+#pragma nounroll
+        for (int row = lane / LANES; row < ROWS; row += STEP) {
+            const int64_t m = m0 + wm + ph * ROWS + row;
+            float d[E];
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                const v4f x = *reinterpret_cast<const v4f*>(mine + row * (PIECES * 16) + ((((c + e) / 4) ^ (row & (PIECES - 1))) << 4));
+#pragma unroll
+                for (int q = 0; q < 4; ++q) d[e + q] = x[q];
+            }
+            if (m >= a.M || count <= 0) continue;
             if (part) {
                 float* const p = part + m * a.N + n;
-                if (count >= 4) store4(p, acc[i][j]);
+                if (count >= E)
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) *reinterpret_cast<f4u*>(p + e) = f4u{d[e], d[e + 1], d[e + 2], d[e + 3]};
                 else
-                    for (int e = 0; e < count; ++e) p[e] = acc[i][j][e];
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (e < count) p[e] = d[e];
             } else {
-                finish4<T>(a, m, n, count, acc[i][j]);
+                finish<T>(a, m, n, count, d);
             }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
-// The partial results of the splits, added in order, and what the layer does with the sum: four columns per thread.
+// The partial results of the splits, added in order, and what the layer does with the sum: 16 bytes of it per thread.
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_join(TileArgs a, int splits) {
-    const int64_t per = (a.N + 3) / 4, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    constexpr int E = Elem<T>::E;
+    const int64_t per = (a.N + E - 1) / E, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t m = t / per;
     if (m >= a.M) return;
-    const int n = (int)(t % per) * 4, count = a.N - n;
+    const int n = (int)(t % per) * E, count = a.N - n;
     const float* p = a.part + m * a.N + n;
-    v4f d = {};
+    float d[E] = {};
     for (int s = 0; s < splits; ++s, p += a.M * a.N) {
-        if (count >= 4) d += load4(p);
-        else
-            for (int e = 0; e < count; ++e) d[e] += p[e];
+        float x[E];
+        load_floats<E>(p, 0, count, 0.f, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] += x[e];
     }
-    finish4<T>(a, m, n, count, d);
+    finish<T>(a, m, n, count, d);
 }
 
 template <typename T> int linear_forward_of(const TileArgs& a, hipStream_t s);          // A by k, B by n, with the epilogue
