@@ -296,7 +296,7 @@ int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const 
  *   dX = dXout + dN/dX'(dH);  dA, dscale, dw_post, db_post, dU from dX through the block's side; dw_pre, db_pre from dH.
  * Each output may be NULL.  dA has the shape of A (with one gate per row a sum over it).  The vectors' gradients are fp32 sums over all
  * rows in a fixed order.  dX, dU and dA may each be U, A, Xout, dXout or dH (same address, leading dimension and width).
- * Widths up to 1024 times 16 bytes (forward: twice that) are held in registers; longer rows are read several times.
+ * Rows of up to 8192 elements are held in registers; longer ones are read several times.
  * ----------------------------------------------------------------------------------------- */
 int gcn_block_norm_forward(int64_t n, int32_t f, int type, int kind, float eps, const void* X, int64_t ldx, const void* U,
                            int64_t ldu, const void* A, int32_t gate_cols, int64_t lda, const float* scale,

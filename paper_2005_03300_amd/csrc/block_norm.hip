@@ -31,232 +31,231 @@ struct NormArgs {
 
 __device__ __forceinline__ float gate_of(float a) { return 1.f / (1.f + expf(-a)); }
 
-template <typename T, int L, int P>
-__global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_block_norm(NormArgs g) {
-    using R = Rows<T, L, P>;
-    constexpr int E = R::E;
+// L lanes (a power of two, up to 1024) hold a row, E neighbouring elements each; a workgroup has as many rows at a time as make 512 threads.  All of them
+// go through the same number of steps, with zeros for a row that is not there.  A lane keeps its columns for all its rows, and what the vectors
+// hold for them; columns behind the row's end have zeros there, which keeps what is computed for them out of every sum.
+template <typename T, int L, int E>
+struct NormRows {
+    static constexpr int THREADS = L > 512 ? L : 512, ROWS = THREADS / L;
+    __device__ static int column() { return (int)(threadIdx.x % L) * E; }
+    __device__ static int row() { return (int)(threadIdx.x / L); }
+};
+__device__ __forceinline__ f4u zero4() { return f4u{0.f, 0.f, 0.f, 0.f}; }
+
+// The next rows are on their way while these are worked on.  Bound by memory.
+template <typename T, int L, int E, bool LAYER>
+__global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(NormArgs g) {
+    using R = NormRows<T, L, E>;
     __shared__ float meet[2][16][4];
     int turn = 0;
-    const int li = threadIdx.x % L;
+    const int c = R::column(), count = g.f - c < 0 ? 0 : (g.f - c > E ? E : g.f - c);
     const float inv_f = 1.f / (float)g.f;
-    for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < g.n; i += (int64_t)gridDim.x * R::ROWS) {
-        float x[P][E], u[P][E];
-        int count[P];
+    float sw[E], sb[E], w_pre[E], b_pre[E];                      // scale w_post, scale b_post
+    load_floats<E>(g.scale, c, count, 1.f, sw);
+    if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
+    {
+        float w[E];
+        load_floats<E>(g.w_post, c, count, 1.f, w);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int c = R::column(p);
-            count[p] = R::there(c, g.f);
-            to_floats<T>(load_vec_part((const T*)g.X + i * g.ldx + c, count[p]), x[p]);
-            if (g.U) to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count[p]), u[p]);
+        for (int e = 0; e < E; ++e) {
+            if (LAYER) sb[e] *= sw[e];
+            sw[e] *= w[e];
         }
-        float umean = 0.f, urstd = 0.f;
-        if (g.U) {
-            if (g.w_post) {
-                float s[1] = {0.f};
-                if (g.layer) {
+    }
+    load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
+    if (LAYER) load_floats<E>(g.b_pre, c, count, 0.f, b_pre);
+    struct Raw {
+        Elems<T, E> x, u, a;
+        float gate;
+    };
+    auto load = [&](int64_t i) {
+        Raw r = {};
+        if (i >= g.n) return r;
+        r.x = load_elems<E>((const T*)g.X + i * g.ldx + c, count);
+        if (g.U) r.u = load_elems<E>((const T*)g.U + i * g.ldu + c, count);
+        if (g.gate > 1) r.a = load_elems<E>((const T*)g.A + i * g.lda + c, count);
+        if (g.gate == 1) r.gate = (float)((const T*)g.A)[i * g.lda];
+        return r;
+    };
+    // mean and deviation of the row's x
+    auto statistics = [&](const float(&x)[E], float& mean, float& rstd) {
+        float s[1] = {0.f};
+        if (LAYER) {
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) s[0] += u[p][e];
-                    join_lanes<L>(s, meet, turn);
-                    umean = s[0] * inv_f;
-                }
-                s[0] = 0.f;
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const float d = e < count[p] ? u[p][e] - umean : 0.f;
-                        s[0] = fmaf(d, d, s[0]);
-                    }
-                join_lanes<L>(s, meet, turn);
-                urstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
-            }
-            const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int c = R::column(p);
-                float w[E], b[E], sc[E], a[E];
-                load_floats<E>(g.scale, c, count[p], 1.f, sc);
-                if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count[p]), a);
-                if (g.w_post) {
-                    load_floats<E>(g.w_post, c, count[p], 1.f, w);
-                    load_floats<E>(g.b_post, c, count[p], 0.f, b);
-                }
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float v = g.w_post ? fmaf((u[p][e] - umean) * urstd, w[e], b[e]) : u[p][e];
-                    x[p][e] = fmaf(sc[e] * (g.gate > 1 ? gate_of(a[e]) : row_gate), v, x[p][e]);
-                }
-                if (g.Xout) store_vec_part((T*)g.Xout + i * g.ldxo + c, from_floats<T>(x[p]), count[p]);
-            }
-        }
-        float xmean = 0.f, xrstd = 0.f;
-        if (g.H) {
-            float s[1] = {0.f};
-            if (g.layer) {
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) s[0] += e < count[p] ? x[p][e] : 0.f;
-                join_lanes<L>(s, meet, turn);
-                xmean = s[0] * inv_f;
-            }
-            s[0] = 0.f;
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float d = e < count[p] ? x[p][e] - xmean : 0.f;
-                    s[0] = fmaf(d, d, s[0]);
-                }
+            for (int e = 0; e < E; ++e) s[0] += e < count ? x[e] : 0.f;
             join_lanes<L>(s, meet, turn);
-            xrstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int c = R::column(p);
-                float w[E], b[E];
-                load_floats<E>(g.w_pre, c, count[p], 1.f, w);
-                load_floats<E>(g.b_pre, c, count[p], 0.f, b);
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[p][e] = fmaf((x[p][e] - xmean) * xrstd, w[e], b[e]);
-                store_vec_part((T*)g.H + i * g.ldh + c, from_floats<T>(x[p]), count[p]);
-            }
+            mean = s[0] * inv_f;
         }
-        if (g.stats && li == 0) *reinterpret_cast<f4u*>(g.stats + 4 * i) = f4u{umean, urstd, xmean, xrstd};
+        s[0] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = e < count ? x[e] - mean : 0.f;
+            s[0] = fmaf(d, d, s[0]);
+        }
+        join_lanes<L>(s, meet, turn);
+        rstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
+    };
+    const int64_t step = (int64_t)gridDim.x * R::ROWS;
+    int64_t base = (int64_t)blockIdx.x * R::ROWS;
+    Raw now = load(base + R::row());
+    for (; base < g.n; base += step) {
+        const int64_t i = base + R::row();
+        const Raw next = load(i + step);
+        float x[E];
+        floats_of<E, T>(now.x, x);
+        f4u st = zero4();
+        if (g.U) {
+            float u[E], a[E];
+            floats_of<E, T>(now.u, u);
+            if (g.w_post) {
+                statistics(u, st.x, st.y);
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] = (u[e] - st.x) * st.y;
+            }
+            if (g.gate > 1) floats_of<E, T>(now.a, a);
+            const float row_gate = g.gate == 1 ? gate_of(now.gate) : 1.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+                x[e] = fmaf(gate, LAYER ? fmaf(u[e], sw[e], sb[e]) : u[e] * sw[e], x[e]);
+            }
+            if (g.Xout && i < g.n) store_elems<E>((T*)g.Xout + i * g.ldxo + c, x, count);
+        }
+        if (g.H) {
+            statistics(x, st.z, st.w);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = LAYER ? fmaf((x[e] - st.z) * st.w, w_pre[e], b_pre[e]) : x[e] * st.w * w_pre[e];
+            if (i < g.n) store_elems<E>((T*)g.H + i * g.ldh + c, x, count);
+        }
+        if (g.stats && c == 0 && i < g.n) *reinterpret_cast<f4u*>(g.stats + 4 * i) = st;
+        now = next;
     }
 }
 
-// The four sums over the rows are kept per column in registers and leave once per workgroup.
-template <typename T, int L, int P>
-__global__ __launch_bounds__((Rows<T, L, P>::THREADS)) void k_block_norm_back(NormArgs g) {
-    using R = Rows<T, L, P>;
-    constexpr int E = R::E;
+// The sums over the rows are kept per column in registers and leave once per workgroup.
+template <typename T, int L, int E, bool LAYER>
+__global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_back(NormArgs g) {
+    using R = NormRows<T, L, E>;
+    constexpr int SUMS = LAYER ? 4 : 2;                // without a mean there are no biases, or they are given to no one
     __shared__ float meet[2][16][4];
     int turn = 0;
-    const int li = threadIdx.x % L;
+    const int c = R::column(), count = g.f - c < 0 ? 0 : (g.f - c > E ? E : g.f - c);
     const float inv_f = 1.f / (float)g.f;
-    float sum[4][P][E] = {};
-    for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < g.n; i += (int64_t)gridDim.x * R::ROWS) {
-        float dx[P][E];
-        int count[P];
-        const f4u st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
+    float sw[E], sb[E], w_pre[E], sum[SUMS][E] = {};
+    load_floats<E>(g.scale, c, count, 1.f, sw);
+    if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
+    {
+        float w[E];
+        load_floats<E>(g.w_post, c, count, 1.f, w);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int c = R::column(p);
-            count[p] = R::there(c, g.f);
-            if (g.dXout) to_floats<T>(load_vec_part((const T*)g.dXout + i * g.lddxo + c, count[p]), dx[p]);
-            else
-#pragma unroll
-                for (int e = 0; e < E; ++e) dx[p][e] = 0.f;
+        for (int e = 0; e < E; ++e) {
+            if (LAYER) sb[e] *= sw[e];
+            sw[e] = e < count ? sw[e] * w[e] : 0.f;
         }
+    }
+    load_floats<E>(g.w_pre, c, count, 0.f, w_pre);
+    struct Raw {
+        Elems<T, E> dxo, xo, dh, u, a;
+        float gate;
+        f4u st;
+    };
+    auto load = [&](int64_t i) {
+        Raw r = {};
+        if (i >= g.n) return r;
+        r.st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
+        if (g.dXout) r.dxo = load_elems<E>((const T*)g.dXout + i * g.lddxo + c, count);
         if (g.dH) {
-            float xh[P][E], gw[P][E];
-            float s[2] = {0.f, 0.f};
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int c = R::column(p);
-                float w[E];
-                to_floats<T>(load_vec_part((const T*)g.Xout + i * g.ldxo + c, count[p]), xh[p]);
-                to_floats<T>(load_vec_part((const T*)g.dH + i * g.lddh + c, count[p]), gw[p]);
-                load_floats<E>(g.w_pre, c, count[p], 1.f, w);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    xh[p][e] = e < count[p] ? (xh[p][e] - st.z) * st.w : 0.f;
-                    sum[2][p][e] = fmaf(gw[p][e], xh[p][e], sum[2][p][e]);
-                    sum[3][p][e] += gw[p][e];
-                    gw[p][e] *= w[e];
-                    s[0] = fmaf(gw[p][e], xh[p][e], s[0]);
-                    s[1] += gw[p][e];
-                }
-            }
-            join_lanes<L>(s, meet, turn);
-            const float along = s[0] * inv_f, mean = g.layer ? s[1] * inv_f : 0.f;
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int e = 0; e < E; ++e) dx[p][e] = fmaf(st.w, gw[p][e] - fmaf(xh[p][e], along, mean), dx[p][e]);
+            r.xo = load_elems<E>((const T*)g.Xout + i * g.ldxo + c, count);
+            r.dh = load_elems<E>((const T*)g.dH + i * g.lddh + c, count);
         }
-        auto store_dx = [&]() {                                  // behind the row's last load: dX may take the place of any of them
-            if (g.dX)
-#pragma unroll
-                for (int p = 0; p < P; ++p) store_vec_part((T*)g.dX + i * g.lddx + R::column(p), from_floats<T>(dx[p]), count[p]);
-        };
-        if (!g.U) {
-            store_dx();
-            continue;
-        }
-        const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
-        float uh[P][E], gv[P][E];
-        float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const int c = R::column(p);
-            float w[E], b[E], sc[E], a[E];
-            load_floats<E>(g.scale, c, count[p], 1.f, sc);
-            load_floats<E>(g.w_post, c, count[p], 1.f, w);
-            load_floats<E>(g.b_post, c, count[p], 0.f, b);
-            to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count[p]), uh[p]);
-            if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count[p]), a);
-            float da[E];
+        if (g.U) r.u = load_elems<E>((const T*)g.U + i * g.ldu + c, count);
+        if (g.gate > 1) r.a = load_elems<E>((const T*)g.A + i * g.lda + c, count);
+        if (g.gate == 1) r.gate = (float)((const T*)g.A)[i * g.lda];
+        return r;
+    };
+    const int64_t step = (int64_t)gridDim.x * R::ROWS;
+    int64_t base = (int64_t)blockIdx.x * R::ROWS;
+    Raw now = load(base + R::row());
+    for (; base < g.n; base += step) {
+        const int64_t i = base + R::row();
+        const Raw next = load(i + step);
+        const bool there = i < g.n;
+        float dx[E];
+        floats_of<E, T>(now.dxo, dx);
+        if (g.dH) {
+            float xh[E], gw[E], s[2] = {0.f, 0.f};
+            floats_of<E, T>(now.xo, xh);
+            floats_of<E, T>(now.dh, gw);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (g.w_post) uh[p][e] = e < count[p] ? (uh[p][e] - st.x) * st.y : 0.f;
-                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
-                const float d = e < count[p] ? dx[p][e] * gate : 0.f;
-                const float v = fmaf(uh[p][e], w[e], b[e]);
-                sum[0][p][e] = fmaf(d, uh[p][e], sum[0][p][e]);
-                sum[1][p][e] += d;
-                da[e] = d * sc[e] * v * (1.f - gate);
-                s[2] += da[e];
-                gv[p][e] = d * sc[e] * w[e];
-                s[0] = fmaf(gv[p][e], uh[p][e], s[0]);
-                s[1] += gv[p][e];
+                xh[e] = (xh[e] - now.st.z) * now.st.w;
+                sum[1][e] = fmaf(gw[e], xh[e], sum[1][e]);
+                if (LAYER) sum[3][e] += gw[e];
+                gw[e] *= w_pre[e];
+                s[0] = fmaf(gw[e], xh[e], s[0]);
+                s[1] += gw[e];
             }
-            if (g.dA && g.gate > 1) store_vec_part((T*)g.dA + i * g.ldda + c, from_floats<T>(da), count[p]);
-        }
-        store_dx();
-        if (!g.dU && g.gate != 1) continue;                      // (the same for all lanes)
-        if (g.w_post || g.gate == 1) join_lanes<L>(s, meet, turn);
-        if (g.dA && g.gate == 1 && li == 0) ((T*)g.dA)[i * g.ldda] = (T)s[2];
-        if (!g.dU) continue;
-        const float along = s[0] * inv_f, mean = g.layer ? s[1] * inv_f : 0.f;
+            join_lanes<L>(s, meet, turn);
+            const float along = s[0] * inv_f, mean = LAYER ? s[1] * inv_f : 0.f;
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (g.w_post)
-#pragma unroll
-                for (int e = 0; e < E; ++e) gv[p][e] = st.y * (gv[p][e] - fmaf(uh[p][e], along, mean));
-            store_vec_part((T*)g.dU + i * g.lddu + R::column(p), from_floats<T>(gv[p]), count[p]);
+            for (int e = 0; e < E; ++e) dx[e] = fmaf(now.st.w, gw[e] - fmaf(xh[e], along, mean), dx[e]);
         }
+        if (g.dX && there) store_elems<E>((T*)g.dX + i * g.lddx + c, dx, count);
+        if (g.U) {
+            const float row_gate = g.gate == 1 ? gate_of(now.gate) : 1.f;
+            const float mean_u = g.w_post ? now.st.x : 0.f, rstd_u = g.w_post ? now.st.y : 1.f;
+            float u[E], a[E], s[3] = {0.f, 0.f, 0.f};
+            floats_of<E, T>(now.u, u);
+            if (g.gate > 1) floats_of<E, T>(now.a, a);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                u[e] = (u[e] - mean_u) * rstd_u;
+                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+                const float d = dx[e] * gate;
+                sum[0][e] = fmaf(d, u[e], sum[0][e]);
+                if (LAYER) sum[2][e] += d;
+                a[e] = d * (LAYER ? fmaf(u[e], sw[e], sb[e]) : u[e] * sw[e]) * (1.f - gate);
+                s[2] += e < count ? a[e] : 0.f;
+                dx[e] = d * sw[e];
+                s[0] = fmaf(dx[e], u[e], s[0]);
+                s[1] += dx[e];
+            }
+            if (g.dA && g.gate > 1 && there) store_elems<E>((T*)g.dA + i * g.ldda + c, a, count);
+            if (g.w_post || g.gate == 1) join_lanes<L>(s, meet, turn);
+            if (g.dA && g.gate == 1 && c == 0 && there) ((T*)g.dA)[i * g.ldda] = (T)s[2];
+            if (g.w_post) {
+                const float along = s[0] * inv_f, mean = LAYER ? s[1] * inv_f : 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) dx[e] = rstd_u * (dx[e] - fmaf(u[e], along, mean));
+            }
+            if (g.dU && there) store_elems<E>((T*)g.dU + i * g.lddu + c, dx, count);
+        }
+        now = next;
     }
     if (!g.part) return;
     // the rows of the workgroup in order, one of the sums at a time
     __shared__ float add[R::ROWS > 1 ? R::THREADS * E : 1];
+    constexpr int AT[4] = {0, 2, 1, 3};                          // sum[] of NormArgs::at[]
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        if (g.at[k] < 0) continue;
-        float* const out = g.part + ((int64_t)blockIdx.x * g.sums + g.at[k]) * g.f;
+        if (AT[k] >= SUMS || g.at[k] < 0) continue;
+        float(&mine)[E] = sum[AT[k] < SUMS ? AT[k] : 0];
+        if constexpr (R::ROWS > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if constexpr (R::ROWS > 1) {
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < E; ++e) add[threadIdx.x * E + e] = sum[k][p][e];
-                __syncthreads();
-                if (threadIdx.x < L) {
+            for (int e = 0; e < E; ++e) add[threadIdx.x * E + e] = mine[e];
+            __syncthreads();
+            if (threadIdx.x < L)
 #pragma nounroll
-                    for (int r = 1; r < R::ROWS; ++r)
+                for (int r = 1; r < R::ROWS; ++r)
 #pragma unroll
-                        for (int e = 0; e < E; ++e) sum[k][p][e] += add[(r * L + threadIdx.x) * E + e];
-                }
-            }
-            if (threadIdx.x < L) {
-                const int c = R::column(p);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (c + e < g.f) out[c + e] = sum[k][p][e];
-            }
+                    for (int e = 0; e < E; ++e) mine[e] += add[(r * L + threadIdx.x) * E + e];
         }
+        float* const out = g.part + ((int64_t)blockIdx.x * g.sums + g.at[k]) * g.f;
+        if (threadIdx.x < L)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e < count) out[c + e] = mine[e];
     }
 }
 
@@ -452,27 +451,31 @@ struct NormVectors {
     const float *scale, *w_post, *b_post;
     float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
 };
+// Sixteen columns by 64 shares of the workgroups, the shares in order.
 __global__ __launch_bounds__(1024) void k_block_norm_vectors(NormArgs g, int blocks, NormVectors v) {
-    __shared__ float s_sum[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float sum[4] = {};
+    __shared__ float shares[4][64][17];
+    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (g.at[k] < 0) continue;
-        __syncthreads();
-        if (c < g.f) s_sum[wave][lane] = strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, wave, 16, blocks);
-        __syncthreads();
-        if (wave == 0 && c < g.f)
-            for (int w = 0; w < 16; ++w) sum[k] += s_sum[w][lane];
+    for (int k = 0; k < 4; ++k)
+        if (g.at[k] >= 0) shares[k][share][col] = c < g.f ? strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, share, 64, blocks) : 0.f;
+    __syncthreads();
+    // (sum, column) of a thread; the others are done
+    __shared__ float total[4][16];
+    if (threadIdx.x < 64) {
+        float s = 0.f;
+        if (g.at[share] >= 0)
+            for (int w = 0; w < 64; ++w) s += shares[share][w][col];
+        total[share][col] = s;
     }
-    if (wave != 0 || c >= g.f) return;
-    const float sc = v.scale ? v.scale[c] : 1.f;
-    if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], sum[0], v.b_post ? v.b_post[c] * sum[1] : 0.f) : sum[0];
-    if (v.dw_post) v.dw_post[c] = sc * sum[0];
-    if (v.db_post) v.db_post[c] = sc * sum[1];
-    if (v.dw_pre) v.dw_pre[c] = sum[2];
-    if (v.db_pre) v.db_pre[c] = sum[3];
+    __syncthreads();
+    if (threadIdx.x >= 16 || c >= g.f) return;
+    const float s0 = total[0][col], s1 = total[1][col], sc = v.scale ? v.scale[c] : 1.f;
+    if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], s0, v.b_post ? v.b_post[c] * s1 : 0.f) : s0;
+    if (v.dw_post) v.dw_post[c] = sc * s0;
+    if (v.db_post) v.db_post[c] = sc * s1;
+    if (v.dw_pre) v.dw_pre[c] = total[2][col];
+    if (v.db_pre) v.db_pre[c] = total[3][col];
 }
 
 __global__ __launch_bounds__(1024) void k_vector_sums(const float* __restrict__ part, int parts, int64_t count, float* __restrict__ out) {
@@ -486,30 +489,32 @@ int vector_sums_launch(const float* part, int parts, int64_t count, float* out, 
     return GCN_OK;
 }
 
-// The fewest lanes that hold a row in one step, more steps where a workgroup's 1024 do not; f(lanes, steps), or f(0, 0) for longer rows than that.
-template <typename T, int MOST, typename F>
+// The fewest lanes that hold a row with E elements each, a workgroup's 1024 with twice as many for longer rows; call(lanes, elements), or call(0, 0) for rows longer than that.
+template <int E, typename F>
 static int by_row(int32_t f, const F& call) {
-    constexpr int E = Elem<T>::E;
     const int64_t pieces = (f + E - 1) / E;
-#define GCN_LANES(L, P) if (pieces <= (int64_t)(L) * (P)) return call(std::integral_constant<int, L>(), std::integral_constant<int, P>())
-    GCN_LANES(4, 1); GCN_LANES(8, 1); GCN_LANES(16, 1); GCN_LANES(32, 1); GCN_LANES(64, 1); GCN_LANES(128, 1); GCN_LANES(256, 1);
-    GCN_LANES(512, 1); GCN_LANES(1024, 1);
-    if constexpr (MOST >= 2) GCN_LANES(1024, 2);
+#define GCN_LANES(L) if (pieces <= (int64_t)(L)) return call(std::integral_constant<int, L>(), std::integral_constant<int, E>())
+    GCN_LANES(4); GCN_LANES(8); GCN_LANES(16); GCN_LANES(32); GCN_LANES(64); GCN_LANES(128); GCN_LANES(256); GCN_LANES(512); GCN_LANES(1024);
 #undef GCN_LANES
+    if constexpr (E < 8)
+        if (f <= 8192) return call(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
     return call(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
 }
 
 template <typename T>
 static int norm_forward(const NormArgs& g, hipStream_t s) {
-    return by_row<T, 2>(g.f, [&](auto l, auto p) -> int {
-        constexpr int L = decltype(l)::value, P = decltype(p)::value;
-        const int64_t most = 16LL * device_info().cus;
+    return by_row<Elem<T>::E>(g.f, [&](auto l, auto elements) -> int {
+        constexpr int L = decltype(l)::value, E = decltype(elements)::value;
+        const int64_t cus = device_info().cus;
         if constexpr (L == 0) {
-            hipLaunchKernelGGL((k_block_norm_long<T>), dim3((unsigned)(g.n < most ? g.n : most)), dim3(1024), 0, s, g);
+            hipLaunchKernelGGL((k_block_norm_long<T>), dim3((unsigned)(g.n < 16 * cus ? g.n : 16 * cus)), dim3(1024), 0, s, g);
         } else {
-            using R = Rows<T, L, P>;
-            const int64_t groups = (g.n + R::ROWS - 1) / R::ROWS;
-            hipLaunchKernelGGL((k_block_norm<T, L, P>), dim3((unsigned)(groups < most ? groups : most)), dim3(R::THREADS), 0, s, g);
+            using R = NormRows<T, L, E>;
+            const int64_t groups = (g.n + R::ROWS - 1) / R::ROWS, most = cus * (2048 / R::THREADS);
+            const dim3 grid((unsigned)(groups < most ? groups : most));
+            // a norm without mean and biases has a kernel of its own
+            if (g.layer || g.b_post || g.b_pre) hipLaunchKernelGGL((k_block_norm<T, L, E, true>), grid, dim3(R::THREADS), 0, s, g);
+            else hipLaunchKernelGGL((k_block_norm<T, L, E, false>), grid, dim3(R::THREADS), 0, s, g);
         }
         GCN_LAUNCH_CHECK();
         return GCN_OK;
@@ -518,14 +523,12 @@ static int norm_forward(const NormArgs& g, hipStream_t s) {
 
 template <typename T>
 static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
-    return by_row<T, 1>(g.f, [&](auto l, auto p) -> int {
-        constexpr int L = decltype(l)::value, P = decltype(p)::value;
-        int64_t groups = g.n, most = device_info().cus;
-        if constexpr (L != 0) {
-            using R = Rows<T, L, P>;
-            groups = (g.n + R::ROWS - 1) / R::ROWS;
-            most *= 2048 / R::THREADS;
-        }
+    // (16-bit elements too by four: eight of them, with the sums, are more than a lane's 128 registers)
+    return by_row<4>(g.f, [&](auto l, auto elements) -> int {
+        constexpr int L = decltype(l)::value, E = decltype(elements)::value;
+        int64_t groups = g.n;
+        const int64_t most = 2LL * device_info().cus;             // of partial sums, which are read again
+        if constexpr (L != 0) groups = (g.n + NormRows<T, L, E>::ROWS - 1) / NormRows<T, L, E>::ROWS;
         const int blocks = (int)(groups < most ? groups : most);
         ScratchLease lease;
         if (g.sums) {
@@ -533,11 +536,16 @@ static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
             GCN_TRY(lease.get(&mem, (size_t)blocks * g.sums * g.f * 4, s));
             g.part = (float*)mem;
         }
-        if constexpr (L == 0) hipLaunchKernelGGL((k_block_norm_back_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, g);
-        else hipLaunchKernelGGL((k_block_norm_back<T, L, P>), dim3((unsigned)blocks), dim3(Rows<T, L, P>::THREADS), 0, s, g);
+        if constexpr (L == 0) {
+            hipLaunchKernelGGL((k_block_norm_back_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, g);
+        } else {
+            using R = NormRows<T, L, E>;
+            if (g.layer || g.b_post || v.db_post || v.db_pre) hipLaunchKernelGGL((k_block_norm_back<T, L, E, true>), dim3((unsigned)blocks), dim3(R::THREADS), 0, s, g);
+            else hipLaunchKernelGGL((k_block_norm_back<T, L, E, false>), dim3((unsigned)blocks), dim3(R::THREADS), 0, s, g);
+        }
         GCN_LAUNCH_CHECK();
         if (g.sums) {
-            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)((g.f + 63) / 64)), dim3(1024), 0, s, g, blocks, v);
+            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)((g.f + 15) / 16)), dim3(1024), 0, s, g, blocks, v);
             GCN_LAUNCH_CHECK();
         }
         return GCN_OK;

@@ -245,7 +245,8 @@ static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream
     };
     const int64_t pieces = (a.C + Elem<T>::E - 1) / Elem<T>::E;
 #define GCN_LANES(L, P) if (pieces <= (int64_t)(L) * (P)) return with(std::integral_constant<int, L>(), std::integral_constant<int, P>())
-    GCN_LANES(4, 1); GCN_LANES(16, 1); GCN_LANES(64, 1); GCN_LANES(64, 4); GCN_LANES(256, 4); GCN_LANES(1024, 4);
+    GCN_LANES(4, 1); GCN_LANES(4, 4); GCN_LANES(8, 4); GCN_LANES(16, 4); GCN_LANES(64, 4); GCN_LANES(256, 4);
+    if (pieces <= 8192) return with(std::integral_constant<int, 256>(), std::integral_constant<int, 0>());
 #undef GCN_LANES
     return with(std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
 }

@@ -66,6 +66,37 @@ __device__ __forceinline__ void store_vec_part(T* p, Vec<T> v, int count) {
 }
 
 inline size_t elem_bytes(int type) { return type == GCN_F32 ? 4 : 2; }
+// Count elements, at any address that the type itself is aligned for; those that are not there are zero.
+template <typename T, int COUNT> using Elems = T __attribute__((ext_vector_type(COUNT)));
+template <typename T, int COUNT>
+struct __attribute__((packed, aligned(sizeof(T)))) LooseElems { uint32_t w[COUNT * sizeof(T) / 4]; };
+template <int COUNT, typename T>
+__device__ __forceinline__ Elems<T, COUNT> load_elems(const T* p, int there) {
+    if (there >= COUNT) return __builtin_bit_cast(Elems<T, COUNT>, *reinterpret_cast<const LooseElems<T, COUNT>*>(p));
+    Elems<T, COUNT> v = {};
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e)
+        if (e < there) v[e] = p[e];
+    return v;
+}
+template <int COUNT, typename T>
+__device__ __forceinline__ void store_elems(T* p, const float (&v)[COUNT], int there) {
+    Elems<T, COUNT> x;
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) x[e] = (T)v[e];
+    if (there >= COUNT) {
+        *reinterpret_cast<LooseElems<T, COUNT>*>(p) = __builtin_bit_cast(LooseElems<T, COUNT>, x);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e)
+        if (e < there) p[e] = x[e];
+}
+template <int COUNT, typename T>
+__device__ __forceinline__ void floats_of(Elems<T, COUNT> x, float (&v)[COUNT]) {
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) v[e] = (float)x[e];
+}
 // Calls f with a value of the element type.
 template <typename F>
 int by_type(int type, const F& f) {

@@ -104,13 +104,13 @@ __device__ __forceinline__ void join_lanes(float (&v)[N], float (*meet)[16][4], 
     fold_lanes<(L < 64 ? L : 64), N, MAXES>(v);
     if constexpr (L > 64) {
         constexpr int WAVES = L / 64;
-        const int lane = threadIdx.x & 63;
+        const int lane = threadIdx.x & 63, first = (int)(threadIdx.x >> 6) & ~(WAVES - 1);    // of the row's wavefronts
         if (lane == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) meet[turn][threadIdx.x >> 6][i] = v[i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = meet[turn][lane & (WAVES - 1)][i];
+        for (int i = 0; i < N; ++i) v[i] = meet[turn][first + (lane & (WAVES - 1))][i];
         fold_lanes<WAVES, N, MAXES>(v);
         turn ^= 1;
     }
