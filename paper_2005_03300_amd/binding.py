@@ -320,41 +320,41 @@ def gcn_layer_backward(a: Csr, Hin, Zprev, W, G, T, S, Y, Gprev, order: int = OR
                                 G.data_ptr(), _at(T), S.data_ptr(), Y.data_ptr(), _at(dbias), _at(Gprev), int(order), _now()))
 
 
-def _elements(rows: int, cols: int, dtype, *tensors):
-    """Checks operands of rows x cols elements of one type (None: not there)."""
-    for t in tensors:
-        if t is not None:
-            assert t.is_cuda, "device tensor expected"
-            assert t.dtype is dtype and t.shape == (rows, cols), (t.dtype, tuple(t.shape), dtype, (rows, cols))
+def _mat(t, shape, dtype):
+    """Address and leading dimension of an operand of that shape and type; (0, 0) for one that is not there."""
+    if t is None:
+        return 0, 0
+    assert t.is_cuda, "device tensor expected"
+    assert t.dtype is dtype and t.shape == shape, (t.dtype, tuple(t.shape), dtype, tuple(shape))
+    s0, s1 = t.stride()
+    rows, cols = shape
+    assert s1 == 1 or cols == 1, "rows must be contiguous"
+    return t.data_ptr(), s0 if rows > 1 else max(s0, cols)
 
 
-def _vectors(size: int, *tensors):
-    """Checks fp32 vectors (None: not there)."""
-    for t in tensors:
-        if t is not None:
-            assert t.is_cuda, "device tensor expected"
-            assert t.dtype is _f32 and t.shape == (size,) and t.is_contiguous(), (t.dtype, tuple(t.shape), size)
+def _vec(t, shape):
+    """Address of an fp32 vector of that shape; 0 for one that is not there."""
+    if t is None:
+        return 0
+    assert t.is_cuda, "device tensor expected"
+    assert t.dtype is _f32 and t.shape == shape and t.is_contiguous(), (t.dtype, tuple(t.shape), tuple(shape))
+    return t.data_ptr()
 
 
-def _place(t):
-    """Address and leading dimension."""
-    return (0, 0) if t is None else (t.data_ptr(), _ld(t))
-
-
-def _type_of(t) -> int:
-    assert t.dtype in _types, f"elements are fp32, bf16 or fp16, not {t.dtype}"
-    return _types[t.dtype]
+def _type_of(dtype) -> int:
+    assert dtype in _types, f"elements are fp32, bf16 or fp16, not {dtype}"
+    return _types[dtype]
 
 
 def gcn_linear_forward(X, W, Y, bias=None, act: int = ACT_NONE, R=None, rho: float = 1.0, Z=None):
     """Y = rho R + act(X W + 1 bias^T); Z receives the argument of act."""
     L = _lib or lib()
+    dt = X.dtype
     n, f_in = X.shape
     f_out = W.shape[1]
-    dt = X.dtype
-    _elements(n, f_in, dt, X), _elements(f_in, f_out, dt, W), _elements(n, f_out, dt, Y, R, Z), _vectors(f_out, bias)
-    rc = L.gcn_linear_forward(n, f_in, f_out, _type_of(X), *_place(X), *_place(W), _at(bias), act, *_place(R), rho, *_place(Z),
-                              *_place(Y), _now())
+    out = (n, f_out)
+    rc = L.gcn_linear_forward(n, f_in, f_out, _type_of(dt), *_mat(X, (n, f_in), dt), *_mat(W, (f_in, f_out), dt), _vec(bias, (f_out,)), act,
+                              *_mat(R, out, dt), rho, *_mat(Z, out, dt), *_mat(Y, out, dt), _raw_stream(_device()))
     if rc:
         _check(rc)
     return Y
@@ -364,12 +364,13 @@ def gcn_linear_backward(X, W, Z, dY, dZ=None, dX=None, dW=None, dbias=None, act:
     """The gradients that are given a place; dZ is workspace of the size of dY (none is needed without an activation).  X may be
     None without dW, W without dX and Z without an activation."""
     L = _lib or lib()
-    n, f_out = dY.shape
-    f_in = next(s for s in (X.shape[1] if X is not None else None, W.shape[0] if W is not None else None, 1) if s is not None)
-    dt = dY.dtype
-    _elements(n, f_out, dt, dY, Z, dZ, dR), _elements(n, f_in, dt, X, dX), _elements(f_in, f_out, dt, W, dW), _vectors(f_out, dbias)
-    rc = L.gcn_linear_backward(n, f_in, f_out, _type_of(dY), *_place(X), *_place(W), *_place(Z), *_place(dY), act, rho, *_place(dZ),
-                               *_place(dX), *_place(dW), _at(dbias), *_place(dR), _now())
+    dt, out = dY.dtype, dY.shape
+    n, f_out = out
+    f_in = X.shape[1] if X is not None else W.shape[0] if W is not None else 1
+    rows, weights = (n, f_in), (f_in, f_out)
+    rc = L.gcn_linear_backward(n, f_in, f_out, _type_of(dt), *_mat(X, rows, dt), *_mat(W, weights, dt), *_mat(Z, out, dt), *_mat(dY, out, dt),
+                               act, rho, *_mat(dZ, out, dt), *_mat(dX, rows, dt), *_mat(dW, weights, dt), _vec(dbias, (f_out,)),
+                               *_mat(dR, out, dt), _raw_stream(_device()))
     if rc:
         _check(rc)
 
@@ -378,16 +379,14 @@ def gcn_block_norm_forward(X, U=None, Xout=None, H=None, w_pre=None, b_pre=None,
                            stats=None, kind: int = NORM_RMS, eps: float = 1e-5):
     """Xout = X + scale sigmoid(A) N(U; w_post, b_post), H = N(Xout; w_pre, b_pre)."""
     L = _lib or lib()
-    n, f = X.shape
-    _elements(n, f, X.dtype, X, U, Xout, H), _vectors(f, w_pre, b_pre, scale, w_post, b_post)
+    dt, shape = X.dtype, X.shape
+    n, f = shape
+    vec = (f,)
     gate = 0 if A is None else A.shape[1]
-    _elements(n, gate, X.dtype, A)
-    if stats is not None:
-        _elements(n, 4, _f32, stats)
-        assert stats.is_contiguous()
-    rc = L.gcn_block_norm_forward(n, f, _type_of(X), kind, eps, *_place(X), *_place(U), _at(A), gate, 0 if A is None else _ld(A),
-                                  _at(scale), _at(w_post), _at(b_post), _at(w_pre), _at(b_pre), *_place(Xout), *_place(H), _at(stats),
-                                  _now())
+    at, lda = _mat(A, (n, gate), dt)
+    rc = L.gcn_block_norm_forward(n, f, _type_of(dt), kind, eps, *_mat(X, shape, dt), *_mat(U, shape, dt), at, gate, lda, _vec(scale, vec),
+                                  _vec(w_post, vec), _vec(b_post, vec), _vec(w_pre, vec), _vec(b_pre, vec), *_mat(Xout, shape, dt),
+                                  *_mat(H, shape, dt), _vec(stats, (n, 4)), _raw_stream(_device()))
     if rc:
         _check(rc)
     return H
@@ -398,18 +397,16 @@ def gcn_block_norm_backward(U, Xout, stats, dXout, dH, dX=None, dU=None, w_pre=N
     """The gradients that are given a place, from dXout and dH (either may be None)."""
     L = _lib or lib()
     some = dH if dH is not None else dXout
-    n, f = some.shape
-    dt = some.dtype
-    _elements(n, f, dt, U, Xout, dXout, dH, dX, dU)
-    _vectors(f, w_pre, scale, w_post, b_post, dscale, dw_post, db_post, dw_pre, db_pre)
+    dt, shape = some.dtype, some.shape
+    n, f = shape
+    vec = (f,)
     gate = 0 if A is None else A.shape[1]
-    _elements(n, gate, dt, A, dA)
-    _elements(n, 4, _f32, stats)
-    assert stats.is_contiguous()
-    rc = L.gcn_block_norm_backward(n, f, _type_of(some), kind, *_place(U), _at(A), gate, 0 if A is None else _ld(A), _at(scale),
-                                   _at(w_post), _at(b_post), _at(w_pre), *_place(Xout), _at(stats), *_place(dXout), *_place(dH),
-                                   *_place(dX), *_place(dU), *_place(dA), _at(dscale), _at(dw_post), _at(db_post), _at(dw_pre),
-                                   _at(db_pre), _now())
+    at, lda = _mat(A, (n, gate), dt)
+    rc = L.gcn_block_norm_backward(n, f, _type_of(dt), kind, *_mat(U, shape, dt), at, gate, lda, _vec(scale, vec), _vec(w_post, vec),
+                                   _vec(b_post, vec), _vec(w_pre, vec), *_mat(Xout, shape, dt), _vec(stats, (n, 4)), *_mat(dXout, shape, dt),
+                                   *_mat(dH, shape, dt), *_mat(dX, shape, dt), *_mat(dU, shape, dt), *_mat(dA, (n, gate), dt),
+                                   _vec(dscale, vec), _vec(dw_post, vec), _vec(db_post, vec), _vec(dw_pre, vec), _vec(db_pre, vec),
+                                   _raw_stream(_device()))
     if rc:
         _check(rc)
 
@@ -419,12 +416,13 @@ def gcn_distill(Z, top, t, loss, G=None, labels=None, temperature: float = 1.0, 
     """Loss of the logits Z against the teacher's list (classes `top`, logits `t`) and the labels, and its gradient G.  m: the divisor
     (None: the number of rows)."""
     L = _lib or lib()
-    n, classes = Z.shape
-    k = top.shape[1]
-    _elements(n, classes, Z.dtype, Z, G), _elements(n, k, Z.dtype, t), _elements(n, k, _i32, top), _vectors(1, loss)
+    dt, shape, lists = Z.dtype, Z.shape, top.shape
+    n, classes = shape
+    k = lists[1]
     assert labels is None or (labels.is_cuda and labels.dtype is _i32 and labels.shape == (n,) and labels.is_contiguous())
-    rc = L.gcn_distill(n, classes, _type_of(Z), *_place(Z), k, *_place(top), *_place(t), _at(labels), temperature, w_teacher,
-                       w_label, n if m is None else m, grad_scale, loss.data_ptr(), *_place(G), _now())
+    rc = L.gcn_distill(n, classes, _type_of(dt), *_mat(Z, shape, dt), k, *_mat(top, (n, k), _i32), *_mat(t, (n, k), dt), _at(labels),
+                       temperature, w_teacher, w_label, n if m is None else m, grad_scale, _vec(loss, (1,)), *_mat(G, shape, dt),
+                       _raw_stream(_device()))
     if rc:
         _check(rc)
     return loss

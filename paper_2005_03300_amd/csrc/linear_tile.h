@@ -226,18 +226,52 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
     v4f acc[FM][FN] = {};
 
-    auto multiply = [&](const char* stage) {
+    // A stage's products; `ahead` sends for the next one.  It comes behind the last transposing read: these wait for everything that is on its way to LDS
+    // (the compiler cannot tell the stages apart), so that behind it each stage would wait for the next before its first product.  With one operand
+    // read so, its fragments of both steps come first (16384 x 4096 x 4096 in bf16: 935 -> 1140 TFLOP/s); with both there are too many for the registers, and the
+    // next stage has the second step's products to arrive in.
+    auto multiply = [&](const char* stage, auto ahead) {
+        constexpr bool BOTH = LA == BY_MN && LB == BY_MN;
+        Vec<T> p[2][FN], q[2][FM];
+        auto read_p = [&](int step) {
 #pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            Vec<T> p[FN], q[FM];
+            for (int j = 0; j < FN; ++j) p[step][j] = OpB::fragment(stage + BM * 128, wn + j * 16, step, lane);
+        };
+        auto read_q = [&](int step) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) p[j] = OpB::fragment(stage + BM * 128, wn + j * 16, step, lane);
-#pragma unroll
-            for (int i = 0; i < FM; ++i) q[i] = OpA::fragment(stage, wm + i * 16, step, lane);
+            for (int i = 0; i < FM; ++i) q[step][i] = OpA::fragment(stage, wm + i * 16, step, lane);
+        };
+        auto products = [&](int step) {
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mma(p[j], q[i], acc[i][j]);
+                for (int j = 0; j < FN; ++j) acc[i][j] = mma(p[step][j], q[step][i], acc[i][j]);
+        };
+        if (BOTH && BM == 256) {                                  // (smaller tiles have other workgroups on their compute unit for that time)
+            read_p(0);
+            read_q(0);
+            products(0);
+            read_p(1);
+            read_q(1);
+            __builtin_amdgcn_sched_barrier(0);
+            ahead();
+            __builtin_amdgcn_sched_barrier(0);
+            products(1);
+            return;
+        }
+        constexpr bool FIRST = LB == BY_MN && !BOTH;
+        if (FIRST) {
+            read_p(0);
+            read_p(1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        ahead();
+        if (FIRST) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            if (!FIRST) read_p(step);
+            read_q(step);
+            products(step);
         }
     };
     const int64_t whole = DIRECT ? (ke - kb) / BK : 0;
@@ -249,11 +283,12 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
         for (int64_t t = 0; t < whole; ++t) {
             char* const now = lds + (t & 1) * STAGE;
             char* const next = lds + ((t + 1) & 1) * STAGE;
-            if (t + 1 < whole) {
-                OpA::direct(A, a.lda, m0, a.M, kb + (t + 1) * BK, next, tid);
-                OpB::direct(B, a.ldb, n0, a.N, kb + (t + 1) * BK, next + BM * 128, tid);
-            }
-            multiply(now);
+            multiply(now, [&]() {
+                if (t + 1 < whole) {
+                    OpA::direct(A, a.lda, m0, a.M, kb + (t + 1) * BK, next, tid);
+                    OpB::direct(B, a.ldb, n0, a.N, kb + (t + 1) * BK, next + BM * 128, tid);
+                }
+            });
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
         }
@@ -268,11 +303,12 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
             OpA::put(va, now, tid);
             OpB::put(vb, now + BM * 128, tid);
             __syncthreads();
-            if (!DIRECT && k + BK < ke) {
-                OpA::fetch(A, a.lda, m0, a.M, k + BK, ke, va, tid);
-                OpB::fetch(B, a.ldb, n0, a.N, k + BK, ke, vb, tid);
-            }
-            multiply(now);
+            multiply(now, [&]() {
+                if (!DIRECT && k + BK < ke) {
+                    OpA::fetch(A, a.lda, m0, a.M, k + BK, ke, va, tid);
+                    OpB::fetch(B, a.ldb, n0, a.N, k + BK, ke, vb, tid);
+                }
+            });
         }
     }
     // Results leave through LDS, a wavefront's own part of it: what the matrix unit leaves with a lane are four columns of a row, and whole rows of the
