@@ -50,6 +50,9 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
     int turn = 0;
     const int c = R::column(), count = g.f - c < 0 ? 0 : (g.f - c > E ? E : g.f - c);
     const float inv_f = 1.f / (float)g.f;
+    const bool ragged = g.f != L * E;                            // lanes whose elements a row's end cuts
+    const int by = settle_by<E>(c, g.f);
+    auto floats = [&](Words<T, E> x, float(&v)[E]) { floats_of<E, T>(ragged ? settle<E, T>(x, by) : __builtin_bit_cast(Elems<T, E>, x), v); };
     float sw[E], sb[E], w_pre[E], b_pre[E];                      // scale w_post, scale b_post
     load_floats<E>(g.scale, c, count, 1.f, sw);
     if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
@@ -65,15 +68,15 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
     load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
     if (LAYER) load_floats<E>(g.b_pre, c, count, 0.f, b_pre);
     struct Raw {
-        Elems<T, E> x, u, a;
+        Words<T, E> x, u, a;
         float gate;
     };
     auto load = [&](int64_t i) {
         Raw r = {};
         if (i >= g.n) return r;
-        r.x = load_elems<E>((const T*)g.X + i * g.ldx + c, count);
-        if (g.U) r.u = load_elems<E>((const T*)g.U + i * g.ldu + c, count);
-        if (g.gate > 1) r.a = load_elems<E>((const T*)g.A + i * g.lda + c, count);
+        r.x = load_near<E>((const T*)g.X + i * g.ldx, c, g.f);
+        if (g.U) r.u = load_near<E>((const T*)g.U + i * g.ldu, c, g.f);
+        if (g.gate > 1) r.a = load_near<E>((const T*)g.A + i * g.lda, c, g.f);
         if (g.gate == 1) r.gate = (float)((const T*)g.A)[i * g.lda];
         return r;
     };
@@ -102,17 +105,17 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
         const int64_t i = base + R::row();
         const Raw next = load(i + step);
         float x[E];
-        floats_of<E, T>(now.x, x);
+        floats(now.x, x);
         f4u st = zero4();
         if (g.U) {
             float u[E], a[E];
-            floats_of<E, T>(now.u, u);
+            floats(now.u, u);
             if (g.w_post) {
                 statistics(u, st.x, st.y);
 #pragma unroll
                 for (int e = 0; e < E; ++e) u[e] = (u[e] - st.x) * st.y;
             }
-            if (g.gate > 1) floats_of<E, T>(now.a, a);
+            if (g.gate > 1) floats(now.a, a);
             const float row_gate = g.gate == 1 ? gate_of(now.gate) : 1.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -141,6 +144,9 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
     int turn = 0;
     const int c = R::column(), count = g.f - c < 0 ? 0 : (g.f - c > E ? E : g.f - c);
     const float inv_f = 1.f / (float)g.f;
+    const bool ragged = g.f != L * E;                            // lanes whose elements a row's end cuts
+    const int by = settle_by<E>(c, g.f);
+    auto floats = [&](Words<T, E> x, float(&v)[E]) { floats_of<E, T>(ragged ? settle<E, T>(x, by) : __builtin_bit_cast(Elems<T, E>, x), v); };
     float sw[E], sb[E], w_pre[E], sum[SUMS][E] = {};
     load_floats<E>(g.scale, c, count, 1.f, sw);
     if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
@@ -155,7 +161,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
     }
     load_floats<E>(g.w_pre, c, count, 0.f, w_pre);
     struct Raw {
-        Elems<T, E> dxo, xo, dh, u, a;
+        Words<T, E> dxo, xo, dh, u, a;
         float gate;
         f4u st;
     };
@@ -163,13 +169,13 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
         Raw r = {};
         if (i >= g.n) return r;
         r.st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
-        if (g.dXout) r.dxo = load_elems<E>((const T*)g.dXout + i * g.lddxo + c, count);
+        if (g.dXout) r.dxo = load_near<E>((const T*)g.dXout + i * g.lddxo, c, g.f);
         if (g.dH) {
-            r.xo = load_elems<E>((const T*)g.Xout + i * g.ldxo + c, count);
-            r.dh = load_elems<E>((const T*)g.dH + i * g.lddh + c, count);
+            r.xo = load_near<E>((const T*)g.Xout + i * g.ldxo, c, g.f);
+            r.dh = load_near<E>((const T*)g.dH + i * g.lddh, c, g.f);
         }
-        if (g.U) r.u = load_elems<E>((const T*)g.U + i * g.ldu + c, count);
-        if (g.gate > 1) r.a = load_elems<E>((const T*)g.A + i * g.lda + c, count);
+        if (g.U) r.u = load_near<E>((const T*)g.U + i * g.ldu, c, g.f);
+        if (g.gate > 1) r.a = load_near<E>((const T*)g.A + i * g.lda, c, g.f);
         if (g.gate == 1) r.gate = (float)((const T*)g.A)[i * g.lda];
         return r;
     };
@@ -181,11 +187,11 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
         const Raw next = load(i + step);
         const bool there = i < g.n;
         float dx[E];
-        floats_of<E, T>(now.dxo, dx);
+        floats(now.dxo, dx);
         if (g.dH) {
             float xh[E], gw[E], s[2] = {0.f, 0.f};
-            floats_of<E, T>(now.xo, xh);
-            floats_of<E, T>(now.dh, gw);
+            floats(now.xo, xh);
+            floats(now.dh, gw);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 xh[e] = (xh[e] - now.st.z) * now.st.w;
@@ -205,8 +211,8 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
             const float row_gate = g.gate == 1 ? gate_of(now.gate) : 1.f;
             const float mean_u = g.w_post ? now.st.x : 0.f, rstd_u = g.w_post ? now.st.y : 1.f;
             float u[E], a[E], s[3] = {0.f, 0.f, 0.f};
-            floats_of<E, T>(now.u, u);
-            if (g.gate > 1) floats_of<E, T>(now.a, a);
+            floats(now.u, u);
+            if (g.gate > 1) floats(now.a, a);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 u[e] = (u[e] - mean_u) * rstd_u;
@@ -259,7 +265,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
     }
 }
 
-// Rows longer than the registers hold: a workgroup reads its row again for every sum, from the caches.
+// Rows longer than the registers hold, and rows shorter than a lane's elements: a workgroup reads its row again for every sum, from the caches.
 template <typename T>
 __global__ __launch_bounds__(1024) void k_block_norm_long(NormArgs g) {
     constexpr int E = Elem<T>::E, STEP = 1024 * E;
@@ -489,15 +495,16 @@ int vector_sums_launch(const float* part, int parts, int64_t count, float* out, 
     return GCN_OK;
 }
 
-// The fewest lanes that hold a row with E elements each, a workgroup's 1024 with twice as many for longer rows; call(lanes, elements), or call(0, 0) for rows longer than that.
+// The fewest lanes that hold a row with E elements each, a workgroup's 1024 with twice as many for longer rows; call(lanes, elements), or call(0, 0) for rows longer than
+// that or shorter than E.
 template <int E, typename F>
 static int by_row(int32_t f, const F& call) {
-    const int64_t pieces = (f + E - 1) / E;
+    const int64_t pieces = f < E ? INT64_MAX : (f + E - 1) / E;
 #define GCN_LANES(L) if (pieces <= (int64_t)(L)) return call(std::integral_constant<int, L>(), std::integral_constant<int, E>())
     GCN_LANES(4); GCN_LANES(8); GCN_LANES(16); GCN_LANES(32); GCN_LANES(64); GCN_LANES(128); GCN_LANES(256); GCN_LANES(512); GCN_LANES(1024);
 #undef GCN_LANES
     if constexpr (E < 8)
-        if (f <= 8192) return call(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
+        if (f >= 8 && f <= 8192) return call(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
     return call(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
 }
 

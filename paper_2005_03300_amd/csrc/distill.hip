@@ -69,15 +69,19 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
             __builtin_amdgcn_wave_barrier();
         }
     };
-    auto load = [&](const T* z, int64_t c) {
+    // (the fewest lanes also have the rows that are shorter than a piece)
+    auto load = [&](const T* z, int64_t c) -> Words<T, E> {
+        if constexpr (L == 4 && P == 1) return __builtin_bit_cast(Words<T, E>, load_elems<E>(z + c, R::there((int)c, a.C)));
+        else return load_near<E>(z, c, a.C);
+    };
+    // behind the row's end: -inf
+    auto whole = [&](Words<T, E> x, int64_t c) {
         const int64_t left = a.C - c;
-        if (left >= E) return load_vec(z + c);
-        Vec<T> v;
+        if (left >= E) return __builtin_bit_cast(Vec<T>, x);
+        Vec<T> v = __builtin_bit_cast(Vec<T>, x);
+        if constexpr (!(L == 4 && P == 1)) v = settle<E, T>(x, settle_by<E>(c, a.C));
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = (T)-INFINITY;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (e < left) v[e] = z[c + e];
+        for (int e = 0; e < E; ++e) v[e] = e < left ? v[e] : (T)-INFINITY;
         return v;
     };
     auto highest = [](Vec<T> v, float m) {
@@ -88,9 +92,10 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
     for (int64_t i = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / L; i < a.n; i += (int64_t)gridDim.x * R::ROWS) {
         const T* const z = (const T*)a.Z + i * a.ldz;
         Vec<T> held[P ? P : 1];
+        Words<T, E> near[P ? P : 1];
         if constexpr (P != 0)
 #pragma unroll
-            for (int p = 0; p < P; ++p) held[p] = load(z, R::column(p));
+            for (int p = 0; p < P; ++p) near[p] = load(z, R::column(p));
         const int32_t y = a.labels ? a.labels[i] : -1;
         const bool labelled = y >= 0 && y < a.C;
         // the list, and the maxima of both sides
@@ -115,10 +120,13 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
         float m = -INFINITY;                                     // P = 0: what the thread's sums are relative to
         if constexpr (P != 0) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) m = highest(held[p], m);
+            for (int p = 0; p < P; ++p) {
+                held[p] = whole(near[p], R::column(p));
+                m = highest(held[p], m);
+            }
         } else {
             for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) {
-                const Vec<T> v = load(z, c);
+                const Vec<T> v = whole(load(z, c), c);
                 const float now = highest(v, m);
                 if (now > m) {
                     const float by = power(m, now, cT);          // (nothing before: 0)
@@ -192,7 +200,7 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
 #pragma unroll
             for (int p = 0; p < P; ++p) put(held[p], R::column(p));
         } else {
-            for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) put(load(z, c), c);
+            for (int64_t c = (int64_t)li * E; c < a.C; c += (int64_t)L * E) put(whole(load(z, c), c), c);
         }
         lanes_meet();                                            // the list's columns are written again, by other lanes
         for (int j = li; j < entries; j += L) {

@@ -1,5 +1,7 @@
 // Elements of 32 and 16 bits: 16 bytes of them at a time, at any address that the type itself is aligned for, and as floats.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 
 namespace gcn {
@@ -72,12 +74,47 @@ template <typename T, int COUNT>
 struct __attribute__((packed, aligned(sizeof(T)))) LooseElems { uint32_t w[COUNT * sizeof(T) / 4]; };
 template <int COUNT, typename T>
 __device__ __forceinline__ Elems<T, COUNT> load_elems(const T* p, int there) {
-    if (there >= COUNT) return __builtin_bit_cast(Elems<T, COUNT>, *reinterpret_cast<const LooseElems<T, COUNT>*>(p));
+    if constexpr (COUNT * sizeof(T) >= 4) {
+        if (there >= COUNT) return __builtin_bit_cast(Elems<T, COUNT>, *reinterpret_cast<const LooseElems<T, COUNT>*>(p));
+    }
     Elems<T, COUNT> v = {};
 #pragma unroll
     for (int e = 0; e < COUNT; ++e)
         if (e < there) v[e] = p[e];
     return v;
+}
+// The elements of a row of `len` from `along` on, zeros behind the row's end, in two steps, so that nothing waits for the load: `load_near` takes any COUNT elements of
+// the row that hold them, one load without a mask, and `settle` moves them to their place.  (An element at a time under masks, each load waits for the one before.)
+// For rows of COUNT elements at least: another way for shorter ones beside it, chosen at run time, brings the waits back.
+template <int COUNT>
+__device__ __forceinline__ int settle_by(int64_t along, int64_t len) {        // 0: nothing to move; COUNT: nothing there
+    if (along + COUNT <= len) return 0;
+    return along - (len - COUNT) < COUNT ? (int)(along - (len - COUNT)) : COUNT;
+}
+// (Words, not elements: of 16-bit elements the compiler would take the loaded registers apart at once.)
+template <typename T, int COUNT> using Words = uint32_t __attribute__((ext_vector_type(COUNT * sizeof(T) / 4)));
+template <int COUNT, typename T>
+__device__ __forceinline__ Words<T, COUNT> load_near(const T* row, int64_t along, int64_t len) {
+    const int64_t at = along + COUNT <= len ? along : len - COUNT;
+    return __builtin_bit_cast(Words<T, COUNT>, *reinterpret_cast<const LooseElems<T, COUNT>*>(row + at));
+}
+template <int COUNT, typename T>
+__device__ __forceinline__ Elems<T, COUNT> settle(Words<T, COUNT> x, int by) {
+    constexpr int BYTES = COUNT * sizeof(T);
+    if constexpr (BYTES == 8 || BYTES == 16) {
+        using Bits = std::conditional_t<BYTES == 8, uint64_t, unsigned __int128>;
+        const Bits bits = __builtin_bit_cast(Bits, x) >> ((by < COUNT ? by : 0) * (int)sizeof(T) * 8);
+        return __builtin_bit_cast(Elems<T, COUNT>, by < COUNT ? bits : (Bits)0);
+    } else {
+        const Elems<T, COUNT> y = __builtin_bit_cast(Elems<T, COUNT>, x);
+        Elems<T, COUNT> v = {};
+#pragma unroll
+        for (int e = 0; e < COUNT; ++e)
+#pragma unroll
+            for (int o = 0; e + o < COUNT; ++o)
+                if (by == o) v[e] = y[e + o];
+        return v;
+    }
 }
 template <int COUNT, typename T>
 __device__ __forceinline__ void store_elems(T* p, const float (&v)[COUNT], int there) {

@@ -1,5 +1,6 @@
 // Which tiles a product takes, and its launch, for one element type.
 #pragma once
+#include "linear_few.h"
 #include "linear_tile.h"
 
 namespace gcn {
@@ -8,6 +9,15 @@ template <typename T, int LIES>
 static bool whole_pieces(const void* p, int64_t ld, int64_t along) {
     constexpr int E = Elem<T>::E;
     return ((uintptr_t)p & 15) == 0 && ld % E == 0 && (LIES == BY_K || along % E == 0);
+}
+
+template <typename T>
+static int launch_join(const TileArgs& a, int splits, hipStream_t s) {
+    const int64_t threads = a.M * ((a.N + Elem<T>::E - 1) / Elem<T>::E);
+    if (splits > 8) hipLaunchKernelGGL((k_linear_join<T, 16>), dim3((unsigned)((threads + 63) / 64)), dim3(1024), 0, s, a, splits);
+    else hipLaunchKernelGGL((k_linear_join<T, 1>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, splits);
+    GCN_LAUNCH_CHECK();
+    return GCN_OK;
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int LA, int LB>
@@ -27,17 +37,12 @@ static int launch_tile(TileArgs a, int splits, hipStream_t s) {
         a.part = (float*)p;
     }
     const dim3 grid((unsigned)(tm * tn), (unsigned)splits);
-    const size_t lds = 2 * (BM + BN) * 128;
     if (whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N))
-        launch_lds<k_linear_tile<T, BM, BN, WM, WN, LA, LB, true>>(grid, WM * WN * 64, lds, s, a);
+        hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, true>), grid, dim3(WM * WN * 64), 0, s, a);
     else
-        launch_lds<k_linear_tile<T, BM, BN, WM, WN, LA, LB, false>>(grid, WM * WN * 64, lds, s, a);
+        hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, false>), grid, dim3(WM * WN * 64), 0, s, a);
     GCN_LAUNCH_CHECK();
-    if (splits > 1) {
-        const int64_t threads = a.M * ((a.N + Elem<T>::E - 1) / Elem<T>::E);
-        hipLaunchKernelGGL((k_linear_join<T>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, splits);
-        GCN_LAUNCH_CHECK();
-    }
+    if (splits > 1) return launch_join<T>(a, splits, s);
     return GCN_OK;
 }
 
@@ -45,24 +50,27 @@ static int launch_tile(TileArgs a, int splits, hipStream_t s) {
 struct TileChoice {
     int edge, splits;
 };
-// The choice with the least estimated time.  A compute unit works through its tiles at a share of the matrix units' rate that grows with the edge (measured on
-// 16384 x 4096 x 4096 in bf16: 1.16 PFLOP/s at 256, 1.03 at 128, 0.70 at 64; in fp32 the three are alike), with a single small tile at a time at little more
-// than half of that; splits fill the chip where there are few tiles, and cost partial results written and read again and a launch.
-inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, int64_t cus) {
-    const double rate = fp32 ? 0.59e6 : 4.5e6;                    // FLOP per microsecond of one compute unit
+// The choice with the least estimated time.  A compute unit has up to 1, 2 or 5 workgroups at a time by the edge, and a stage of theirs takes what the products of all
+// of them do, at a rate that grows with the edge (16384 x 4096 x 4096 in bf16: 1.2 PFLOP/s at 256, 1.05 at 128, 0.73 at 64; 4096 x 2048 x 4096 in fp32:
+// 132 and 125 TFLOP/s at 128 and 64), but no less than a stage's way from memory, which is longer through registers.  Splits fill the chip where there are few
+// tiles, and cost partial results written and read again and a launch.
+inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, bool direct, int64_t cus) {
+    const double rate = fp32 ? 0.52e6 : 4.7e6;                    // FLOP per microsecond of one compute unit
     const int64_t depth = fp32 ? 32 : 64, stages = (K + depth - 1) / depth;
     TileChoice best{64, 1};
     double least = 1e300;
     for (const int edge : {256, 128, 64}) {
         if (fp32 && edge == 256) continue;                        // (nothing to win, and fewer tiles)
-        const int64_t tiles = ((M + edge - 1) / edge) * ((N + edge - 1) / edge);
+        const int64_t tiles = ((M + edge - 1) / edge) * ((N + edge - 1) / edge), most = edge == 256 ? 1 : edge == 128 ? 2 : 5;
+        const double full = edge == 256 ? 1.0 : edge == 128 ? (fp32 ? 1.0 : 0.88) : (fp32 ? 0.93 : 0.61);
+        const double way = (edge == 256 ? 1.2 : edge == 128 ? 0.8 : 0.6) * (direct ? 1.0 : 1.5);
         for (int64_t splits = 1; splits <= 512; splits += splits < 4 ? 1 : splits / 2) {
             const int64_t share = (stages + splits - 1) / splits;
-            if (splits > 1 && (share < 4 || tiles * (splits - 1) > 4 * cus)) break;
-            const int64_t count = tiles * splits, rounds = (count + cus - 1) / cus;
-            const double full = fp32 ? 1.0 : edge == 256 ? 1.0 : edge == 128 ? 0.9 : 0.62;
-            const double part = edge == 256 || rounds >= (edge == 128 ? 2 : 4) ? full : 0.55 * full;
-            double us = rounds * (2.0 * edge * edge * depth * share / (rate * part) + 1.0);
+            if (splits > 1 && (share < 2 || tiles * (splits - 1) > 4 * cus)) break;
+            const int64_t count = tiles * splits, each = (count + cus - 1) / cus;      // of one compute unit
+            const int64_t rounds = (each + most - 1) / most, together = each < most ? each : most;
+            const double products = together * 2.0 * edge * edge * depth / (rate * full);
+            double us = rounds * (share * (products > way ? products : way) + 1.5);
             if (splits > 1) us += 3.0 + splits * (double)M * N * 8 / 4.0e6;
             if (us < least) {
                 least = us;
@@ -75,14 +83,50 @@ inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, int64
 
 template <typename T, int LA, int LB>
 static int linear_product(const TileArgs& a, hipStream_t s) {
-    const TileChoice c = choose_tiles(a.M, a.N, a.K, sizeof(T) == 4, device_info().cus);
+    const bool direct = whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N);
+    const TileChoice c = choose_tiles(a.M, a.N, a.K, sizeof(T) == 4, direct, device_info().cus);
     if constexpr (sizeof(T) == 2)
         if (c.edge == 256) return launch_tile<T, 256, 256, 2, 4, LA, LB>(a, c.splits, s);
     if (c.edge == 128) return launch_tile<T, 128, 128, 2, 2, LA, LB>(a, c.splits, s);
     return launch_tile<T, 64, 64, 2, 2, LA, LB>(a, c.splits, s);
 }
 
-template <> int linear_forward_of<GCN_LINEAR_ELEM>(const TileArgs& a, hipStream_t s) { return linear_product<GCN_LINEAR_ELEM, BY_K, BY_MN>(a, s); }
+template <typename T, int C, int RT>
+static int launch_few(TileArgs a, hipStream_t s) {
+    constexpr int STEP = 4 * Elem<T>::E * FEW_WAVES;              // values of k that a workgroup takes at a time
+    const int strips = (a.N + 16 * C - 1) / (16 * C);
+    // One launch where the strips give enough compute units work; else up to 128 workgroups, each with two steps at least.
+    int64_t splits = 1;
+    if (strips < FEW_STRIPS) {
+        splits = 128 / strips;
+        const int64_t most = (a.K + 2 * STEP - 1) / (2 * STEP);
+        if (splits > most) splits = most;
+    }
+    const int64_t steps = (a.K + STEP - 1) / STEP;
+    a.k_share = (steps + splits - 1) / splits * STEP;
+    splits = (a.K + a.k_share - 1) / a.k_share;
+    ScratchLease lease;
+    if (splits > 1) {
+        void* p = nullptr;
+        GCN_TRY(lease.get(&p, (size_t)splits * a.M * a.N * 4, s));
+        a.part = (float*)p;
+    }
+    launch_lds<k_linear_few<T, C, RT>>(dim3((unsigned)((strips + 7) / 8 * 8), (unsigned)splits), FEW_WAVES * 64, few_lds<T, C, RT>(), s, a, strips);
+    GCN_LAUNCH_CHECK();
+    return splits > 1 ? launch_join<T>(a, (int)splits, s) : GCN_OK;
+}
+
+template <typename T>
+static int linear_forward_impl(const TileArgs& a, hipStream_t s) {
+    const int64_t cus = device_info().cus;
+    if (a.M > 32) return linear_product<T, BY_K, BY_MN>(a, s);
+    // the widest strips that are still one for every compute unit
+    const int c = a.N >= 64 * cus ? 4 : a.N >= 32 * cus ? 2 : 1;
+    if (a.M <= 16) return c == 4 ? launch_few<T, 4, 1>(a, s) : c == 2 ? launch_few<T, 2, 1>(a, s) : launch_few<T, 1, 1>(a, s);
+    return c == 4 ? launch_few<T, 4, 2>(a, s) : c == 2 ? launch_few<T, 2, 2>(a, s) : launch_few<T, 1, 2>(a, s);
+}
+
+template <> int linear_forward_of<GCN_LINEAR_ELEM>(const TileArgs& a, hipStream_t s) { return linear_forward_impl<GCN_LINEAR_ELEM>(a, s); }
 template <> int linear_dx_of<GCN_LINEAR_ELEM>(const TileArgs& a, hipStream_t s) { return linear_product<GCN_LINEAR_ELEM, BY_K, BY_K>(a, s); }
 template <> int linear_dw_of<GCN_LINEAR_ELEM>(const TileArgs& a, hipStream_t s) { return linear_product<GCN_LINEAR_ELEM, BY_MN, BY_MN>(a, s); }
 

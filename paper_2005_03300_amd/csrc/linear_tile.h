@@ -124,19 +124,65 @@ struct Operand {
 #endif
         }
     }
-    // Any alignment and any k: through registers, zeros for what is not there.
-    __device__ static void fetch(const T* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int64_t K, Vec<T> (&v)[PER], int tid) {
+    // Any alignment and any k: through registers.  What lies beyond the matrix along the other dimension is, as with `direct`, something else of it; a piece that its
+    // end cuts is the last whole one (see `piece_at`).
+    struct Source {                                               // where a thread's pieces of the next stage are
+        const T* src[PER];
+    };
+    __device__ static Source source(const T* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int tid) {
+        Source s;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             int row, piece;
             at(i * THREADS + tid, row, piece);
-            const int64_t along = (LIES == BY_K ? k0 : r0) + piece * E, across = (LIES == BY_K ? r0 : k0) + row;
-            const int64_t left = (LIES == BY_K ? K : rows) - along;
-            const bool there = across < (LIES == BY_K ? rows : K) && left > 0;
-            v[i] = Vec<T>{};
-            if (there) v[i] = load_vec_part(p + across * ld + along, left < E ? (int)left : E);
+            if (LIES == BY_K) s.src[i] = p + (r0 + row < rows ? r0 + row : rows - 1) * ld + k0 + piece * E;
+            else s.src[i] = p + (k0 + row) * ld + piece_at(r0 + piece * E, rows);
+        }
+        return s;
+    }
+    __device__ static void fetch(Source& s, int64_t ld, Vec<T> (&v)[PER]) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            v[i] = load_vec(s.src[i]);
+            s.src[i] += LIES == BY_K ? (int64_t)BK : BK * ld;
         }
     }
+    // A stage of which not all k are there: zeros for the others, in both operands.  Also rows shorter than a piece.
+    __device__ static void fetch_end(const T* p, int64_t ld, int64_t r0, int64_t rows, int64_t k0, int64_t K, Vec<T> (&v)[PER], int tid) {
+        if (LIES == BY_K && K < E) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                int row, piece;
+                at(i * THREADS + tid, row, piece);
+                v[i] = load_vec_part(p + (r0 + row < rows ? r0 + row : rows - 1) * ld, piece == 0 ? (int)K : 0);
+            }
+            return;
+        }
+        if (LIES == BY_K) {
+            Words<T, E> x[PER];
+            int by[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                int row, piece;
+                at(i * THREADS + tid, row, piece);
+                x[i] = load_near<E>(p + (r0 + row < rows ? r0 + row : rows - 1) * ld, k0 + piece * E, K);
+                by[i] = settle_by<E>(k0 + piece * E, K);
+            }
+#pragma unroll
+            for (int i = 0; i < PER; ++i) v[i] = settle<E, T>(x[i], by[i]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            int row, piece;
+            at(i * THREADS + tid, row, piece);
+            const int64_t r = r0 + piece * E, k = k0 + row;
+            if (rows >= E) v[i] = k < K ? load_vec(p + k * ld + piece_at(r, rows)) : Vec<T>{};
+            else v[i] = k < K && r == 0 ? load_vec_part(p + k * ld, (int)rows) : Vec<T>{};
+        }
+    }
+    // Where the piece from r on (a multiple of E) of a dimension that is contiguous in memory is taken from.
+    __device__ static int64_t piece_at(int64_t r, int64_t rows) { return r + E <= rows ? r : rows - E; }
     __device__ static void put(const Vec<T> (&v)[PER], char* lds, int tid) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) *reinterpret_cast<Vec<T>*>(lds + (i * THREADS + tid) * 16) = v[i];
@@ -199,13 +245,15 @@ __device__ __forceinline__ v4f mma(Vec<float> p, Vec<float> q, v4f acc) {
 // holds four neighbouring columns of one row.
 // DIRECT: rows of both operands at 16-byte addresses in whole pieces.
 template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT>
-__global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
+__global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, E = Elem<T>::E, BK = 8 * E;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     constexpr int STAGE = (BM + BN) * 128;
     using OpA = Operand<T, BM, LA, THREADS>;
     using OpB = Operand<T, BN, LB, THREADS>;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    // Two arrays, so that the compiler can tell what is on its way to the one from what is read of the other: it makes a transposing read wait for everything
+    // that may be on its way to the same array (16384 x 4096 x 4096 in bf16 with one: 935 TFLOP/s).
+    __shared__ __attribute__((aligned(16))) char stage0[STAGE], stage1[STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // Neighbouring workgroups run on different XCDs, each with an L2 of its own: every XCD gets a contiguous share of the tiles, and walks it in
     // groups of eight rows of tiles, column by column, so that what runs at one time shares operands.
@@ -226,96 +274,85 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
     v4f acc[FM][FN] = {};
 
-    // A stage's products; `ahead` sends for the next one.  It comes behind the last transposing read: these wait for everything that is on its way to LDS
-    // (the compiler cannot tell the stages apart), so that behind it each stage would wait for the next before its first product.  With one operand
-    // read so, its fragments of both steps come first (16384 x 4096 x 4096 in bf16: 935 -> 1140 TFLOP/s); with both there are too many for the registers, and the
-    // next stage has the second step's products to arrive in.
-    auto multiply = [&](const char* stage, auto ahead) {
-        constexpr bool BOTH = LA == BY_MN && LB == BY_MN;
-        Vec<T> p[2][FN], q[2][FM];
-        auto read_p = [&](int step) {
+    auto multiply = [&](const char* stage) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) p[step][j] = OpB::fragment(stage + BM * 128, wn + j * 16, step, lane);
-        };
-        auto read_q = [&](int step) {
+        for (int step = 0; step < 2; ++step) {
+            Vec<T> p[FN], q[FM];
 #pragma unroll
-            for (int i = 0; i < FM; ++i) q[step][i] = OpA::fragment(stage, wm + i * 16, step, lane);
-        };
-        auto products = [&](int step) {
+            for (int j = 0; j < FN; ++j) p[j] = OpB::fragment(stage + BM * 128, wn + j * 16, step, lane);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) q[i] = OpA::fragment(stage, wm + i * 16, step, lane);
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mma(p[step][j], q[step][i], acc[i][j]);
-        };
-        if (BOTH && BM == 256) {                                  // (smaller tiles have other workgroups on their compute unit for that time)
-            read_p(0);
-            read_q(0);
-            products(0);
-            read_p(1);
-            read_q(1);
-            __builtin_amdgcn_sched_barrier(0);
-            ahead();
-            __builtin_amdgcn_sched_barrier(0);
-            products(1);
-            return;
-        }
-        constexpr bool FIRST = LB == BY_MN && !BOTH;
-        if (FIRST) {
-            read_p(0);
-            read_p(1);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        ahead();
-        if (FIRST) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            if (!FIRST) read_p(step);
-            read_q(step);
-            products(step);
+                for (int j = 0; j < FN; ++j) acc[i][j] = mma(p[j], q[i], acc[i][j]);
         }
     };
     const int64_t whole = DIRECT ? (ke - kb) / BK : 0;
     if (DIRECT && whole > 0) {
-        OpA::direct(A, a.lda, m0, a.M, kb, lds, tid);
-        OpB::direct(B, a.ldb, n0, a.N, kb, lds + BM * 128, tid);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        for (int64_t t = 0; t < whole; ++t) {
-            char* const now = lds + (t & 1) * STAGE;
-            char* const next = lds + ((t + 1) & 1) * STAGE;
-            multiply(now, [&]() {
-                if (t + 1 < whole) {
-                    OpA::direct(A, a.lda, m0, a.M, kb + (t + 1) * BK, next, tid);
-                    OpB::direct(B, a.ldb, n0, a.N, kb + (t + 1) * BK, next + BM * 128, tid);
-                }
-            });
+        auto send = [&](char* stage, int64_t t) {
+            OpA::direct(A, a.lda, m0, a.M, kb + t * BK, stage, tid);
+            OpB::direct(B, a.ldb, n0, a.N, kb + t * BK, stage + BM * 128, tid);
+        };
+        auto arrived = []() {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
+        };
+        send(stage0, 0);
+        arrived();
+        for (int64_t t = 0; t < whole; t += 2) {
+            if (t + 1 < whole) send(stage1, t + 1);
+            multiply(stage0);
+            arrived();
+            if (t + 1 == whole) break;
+            if (t + 2 < whole) send(stage0, t + 2);
+            multiply(stage1);
+            arrived();
         }
     }
     int64_t k = kb + whole * BK;
     if (k < ke) {
         Vec<T> va[OpA::PER], vb[OpB::PER];
-        OpA::fetch(A, a.lda, m0, a.M, k, ke, va, tid);
-        OpB::fetch(B, a.ldb, n0, a.N, k, ke, vb, tid);
-        for (int t = 0; k < ke; k += BK, t ^= 1) {
-            char* const now = lds + t * STAGE;
-            OpA::put(va, now, tid);
-            OpB::put(vb, now + BM * 128, tid);
-            __syncthreads();
-            multiply(now, [&]() {
-                if (!DIRECT && k + BK < ke) {
-                    OpA::fetch(A, a.lda, m0, a.M, k + BK, ke, va, tid);
-                    OpB::fetch(B, a.ldb, n0, a.N, k + BK, ke, vb, tid);
-                }
-            });
+        // whole stages one after the other, then what is left; none are whole where rows are shorter than a piece
+        const int64_t end = DIRECT || (LA == BY_MN && a.M < E) || (LB == BY_MN && a.N < E) ? k : k + (ke - k) / BK * BK;
+        typename OpA::Source sa;
+        typename OpB::Source sb;
+        if (!DIRECT && k < end) {
+            sa = OpA::source(A, a.lda, m0, a.M, k, tid);
+            sb = OpB::source(B, a.ldb, n0, a.N, k, tid);
         }
+        auto next = [&]() {
+            if (!DIRECT && k < end) {
+                OpA::fetch(sa, a.lda, va);
+                OpB::fetch(sb, a.ldb, vb);
+            } else {
+                OpA::fetch_end(A, a.lda, m0, a.M, k, ke, va, tid);
+                OpB::fetch_end(B, a.ldb, n0, a.N, k, ke, vb, tid);
+            }
+        };
+        auto step = [&](char* stage) {
+            OpA::put(va, stage, tid);
+            OpB::put(vb, stage + BM * 128, tid);
+            __syncthreads();
+            k += BK;
+            if (!DIRECT && k < ke) next();
+            multiply(stage);
+        };
+        next();
+        step(stage0);                                             // (DIRECT: the only one)
+        if (!DIRECT)
+            while (k < ke) {
+                step(stage1);
+                if (k < ke) step(stage0);
+            }
     }
     // Results leave through LDS, a wavefront's own part of it: what the matrix unit leaves with a lane are four columns of a row, and whole rows of the
     // wavefront's tile go out together, 16 bytes per lane.  The pieces of a row are moved about by the row, so that the lanes' writes meet all banks.
     constexpr int PHASES = BM * BN * 4 > 2 * STAGE ? BM * BN * 4 / (2 * STAGE) : 1, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
     static_assert(FM % PHASES == 0, "whole phases");
-    char* const mine = lds + wave * (ROWS * PIECES * 16);
+    constexpr int HALF = WM * WN / 2;                             // wavefronts that have their part in the first stage
+    static_assert(HALF * ROWS * PIECES * 16 <= STAGE, "results have room");
+    char* const mine = (wave < HALF ? stage0 : stage1) + (wave % HALF) * (ROWS * PIECES * 16);
     float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N : nullptr;
     __syncthreads();
 #pragma unroll
@@ -329,11 +366,12 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         constexpr int LANES = FN * 16 / E, STEP = 64 / LANES;     // lanes of a row, rows at a time
-        const int c = (lane % LANES) * E;
-        const int n = n0 + wn + c, count = a.N - n;
+        const int c = (lane % LANES) * E, n = n0 + wn + c, count = a.N - n;
+        // a piece that the end of a dimension cut holds the last whole one: its last `count` columns, and likewise rows
+        const bool shifted = LB == BY_MN && !DIRECT && count < E && a.N >= E;
 #pragma nounroll
         for (int row = lane / LANES; row < ROWS; row += STEP) {
-            const int64_t m = m0 + wm + ph * ROWS + row;
+            int64_t m = m0 + wm + ph * ROWS + row;
             float d[E];
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
@@ -341,7 +379,23 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) d[e + q] = x[q];
             }
+            if (LA == BY_MN && !DIRECT && a.M >= E) {
+                const int64_t first = m - row % E;                 // of the piece (a wavefront's rows are whole ones)
+                if (first + E > a.M) {
+                    if (first >= a.M) continue;
+                    m += a.M - E - first;
+                    if (m < first) continue;
+                }
+            }
             if (m >= a.M || count <= 0) continue;
+            if (shifted)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float x = d[e];
+#pragma unroll
+                    for (int o = 1; o < E; ++o) x = e + o < E && E - count == o ? d[e + o < E ? e + o : e] : x;
+                    d[e] = x;
+                }
             if (part) {
                 float* const p = part + m * a.N + n;
                 if (count >= E)
@@ -359,23 +413,37 @@ __global__ __launch_bounds__(WM* WN * 64) void k_linear_tile(TileArgs a) {
     }
 }
 
-// The partial results of the splits, added in order, and what the layer does with the sum: 16 bytes of it per thread.
-template <typename T>
-__global__ __launch_bounds__(256) void k_linear_join(TileArgs a, int splits) {
-    constexpr int E = Elem<T>::E;
-    const int64_t per = (a.N + E - 1) / E, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// The partial results of the splits, added in order, and what the layer does with the sum: 16 bytes of it per thread; SHARES threads, a wavefront apart, take a
+// share of the splits each where there are many of them and few results (one thread after 211 of them: 60 us).
+template <typename T, int SHARES>
+__global__ __launch_bounds__(64 * (SHARES > 1 ? SHARES : 4)) void k_linear_join(TileArgs a, int splits) {
+    constexpr int E = Elem<T>::E, PER = SHARES > 1 ? 64 : 256;
+    __shared__ float add[SHARES > 1 ? SHARES : 1][SHARES > 1 ? 64 : 1][E + 1];
+    const int64_t per = (a.N + E - 1) / E, t = (int64_t)blockIdx.x * PER + threadIdx.x % PER;
+    const int share = threadIdx.x / PER;
     const int64_t m = t / per;
-    if (m >= a.M) return;
     const int n = (int)(t % per) * E, count = a.N - n;
-    const float* p = a.part + m * a.N + n;
     float d[E] = {};
-    for (int s = 0; s < splits; ++s, p += a.M * a.N) {
-        float x[E];
-        load_floats<E>(p, 0, count, 0.f, x);
+    if (m < a.M) {
+        const float* const p = a.part + m * a.N + n;
+#pragma unroll 4
+        for (int s = share; s < splits; s += SHARES) {
+            float x[E];
+            load_floats<E>(p + (int64_t)s * a.M * a.N, 0, count, 0.f, x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) d[e] += x[e];
+            for (int e = 0; e < E; ++e) d[e] += x[e];
+        }
     }
-    finish<T>(a, m, n, count, d);
+    if constexpr (SHARES > 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) add[share][threadIdx.x % PER][e] = d[e];
+        __syncthreads();
+        if (share) return;
+        for (int w = 1; w < SHARES; ++w)
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] += add[w][threadIdx.x][e];
+    }
+    if (m < a.M) finish<T>(a, m, n, count, d);
 }
 
 template <typename T> int linear_forward_of(const TileArgs& a, hipStream_t s);          // A by k, B by n, with the epilogue
