@@ -533,9 +533,13 @@ static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
     // (16-bit elements too by four: eight of them, with the sums, are more than a lane's 128 registers)
     return by_row<4>(g.f, [&](auto l, auto elements) -> int {
         constexpr int L = decltype(l)::value, E = decltype(elements)::value;
-        int64_t groups = g.n;
-        const int64_t most = 2LL * device_info().cus;             // of partial sums, which are read again
-        if constexpr (L != 0) groups = (g.n + NormRows<T, L, E>::ROWS - 1) / NormRows<T, L, E>::ROWS;
+        // as many workgroups as run at one time: each leaves partial sums, which are read again
+        int64_t groups = g.n, most = device_info().cus;
+        if constexpr (L != 0) {
+            using R = NormRows<T, L, E>;
+            groups = (g.n + R::ROWS - 1) / R::ROWS;
+            most *= 1024 / R::THREADS;
+        }
         const int blocks = (int)(groups < most ? groups : most);
         ScratchLease lease;
         if (g.sums) {
