@@ -29,7 +29,14 @@ struct NormArgs {
     int at[4] = {-1, -1, -1, -1};  // which of them are sum dX' a u^, sum dX' a, sum dH x^, sum dH
 };
 
-__device__ __forceinline__ float gate_of(float a) { return 1.f / (1.f + expf(-a)); }
+// (by the instructions for a power of 2 and a reciprocal: off by a few 2^-24)
+__device__ __forceinline__ float gate_of(float a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -1.4426950408889634f));
+#else
+    return 0.f;
+#endif
+}
 
 // L lanes (a power of two, up to 1024) hold a row, E neighbouring elements each; a workgroup has as many rows at a time as make 512 threads.  All of them
 // go through the same number of steps, with zeros for a row that is not there.  A lane keeps its columns for all its rows, and what the vectors
@@ -53,6 +60,22 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
     const bool ragged = g.f != L * E;                            // lanes whose elements a row's end cuts
     const int by = settle_by<E>(c, g.f);
     auto floats = [&](Words<T, E> x, float(&v)[E]) { floats_of<E, T>(ragged ? settle<E, T>(x, by) : __builtin_bit_cast(Elems<T, E>, x), v); };
+    struct Raw {
+        Words<T, E> x, u, a;
+        float gate;
+    };
+    auto load = [&](int64_t i) {
+        Raw r = {};
+        if (i >= g.n) return r;
+        r.x = load_near<E>((const T*)g.X + i * g.ldx, c, g.f);
+        if (g.U) r.u = load_near<E>((const T*)g.U + i * g.ldu, c, g.f);
+        if (g.gate > 1) r.a = load_near<E>((const T*)g.A + i * g.lda, c, g.f);
+        if (g.gate == 1) r.gate = (float)((const T*)g.A)[i * g.lda];
+        return r;
+    };
+    const int64_t step = (int64_t)gridDim.x * R::ROWS;
+    int64_t base = (int64_t)blockIdx.x * R::ROWS;
+    Raw now = load(base + R::row());
     float sw[E], sb[E], w_pre[E], b_pre[E];                      // scale w_post, scale b_post
     load_floats<E>(g.scale, c, count, 1.f, sw);
     if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
@@ -67,19 +90,6 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
     }
     load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
     if (LAYER) load_floats<E>(g.b_pre, c, count, 0.f, b_pre);
-    struct Raw {
-        Words<T, E> x, u, a;
-        float gate;
-    };
-    auto load = [&](int64_t i) {
-        Raw r = {};
-        if (i >= g.n) return r;
-        r.x = load_near<E>((const T*)g.X + i * g.ldx, c, g.f);
-        if (g.U) r.u = load_near<E>((const T*)g.U + i * g.ldu, c, g.f);
-        if (g.gate > 1) r.a = load_near<E>((const T*)g.A + i * g.lda, c, g.f);
-        if (g.gate == 1) r.gate = (float)((const T*)g.A)[i * g.lda];
-        return r;
-    };
     // mean and deviation of the row's x
     auto statistics = [&](const float(&x)[E], float& mean, float& rstd) {
         float s[1] = {0.f};
@@ -98,9 +108,6 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
         join_lanes<L>(s, meet, turn);
         rstd = 1.f / sqrtf(fmaf(s[0], inv_f, g.eps));
     };
-    const int64_t step = (int64_t)gridDim.x * R::ROWS;
-    int64_t base = (int64_t)blockIdx.x * R::ROWS;
-    Raw now = load(base + R::row());
     for (; base < g.n; base += step) {
         const int64_t i = base + R::row();
         const Raw next = load(i + step);
@@ -147,19 +154,6 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
     const bool ragged = g.f != L * E;                            // lanes whose elements a row's end cuts
     const int by = settle_by<E>(c, g.f);
     auto floats = [&](Words<T, E> x, float(&v)[E]) { floats_of<E, T>(ragged ? settle<E, T>(x, by) : __builtin_bit_cast(Elems<T, E>, x), v); };
-    float sw[E], sb[E], w_pre[E], sum[SUMS][E] = {};
-    load_floats<E>(g.scale, c, count, 1.f, sw);
-    if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
-    {
-        float w[E];
-        load_floats<E>(g.w_post, c, count, 1.f, w);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            if (LAYER) sb[e] *= sw[e];
-            sw[e] = e < count ? sw[e] * w[e] : 0.f;
-        }
-    }
-    load_floats<E>(g.w_pre, c, count, 0.f, w_pre);
     struct Raw {
         Words<T, E> dxo, xo, dh, u, a;
         float gate;
@@ -182,6 +176,19 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
     const int64_t step = (int64_t)gridDim.x * R::ROWS;
     int64_t base = (int64_t)blockIdx.x * R::ROWS;
     Raw now = load(base + R::row());
+    float sw[E], sb[E], w_pre[E], sum[SUMS][E] = {};
+    load_floats<E>(g.scale, c, count, 1.f, sw);
+    if (LAYER) load_floats<E>(g.b_post, c, count, 0.f, sb);
+    {
+        float w[E];
+        load_floats<E>(g.w_post, c, count, 1.f, w);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (LAYER) sb[e] *= sw[e];
+            sw[e] = e < count ? sw[e] * w[e] : 0.f;
+        }
+    }
+    load_floats<E>(g.w_pre, c, count, 0.f, w_pre);
     for (; base < g.n; base += step) {
         const int64_t i = base + R::row();
         const Raw next = load(i + step);

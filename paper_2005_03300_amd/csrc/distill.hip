@@ -164,20 +164,26 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
             if (POWER != 1) sum[1] *= plain_power<POWER>(by, m, zh);
         }
         for (int j = li; j < a.k; j += L)
-            if (l_at[j] >= 0) sum[2] += expf((l_p[j] - th) * a.inv_T);
+            if (l_at[j] >= 0) {
+                const float e = expf((l_p[j] - th) * a.inv_T);
+                l_p[j] = e;
+                sum[2] += e;
+            }
         join_lanes<L, 3>(sum, meet, turn);
         if (POWER == 1) sum[1] = sum[0];
-        const float logt = logf(sum[0]), logl = logf(sum[2]);
-        for (int j = li; j < entries; j += L) {
-            if (j == a.k) {
-                if (labelled) mine -= (double)a.wl * (double)((l_z[j] - zh) - logf(sum[1]));
-            } else if (l_at[j] >= 0) {
-                const float x = (l_p[j] - th) * a.inv_T, p = expf(x) / sum[2];
-                const float logq = (l_z[j] - zh) * a.inv_T - logt;
-                if (p != 0.f) mine += (double)(a.wt * p) * (double)((x - logl) - logq);
-                l_p[j] = p;
-            }
+        const float over = taught ? 1.f / sum[2] : 0.f;
+        // sum of p (log p - log q), the list's constant part log(sum of e^((z - zh) / T)) - log(sum of e^((t - th) / T)) taken out of the logarithms; log p is that of
+        // the p that counts, and where p is 0 nothing does
+        const float apart = taught ? logf(sum[0]) - logf(sum[2]) : 0.f;
+        float kl = 0.f;
+        for (int j = li; j < a.k; j += L) {
+            if (l_at[j] < 0) continue;
+            const float p = l_p[j] * over, t = (float)((const T*)a.t)[i * a.ldt + j];
+            l_p[j] = p;
+            if (p != 0.f) kl = fmaf(p, fmaf((t - th) - (l_z[j] - zh), a.inv_T, apart), kl);
         }
+        mine += (double)a.wt * (double)kl;
+        if (labelled && li == a.k % L) mine -= (double)a.wl * (double)((l_z[a.k] - zh) - logf(sum[1]));
         lanes_meet();                                            // all of the list is there; the next row writes it anew
         if (!a.G) continue;
         T* const G = (T*)a.G + i * a.ldg;
@@ -233,7 +239,7 @@ static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream
     auto launch = [&](auto l, auto p, auto power) -> int {
         constexpr int L = decltype(l)::value, P = decltype(p)::value;
         using R = Rows<T, L, P>;
-        const int64_t groups = (a.n + R::ROWS - 1) / R::ROWS, most = (int64_t)device_info().cus * (2048 / R::THREADS);
+        const int64_t groups = (a.n + R::ROWS - 1) / R::ROWS, most = (int64_t)device_info().cus * (L <= 64 ? 16 : 2048 / R::THREADS);
         const int blocks = (int)(groups < most ? groups : most);
         ScratchLease lease;
         void* part = nullptr;

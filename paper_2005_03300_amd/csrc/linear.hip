@@ -4,67 +4,91 @@
 namespace gcn {
 
 // dZ = dY * act'(Z), dR = rho dY, and the column sums of dZ (the bias gradient, of the unrounded products): one pass over the matrices for the elementwise
-// part.  A workgroup has 64 lanes of four columns by four rows at a time, and a share of the rows; the four row sets are added in order.
+// part, bound by memory.  A workgroup has 64 lanes of 16 bytes by four rows at a time, two such sets on their way, and a share of the rows; the four row sets are
+// added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int64_t rows_per_block, const T* Z, int64_t ldz,
                                                       const T* dY, int64_t lddy, int act, float rho, T* dZ, int64_t lddz, T* dR,
                                                       int64_t lddr, float* __restrict__ part) {
-    __shared__ v4f sums[4][64];
+    constexpr int E = Elem<T>::E, SETS = 4, AHEAD = 2;
+    __shared__ float sums[SETS][64][E + 1];
     const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
-    const int64_t c = ((int64_t)blockIdx.y * 64 + lane) * 4;
+    const int64_t c = ((int64_t)blockIdx.y * 64 + lane) * E;
     const int64_t rb = (int64_t)blockIdx.x * rows_per_block, re = rb + rows_per_block < n ? rb + rows_per_block : n;
-    const int64_t count = N - c;
-    v4f sum = {};
-    if (count >= 4) {
-        for (int64_t i = rb + set; i < re; i += 4) {
-            const v4f g = load4(dY + i * lddy + c);
-            v4f d = g;
-            if (act != GCN_ACT_NONE) {
-                const v4f z = load4(Z + i * ldz + c);
+    const int count = c >= N ? 0 : N - c < E ? (int)(N - c) : E;
+    float sum[E] = {};
+    auto row = [&](int64_t i, Vec<T> y, Vec<T> z) {
+        float d[E], g[E];
+        to_floats<T>(y, g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[e] *= slope_of(z[e], act);
-                if (dZ) store4(dZ + i * lddz + c, d);
+        for (int e = 0; e < E; ++e) d[e] = g[e];
+        if (act != GCN_ACT_NONE) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] *= slope_of<T>((float)z[e], act);
+            if (dZ) store_vec_part(dZ + i * lddz + c, from_floats<T>(d), count);
+        }
+        if (dR) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) g[e] *= rho;
+            store_vec_part(dR + i * lddr + c, from_floats<T>(g), count);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += d[e];
+    };
+    if (count == E) {
+        for (int64_t i = rb + set; i < re; i += AHEAD * SETS) {
+            Vec<T> y[AHEAD], z[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t at = i + u * SETS < re ? i + u * SETS : i;           // (the first again where there is no second)
+                y[u] = load_vec(dY + at * lddy + c);
+                if (act != GCN_ACT_NONE) z[u] = load_vec(Z + at * ldz + c);
             }
-            if (dR) store4(dR + i * lddr + c, g * rho);
-            sum += d;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (i + u * SETS < re) row(i + u * SETS, y[u], z[u]);
+        }
+    } else if (count > 0 && N >= E) {
+        const int by = settle_by<E>(c, N);
+        for (int64_t i = rb + set; i < re; i += SETS) {
+            const Words<T, E> y = load_near<E>(dY + i * lddy, c, N);
+            Words<T, E> z = {};
+            if (act != GCN_ACT_NONE) z = load_near<E>(Z + i * ldz, c, N);
+            row(i, settle<E, T>(y, by), settle<E, T>(z, by));
         }
     } else if (count > 0) {
-        for (int64_t i = rb + set; i < re; i += 4)
-            for (int e = 0; e < count; ++e) {
-                const float g = (float)dY[i * lddy + c + e];
-                float d = g;
-                if (act != GCN_ACT_NONE) {
-                    d *= slope_of((float)Z[i * ldz + c + e], act);
-                    if (dZ) dZ[i * lddz + c + e] = (T)d;
-                }
-                if (dR) dR[i * lddr + c + e] = (T)(g * rho);
-                sum[e] += d;
-            }
+        for (int64_t i = rb + set; i < re; i += SETS)
+            row(i, load_vec_part(dY + i * lddy + c, count), act != GCN_ACT_NONE ? load_vec_part(Z + i * ldz + c, count) : Vec<T>{});
     }
     if (!part) return;
-    sums[set][lane] = sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[set][lane][e] = sum[e];
     __syncthreads();
     if (set) return;
-    for (int w = 1; w < 4; ++w) sum += sums[w][lane];
-    for (int e = 0; e < 4 && e < count; ++e) part[(int64_t)blockIdx.x * N + c + e] = sum[e];
+    for (int w = 1; w < SETS; ++w)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += sums[w][lane][e];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (e < count) part[(int64_t)blockIdx.x * N + c + e] = sum[e];
 }
 
 template <typename T>
 static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho, void* dZ,
                         int64_t lddz, void* dR, int64_t lddr, float* dbias, hipStream_t s) {
-    const int64_t across = ((int64_t)N + 255) / 256;
+    const int64_t wide = 64 * Elem<T>::E, across = (N + wide - 1) / wide;
     int64_t blocks = (8LL * device_info().cus + across - 1) / across;
     if (blocks > (n + 15) / 16) blocks = (n + 15) / 16;
     if (blocks > 1024) blocks = 1024;
     const int64_t per = ((n + blocks - 1) / blocks + 3) / 4 * 4;
     blocks = (n + per - 1) / per;
     ScratchLease lease;
-    void* part = nullptr;
-    if (dbias) GCN_TRY(lease.get(&part, (size_t)blocks * N * 4, s));
+    void* part = dbias;                                           // the sums of a single share of the rows are the result
+    if (dbias && blocks > 1) GCN_TRY(lease.get(&part, (size_t)blocks * N * 4, s));
     hipLaunchKernelGGL(k_linear_slope<T>, dim3((unsigned)blocks, (unsigned)across), dim3(256), 0, s, n, N, per, (const T*)Z, ldz,
                        (const T*)dY, lddy, act, rho, (T*)dZ, lddz, (T*)dR, lddr, (float*)part);
     GCN_LAUNCH_CHECK();
-    if (dbias) return vector_sums_launch((const float*)part, (int)blocks, N, dbias, s);
+    if (dbias && blocks > 1) return vector_sums_launch((const float*)part, (int)blocks, N, dbias, s);
     return GCN_OK;
 }
 

@@ -30,21 +30,61 @@ struct TileArgs {
     int act = GCN_ACT_NONE;
 };
 
+// e^x and 1/x by the instructions (2 to a power; a reciprocal), each off by a unit in the last place, the power also by 2^-24 for each unit of its argument.
+__device__ __forceinline__ float fast_exp(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
+#else
+    return 0.f;
+#endif
+}
+__device__ __forceinline__ float fast_inverse(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_rcpf(x);
+#else
+    return 0.f;
+#endif
+}
+__device__ __forceinline__ float sigmoid(float z) { return fast_inverse(1.f + fast_exp(-z)); }
+// The normal distribution function Phi(z) and its density.  For 16-bit elements erfc by Abramowitz and Stegun's formula 7.1.26, off by 1.5e-7 at most, whose
+// exponential is the density's (erff's way through its ranges made the activation of 16384 x 4096 elements 100 us).
+template <typename T>
+__device__ __forceinline__ float normal_cdf(float z, float& density) {
+    if (sizeof(T) == 4) {
+        density = 0.39894228040143268f * expf(-0.5f * z * z);
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f));
+    }
+    const float g = fast_exp(-0.5f * z * z), t = fast_inverse(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float tail = 0.5f * p * t * g;
+    density = 0.39894228040143268f * g;
+    return z < 0.f ? tail : 1.f - tail;
+}
 // act and its derivative.  NaN stays NaN.
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+template <typename T>
 __device__ __forceinline__ float act_of(float z, int act) {
     if (act == GCN_ACT_RELU) return z < 0.f ? 0.f : z;
-    if (act == GCN_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if (act == GCN_ACT_SILU) return z / (1.f + expf(-z));
+    if (act == GCN_ACT_GELU) {
+        float density;
+        return z * normal_cdf<T>(z, density);
+    }
+    if (act == GCN_ACT_SILU) return z * sigmoid(z);
     return z;
 }
+template <typename T>
 __device__ __forceinline__ float slope_of(float z, int act) {
     if (act == GCN_ACT_RELU) return z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
-    if (act == GCN_ACT_GELU)
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    if (act == GCN_ACT_GELU) {
+        float density;
+        const float phi = normal_cdf<T>(z, density);
+        return fmaf(z, density, phi);
+    }
     if (act == GCN_ACT_SILU) {
         const float s = sigmoid(z);
-        return s * (1.f + z * (1.f - s));
+        return s * fmaf(z, 1.f - s, 1.f);
     }
     return 1.f;
 }
@@ -62,7 +102,7 @@ __device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int 
     if (a.Z) store_vec_part((T*)a.Z + m * a.ldz + n, from_floats<T>(d), count);
     if (a.act != GCN_ACT_NONE)
 #pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = act_of(d[e], a.act);
+        for (int e = 0; e < E; ++e) d[e] = act_of<T>(d[e], a.act);
     if (a.R) {
         float r[E];
         to_floats<T>(load_vec_part((const T*)a.R + m * a.ldr + n, count), r);
@@ -348,7 +388,7 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
     }
     // Results leave through LDS, a wavefront's own part of it: what the matrix unit leaves with a lane are four columns of a row, and whole rows of the
     // wavefront's tile go out together, 16 bytes per lane.  The pieces of a row are moved about by the row, so that the lanes' writes meet all banks.
-    constexpr int PHASES = BM * BN * 4 > 2 * STAGE ? BM * BN * 4 / (2 * STAGE) : 1, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
+    constexpr int PHASES = (BM * BN * 4 + 2 * STAGE - 1) / (2 * STAGE), FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
     static_assert(FM % PHASES == 0, "whole phases");
     constexpr int HALF = WM * WN / 2;                             // wavefronts that have their part in the first stage
     static_assert(HALF * ROWS * PIECES * 16 <= STAGE, "results have room");
