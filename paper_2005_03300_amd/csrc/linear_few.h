@@ -89,7 +89,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int s
                 for (int e = 0; e < E; ++e)
                     if (e < count) p[e] = d[e];
             } else {
-                finish<T>(a, row, n0 + c, count, d);
+                float r_[E];
+                finish<T>(a, row, n0 + c, count, d, false, r_);
             }
         }
     }

@@ -89,9 +89,9 @@ __device__ __forceinline__ float slope_of(float z, int act) {
     return 1.f;
 }
 
-// What becomes of the results of row m, columns n to n + E - 1, of which `count` are there.
+// What becomes of the results of row m, columns n to n + E - 1, of which `count` are there; r: the residual's, where they have been loaded already.
 template <typename T>
-__device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int count, float (&d)[Elem<T>::E]) {
+__device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int count, float (&d)[Elem<T>::E], bool loaded, float (&r)[Elem<T>::E]) {
     constexpr int E = Elem<T>::E;
     if (a.bias) {
         float b[E];
@@ -104,8 +104,7 @@ __device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int 
 #pragma unroll
         for (int e = 0; e < E; ++e) d[e] = act_of<T>(d[e], a.act);
     if (a.R) {
-        float r[E];
-        to_floats<T>(load_vec_part((const T*)a.R + m * a.ldr + n, count), r);
+        if (!loaded) to_floats<T>(load_vec_part((const T*)a.R + m * a.ldr + n, count), r);
 #pragma unroll
         for (int e = 0; e < E; ++e) d[e] = fmaf(a.rho, r[e], d[e]);
     }
@@ -409,44 +408,61 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
         const int c = (lane % LANES) * E, n = n0 + wn + c, count = a.N - n;
         // a piece that the end of a dimension cut holds the last whole one: its last `count` columns, and likewise rows
         const bool shifted = LB == BY_MN && !DIRECT && count < E && a.N >= E;
+        // the residual's pieces of several rows are on their way together (one after the other: 130 us of 16384 x 4096 x 4096 in bf16)
+        constexpr int AHEAD = ROWS / STEP < 4 ? ROWS / STEP : 4;
+        const bool ahead = !part && a.R && a.N >= E;
+        const int by = settle_by<E>(n, a.N);
 #pragma nounroll
-        for (int row = lane / LANES; row < ROWS; row += STEP) {
-            int64_t m = m0 + wm + ph * ROWS + row;
-            float d[E];
+        for (int row0 = lane / LANES; row0 < ROWS; row0 += AHEAD * STEP) {
+            Words<T, E> near[AHEAD] = {};
+            if (ahead)
 #pragma unroll
-            for (int e = 0; e < E; e += 4) {
-                const v4f x = *reinterpret_cast<const v4f*>(mine + row * (PIECES * 16) + ((((c + e) / 4) ^ (row & (PIECES - 1))) << 4));
-#pragma unroll
-                for (int q = 0; q < 4; ++q) d[e + q] = x[q];
-            }
-            if (LA == BY_MN && !DIRECT && a.M >= E) {
-                const int64_t first = m - row % E;                 // of the piece (a wavefront's rows are whole ones)
-                if (first + E > a.M) {
-                    if (first >= a.M) continue;
-                    m += a.M - E - first;
-                    if (m < first) continue;
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int64_t m = m0 + wm + ph * ROWS + row0 + u * STEP;
+                    near[u] = load_near<E>((const T*)a.R + (m < a.M ? m : a.M - 1) * a.ldr, n, a.N);
                 }
-            }
-            if (m >= a.M || count <= 0) continue;
-            if (shifted)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    float x = d[e];
+            for (int u = 0; u < AHEAD; ++u) {
+                const int row = row0 + u * STEP;
+                int64_t m = m0 + wm + ph * ROWS + row;
+                float d[E];
 #pragma unroll
-                    for (int o = 1; o < E; ++o) x = e + o < E && E - count == o ? d[e + o < E ? e + o : e] : x;
-                    d[e] = x;
+                for (int e = 0; e < E; e += 4) {
+                    const v4f x = *reinterpret_cast<const v4f*>(mine + row * (PIECES * 16) + ((((c + e) / 4) ^ (row & (PIECES - 1))) << 4));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[e + q] = x[q];
                 }
-            if (part) {
-                float* const p = part + m * a.N + n;
-                if (count >= E)
+                if (LA == BY_MN && !DIRECT && a.M >= E) {
+                    const int64_t first = m - row % E;             // of the piece (a wavefront's rows are whole ones)
+                    if (first + E > a.M) {
+                        if (first >= a.M) continue;
+                        m += a.M - E - first;
+                        if (m < first) continue;
+                    }
+                }
+                if (m >= a.M || count <= 0) continue;
+                if (shifted)
 #pragma unroll
-                    for (int e = 0; e < E; e += 4) *reinterpret_cast<f4u*>(p + e) = f4u{d[e], d[e + 1], d[e + 2], d[e + 3]};
-                else
+                    for (int e = 0; e < E; ++e) {
+                        float x = d[e];
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (e < count) p[e] = d[e];
-            } else {
-                finish<T>(a, m, n, count, d);
+                        for (int o = 1; o < E; ++o) x = e + o < E && E - count == o ? d[e + o < E ? e + o : e] : x;
+                        d[e] = x;
+                    }
+                if (part) {
+                    float* const p = part + m * a.N + n;
+                    if (count >= E)
+#pragma unroll
+                        for (int e = 0; e < E; e += 4) *reinterpret_cast<f4u*>(p + e) = f4u{d[e], d[e + 1], d[e + 2], d[e + 3]};
+                    else
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (e < count) p[e] = d[e];
+                } else {
+                    float r[E];
+                    floats_of<E, T>(by ? settle<E, T>(near[u], by) : __builtin_bit_cast(Vec<T>, near[u]), r);
+                    finish<T>(a, m, n, count, d, ahead, r);
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -483,7 +499,8 @@ __global__ __launch_bounds__(64 * (SHARES > 1 ? SHARES : 4)) void k_linear_join(
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] += add[w][threadIdx.x][e];
     }
-    if (m < a.M) finish<T>(a, m, n, count, d);
+    float r[E];
+    if (m < a.M) finish<T>(a, m, n, count, d, false, r);
 }
 
 template <typename T> int linear_forward_of(const TileArgs& a, hipStream_t s);          // A by k, B by n, with the epilogue
