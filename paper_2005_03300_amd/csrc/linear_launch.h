@@ -1,6 +1,7 @@
 // Which tiles a product takes, and its launch, for one element type.
 #pragma once
 #include "linear_few.h"
+#include "linear_thirds.h"
 #include "linear_tile.h"
 
 namespace gcn {
@@ -37,10 +38,14 @@ static int launch_tile(TileArgs a, int splits, hipStream_t s) {
         a.part = (float*)p;
     }
     const dim3 grid((unsigned)(tm * tn), (unsigned)splits);
-    if (whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N))
-        hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, true>), grid, dim3(WM * WN * 64), 0, s, a);
-    else
-        hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, false>), grid, dim3(WM * WN * 64), 0, s, a);
+    if constexpr (sizeof(T) == 4) {
+        hipLaunchKernelGGL((k_linear_thirds<BM, BN, WM, WN, LA, LB>), grid, dim3(WM * WN * 64), 0, s, a);
+    } else {
+        if (whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N))
+            hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, true>), grid, dim3(WM * WN * 64), 0, s, a);
+        else
+            hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, false>), grid, dim3(WM * WN * 64), 0, s, a);
+    }
     GCN_LAUNCH_CHECK();
     if (splits > 1) return launch_join<T>(a, splits, s);
     return GCN_OK;
@@ -55,13 +60,13 @@ struct TileKind {
     double full, way;             // share of the matrix units' rate with that many; microseconds that a stage takes to come from memory
 };
 // The choice with the least estimated time.  A stage takes what the products of all workgroups of a compute unit do, at a rate that grows with the tiles
-// (16384 x 4096 x 4096 in bf16: 1.2 PFLOP/s at 256 x 256, 1.05 at 128 x 128, 0.73 at 64 x 64; 4096 x 2048 x 4096 in fp32: 132 and 125 TFLOP/s at 128 and 64), but no
+// (16384 x 4096 x 4096 in bf16: 1.2 PFLOP/s at 256 x 256, 1.05 at 128 x 128, 0.73 at 64 x 64; 8192 x 8192 x 8192 in fp32: 210 and 155 TFLOP/s at 128 and 64), but no
 // less than a stage's way from memory, which is longer through registers.  Splits fill the chip where there are few tiles, and cost partial results written and
 // read again and a launch.
 inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, bool direct, int64_t cus) {
     static const TileKind KINDS16[] = {{256, 1, 1.0, 1.2}, {128, 2, 0.88, 0.8}, {64, 5, 0.61, 0.6}};
-    static const TileKind KINDS32[] = {{128, 2, 1.0, 0.8}, {64, 5, 0.93, 0.6}};      // (larger ones win nothing, and there are fewer of them)
-    const double rate = fp32 ? 0.52e6 : 4.7e6;                    // FLOP per microsecond of one compute unit
+    static const TileKind KINDS32[] = {{128, 2, 1.0, 1.1}, {64, 3, 0.74, 0.5}};               // (larger ones win nothing, and there are fewer of them)
+    const double rate = fp32 ? 0.82e6 : 4.7e6;                    // FLOP per microsecond of one compute unit
     const int64_t depth = fp32 ? 32 : 64, stages = (K + depth - 1) / depth;
     TileChoice best{64, 1};
     double least = 1e300;
@@ -89,7 +94,7 @@ inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, bool 
 template <typename T, int LA, int LB>
 static int linear_product(const TileArgs& a, hipStream_t s) {
     const bool direct = whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N);
-    const TileChoice c = choose_tiles(a.M, a.N, a.K, sizeof(T) == 4, direct, device_info().cus);
+    const TileChoice c = choose_tiles(a.M, a.N, a.K, sizeof(T) == 4, sizeof(T) == 2 && direct, device_info().cus);
     if constexpr (sizeof(T) == 2)
         if (c.edge == 256) return launch_tile<T, 256, 256, 2, 4, LA, LB>(a, c.splits, s);
     if (c.edge == 128) return launch_tile<T, 128, 128, 2, 2, LA, LB>(a, c.splits, s);

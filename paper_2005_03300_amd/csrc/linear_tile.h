@@ -279,6 +279,100 @@ __device__ __forceinline__ v4f mma(Vec<float> p, Vec<float> q, v4f acc) {
     return acc;
 }
 
+// The tile of a workgroup.  Neighbouring workgroups run on different XCDs, each with an L2 of its own: every XCD gets a contiguous share of the tiles, and walks it in
+// groups of eight rows of tiles, column by column, so that what runs at one time shares operands.
+__device__ __forceinline__ void tile_place(const TileArgs& a, int& tm, int& tn) {
+    const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, b = blockIdx.x, x = b & 7, q = tiles >> 3, r = tiles & 7;
+    const int64_t t = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + (b >> 3);
+    const int64_t per = (int64_t)8 * a.tiles_n, g = t / per;
+    const int first = (int)(g * 8), rows = a.tiles_m - first < 8 ? a.tiles_m - first : 8, in = (int)(t % per);
+    tm = first + in % rows;
+    tn = in / rows;
+}
+
+// A wavefront's results, 16 FM rows from m0 and 16 FN columns from n0 on, leave through LDS, its own part `mine` of it, in PHASES: what the matrix unit leaves with a
+// lane are four columns of a row, and whole rows of the wavefront's tile go out together, 16 bytes per lane.  The pieces of a row are moved about by the row, so that
+// the lanes' writes meet all banks.  CUT_M, CUT_N: pieces that the end of a dimension cuts were taken from its last whole one.
+template <typename T, int FM, int FN, int PHASES, bool CUT_M, bool CUT_N>
+__device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[FM][FN], char* mine, int64_t m0, int n0, int lane) {
+    constexpr int E = Elem<T>::E, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
+    static_assert(FM % PHASES == 0, "whole phases");
+    float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N : nullptr;
+#pragma unroll
+    for (int ph = 0; ph < PHASES; ++ph) {
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int row = i * 16 + (lane & 15);
+                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[ph * FP + i][j];
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        constexpr int LANES = FN * 16 / E, STEP = 64 / LANES;     // lanes of a row, rows at a time
+        const int c = (lane % LANES) * E, n = n0 + c, count = a.N - n;
+        // a piece that the end of a dimension cut holds the last whole one: its last `count` columns, and likewise rows
+        const bool shifted = CUT_N && count < E && a.N >= E;
+        // the residual's pieces of several rows are on their way together (one after the other: 130 us of 16384 x 4096 x 4096 in bf16)
+        constexpr int AHEAD = ROWS / STEP < 4 ? ROWS / STEP : 4;
+        const bool ahead = !part && a.R && a.N >= E;
+        const int by = settle_by<E>(n, a.N);
+#pragma nounroll
+        for (int row0 = lane / LANES; row0 < ROWS; row0 += AHEAD * STEP) {
+            Words<T, E> near[AHEAD] = {};
+            if (ahead)
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const int64_t m = m0 + ph * ROWS + row0 + u * STEP;
+                    near[u] = load_near<E>((const T*)a.R + (m < a.M ? m : a.M - 1) * a.ldr, n, a.N);
+                }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int row = row0 + u * STEP;
+                int64_t m = m0 + ph * ROWS + row;
+                float d[E];
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    const v4f x = *reinterpret_cast<const v4f*>(mine + row * (PIECES * 16) + ((((c + e) / 4) ^ (row & (PIECES - 1))) << 4));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[e + q] = x[q];
+                }
+                if (CUT_M && a.M >= E) {
+                    const int64_t first = m - row % E;             // of the piece (a wavefront's rows are whole ones)
+                    if (first + E > a.M) {
+                        if (first >= a.M) continue;
+                        m += a.M - E - first;
+                        if (m < first) continue;
+                    }
+                }
+                if (m >= a.M || count <= 0) continue;
+                if (shifted)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        float x = d[e];
+#pragma unroll
+                        for (int o = 1; o < E; ++o) x = e + o < E && E - count == o ? d[e + o < E ? e + o : e] : x;
+                        d[e] = x;
+                    }
+                if (part) {
+                    float* const p = part + m * a.N + n;
+                    if (count >= E)
+#pragma unroll
+                        for (int e = 0; e < E; e += 4) *reinterpret_cast<f4u*>(p + e) = f4u{d[e], d[e + 1], d[e + 2], d[e + 3]};
+                    else
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (e < count) p[e] = d[e];
+                } else {
+                    float r[E];
+                    floats_of<E, T>(by ? settle<E, T>(near[u], by) : __builtin_bit_cast(Vec<T>, near[u]), r);
+                    finish<T>(a, m, n, count, d, ahead, r);
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
 // BM x BN results of a workgroup of WM x WN wavefronts, 128 bytes of k at a time (64 values of 16 bits, 32 of 32), two such stages in LDS: one is
 // fetched while the other is multiplied.  A wavefront's results are the transpose of what the matrix unit is given (B's columns as its rows), so that a lane
 // holds four neighbouring columns of one row.
@@ -294,17 +388,8 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
     // that may be on its way to the same array (16384 x 4096 x 4096 in bf16 with one: 935 TFLOP/s).
     __shared__ __attribute__((aligned(16))) char stage0[STAGE], stage1[STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    // Neighbouring workgroups run on different XCDs, each with an L2 of its own: every XCD gets a contiguous share of the tiles, and walks it in
-    // groups of eight rows of tiles, column by column, so that what runs at one time shares operands.
     int tm, tn;
-    {
-        const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n, b = blockIdx.x, x = b & 7, q = tiles >> 3, r = tiles & 7;
-        const int64_t t = (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + (b >> 3);
-        const int64_t per = (int64_t)8 * a.tiles_n, g = t / per;
-        const int first = (int)(g * 8), rows = a.tiles_m - first < 8 ? a.tiles_m - first : 8, in = (int)(t % per);
-        tm = first + in % rows;
-        tn = in / rows;
-    }
+    tile_place(a, tm, tn);
     const int64_t m0 = (int64_t)tm * BM;
     const int n0 = tn * BN;
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
@@ -385,88 +470,12 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
                 if (k < ke) step(stage0);
             }
     }
-    // Results leave through LDS, a wavefront's own part of it: what the matrix unit leaves with a lane are four columns of a row, and whole rows of the
-    // wavefront's tile go out together, 16 bytes per lane.  The pieces of a row are moved about by the row, so that the lanes' writes meet all banks.
-    constexpr int PHASES = (BM * BN * 4 + 2 * STAGE - 1) / (2 * STAGE), FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
-    static_assert(FM % PHASES == 0, "whole phases");
+    constexpr int PHASES = (BM * BN * 4 + 2 * STAGE - 1) / (2 * STAGE), PART = BM / WM / PHASES * (BN / WN) * 4;
     constexpr int HALF = WM * WN / 2;                             // wavefronts that have their part in the first stage
-    static_assert(HALF * ROWS * PIECES * 16 <= STAGE, "results have room");
-    char* const mine = (wave < HALF ? stage0 : stage1) + (wave % HALF) * (ROWS * PIECES * 16);
-    float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N : nullptr;
+    static_assert(HALF * PART <= STAGE, "results have room");
     __syncthreads();
-#pragma unroll
-    for (int ph = 0; ph < PHASES; ++ph) {
-#pragma unroll
-        for (int i = 0; i < FP; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int row = i * 16 + (lane & 15);
-                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[ph * FP + i][j];
-            }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        constexpr int LANES = FN * 16 / E, STEP = 64 / LANES;     // lanes of a row, rows at a time
-        const int c = (lane % LANES) * E, n = n0 + wn + c, count = a.N - n;
-        // a piece that the end of a dimension cut holds the last whole one: its last `count` columns, and likewise rows
-        const bool shifted = LB == BY_MN && !DIRECT && count < E && a.N >= E;
-        // the residual's pieces of several rows are on their way together (one after the other: 130 us of 16384 x 4096 x 4096 in bf16)
-        constexpr int AHEAD = ROWS / STEP < 4 ? ROWS / STEP : 4;
-        const bool ahead = !part && a.R && a.N >= E;
-        const int by = settle_by<E>(n, a.N);
-#pragma nounroll
-        for (int row0 = lane / LANES; row0 < ROWS; row0 += AHEAD * STEP) {
-            Words<T, E> near[AHEAD] = {};
-            if (ahead)
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    const int64_t m = m0 + wm + ph * ROWS + row0 + u * STEP;
-                    near[u] = load_near<E>((const T*)a.R + (m < a.M ? m : a.M - 1) * a.ldr, n, a.N);
-                }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int row = row0 + u * STEP;
-                int64_t m = m0 + wm + ph * ROWS + row;
-                float d[E];
-#pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    const v4f x = *reinterpret_cast<const v4f*>(mine + row * (PIECES * 16) + ((((c + e) / 4) ^ (row & (PIECES - 1))) << 4));
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) d[e + q] = x[q];
-                }
-                if (LA == BY_MN && !DIRECT && a.M >= E) {
-                    const int64_t first = m - row % E;             // of the piece (a wavefront's rows are whole ones)
-                    if (first + E > a.M) {
-                        if (first >= a.M) continue;
-                        m += a.M - E - first;
-                        if (m < first) continue;
-                    }
-                }
-                if (m >= a.M || count <= 0) continue;
-                if (shifted)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        float x = d[e];
-#pragma unroll
-                        for (int o = 1; o < E; ++o) x = e + o < E && E - count == o ? d[e + o < E ? e + o : e] : x;
-                        d[e] = x;
-                    }
-                if (part) {
-                    float* const p = part + m * a.N + n;
-                    if (count >= E)
-#pragma unroll
-                        for (int e = 0; e < E; e += 4) *reinterpret_cast<f4u*>(p + e) = f4u{d[e], d[e + 1], d[e + 2], d[e + 3]};
-                    else
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (e < count) p[e] = d[e];
-                } else {
-                    float r[E];
-                    floats_of<E, T>(by ? settle<E, T>(near[u], by) : __builtin_bit_cast(Vec<T>, near[u]), r);
-                    finish<T>(a, m, n, count, d, ahead, r);
-                }
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
+    leave_tile<T, FM, FN, PHASES, LA == BY_MN && !DIRECT, LB == BY_MN && !DIRECT>(a, acc, (wave < HALF ? stage0 : stage1) + (wave % HALF) * PART, m0 + wm,
+                                                                                 n0 + wn, lane);
 }
 
 // The partial results of the splits, added in order, and what the layer does with the sum: 16 bytes of it per thread; SHARES threads, a wavefront apart, take a
