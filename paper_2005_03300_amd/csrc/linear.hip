@@ -106,6 +106,7 @@ extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int ty
     if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
     if (!known_act(act)) return fail(GCN_ERR_BADARG, "%s: unknown activation %d", who, act);
     if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (f_in > (1 << 30) || f_out > (1 << 30)) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^30", who);
     if (ldx < f_in || ldw < f_out || ldy < f_out || (R && ldr < f_out) || (Z && ldz < f_out))
         return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     const size_t b = elem_bytes(type);
@@ -132,6 +133,7 @@ extern "C" int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int t
     if (curved && (products || dbias || dZ) && !Z) return fail(GCN_ERR_BADARG, "%s: the activation's derivative needs Z", who);
     if (curved && products && !dZ) return fail(GCN_ERR_BADARG, "%s: the products need dZ as workspace", who);
     if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (f_in > (1 << 30) || f_out > (1 << 30)) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^30", who);
     if (lddy < f_out || (X && ldx < f_in) || (W && ldw < f_out) || (Z && ldz < f_out) || (dZ && lddz < f_out) || (dX && lddx < f_in) ||
         (dW && lddw < f_out) || (dR && lddr < f_out))
         return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);

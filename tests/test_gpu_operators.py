@@ -229,6 +229,50 @@ def test_linear_in_place_and_special_values(type_, n, K, N):
     assert bool(torch.isnan(Y[1]).all()) and bool((Y[keep] >= 0).all())
 
 
+@pytest.mark.parametrize("n,K,N", [(300, 200, 130), (2049, 72, 1608)])
+def test_linear_fp32_keeps_its_bits_and_infinities(n, K, N):
+    """Products of fp32 numbers keep 24 bits over the whole range of magnitudes; infinities, NaN and numbers next to the largest one in either operand give what
+    fp32 products give, and change no other result."""
+    g = lib()
+    gen = gen_of("thirds", n)
+    scale = torch.exp2(torch.randint(-20, 21, (n, K), generator=gen).double())
+    X = (torch.randn(n, K, generator=gen, dtype=torch.float64) * scale).float().cuda()
+    W = (torch.randn(K, N, generator=gen, dtype=torch.float64) * torch.exp2(torch.randint(-20, 21, (K, N), generator=gen).double())).float().cuda()
+    Y = torch.empty(n, N, device="cuda")
+    g.gcn_linear_forward(X, W, Y)
+    x, w = X.double().cpu(), W.double().cpu()
+    check(Y, x @ w, (K + 2) * EPS * (x.abs() @ w.abs()), "Y")
+    x1, w1 = X.clone(), W.clone()
+    big = torch.finfo(torch.float32).max
+    x1[3, 1], x1[70, K - 1], x1[n - 1, 5], x1[140, 2] = float("inf"), float("-inf"), float("nan"), big
+    w1[:, 4] *= 2.0 ** -40                                     # (so that the largest number's products are finite in one column)
+    w1[6, N - 1] = float("inf")
+    got = torch.empty_like(Y)
+    g.gcn_linear_forward(x1, w1, got)
+    rows, cols = [i for i in range(n) if i not in (3, 70, n - 1, 140)], [j for j in range(N) if j not in (4, N - 1)]
+    assert torch.equal(got[rows][:, cols], Y[rows][:, cols])
+    ref = x1.double().cpu() @ w1.double().cpu()
+    ref = torch.where(ref.abs() > big, ref.sign() * float("inf"), ref)
+    for i in (3, 70, n - 1):
+        assert torch.equal(got[i].double().cpu().nan_to_num(7.0, 8.0, 9.0), ref[i].nan_to_num(7.0, 8.0, 9.0)), i
+    assert torch.equal(torch.isfinite(got[140]).cpu(), torch.isfinite(ref[140])) and bool(torch.isfinite(got[140, 4]))
+    size = x1.abs().double().cpu() @ w1.abs().double().cpu()
+    assert abs(float(got[140, 4]) - float(ref[140, 4])) <= (K + 2) * EPS * float(size[140, 4])
+    assert torch.equal(got[rows][:, N - 1].cpu().double().sign(), x1[rows][:, 6].cpu().double().sign()) and bool(torch.isinf(got[rows][:, N - 1]).all())
+    # the gradients' products too
+    dX, dW = torch.empty_like(X), torch.empty_like(W)
+    dY = normal(gen, (n, N), "f32").cuda()
+    g.gcn_linear_backward(X, W, None, dY, dX=dX, dW=dW)
+    d1 = dY.clone()
+    d1[5, 7] = float("inf")
+    dX1, dW1 = torch.empty_like(X), torch.empty_like(W)
+    g.gcn_linear_backward(X, W, None, d1, dX=dX1, dW=dW1)
+    others = [i for i in range(n) if i != 5]
+    assert torch.equal(dX1[others], dX[others]) and torch.equal(dX1[5].sign(), W[:, 7].sign()) and bool(torch.isinf(dX1[5]).all())
+    others = [j for j in range(N) if j != 7]
+    assert torch.equal(dW1[:, others], dW[:, others]) and torch.equal(dW1[:, 7].sign(), X[5].sign()) and bool(torch.isinf(dW1[:, 7]).all())
+
+
 def test_linear_backward_in_place_of_its_inputs():
     g = lib()
     gen = gen_of("aliases")
@@ -262,6 +306,9 @@ def test_linear_refusals():
     refused(lambda: fwd(x=None), "NULL")
     refused(lambda: fwd(n=0), "positive")
     refused(lambda: fwd(fi=-1), "positive")
+    with pytest.raises(g.GcnError) as e:
+        fwd(fo=(1 << 30) + 1)
+    assert e.value.code == -2
     refused(lambda: fwd(type_=3), "element type")
     refused(lambda: fwd(act=4), "activation")
     refused(lambda: fwd(ldx=7), "leading dimension")
