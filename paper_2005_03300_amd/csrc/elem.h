@@ -38,6 +38,11 @@ template <typename T>
 __device__ __forceinline__ void store_vec(T* p, Vec<T> v) {
     *reinterpret_cast<typename Elem<T>::Loose*>(p) = __builtin_bit_cast(typename Elem<T>::Loose, v);
 }
+typedef float v4f_loose __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T>
+__device__ __forceinline__ void stream_vec(T* p, Vec<T> v) {       // past the caches
+    __builtin_nontemporal_store((v4f_loose)__builtin_bit_cast(v4f, v), reinterpret_cast<v4f_loose*>(p));
+}
 template <typename T>
 __device__ __forceinline__ v4f load4(const T* p) {
     return __builtin_convertvector(__builtin_bit_cast(Vec4<T>, *reinterpret_cast<const typename Elem<T>::Loose4*>(p)), v4f);
