@@ -93,7 +93,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
     // mean and deviation of the row's x
     auto statistics = [&](const float(&x)[E], float& mean, float& rstd) {
         float s[1] = {0.f};
-        if (LAYER) {
+        if (LAYER && g.layer) {
 #pragma unroll
             for (int e = 0; e < E; ++e) s[0] += e < count ? x[e] : 0.f;
             join_lanes<L>(s, meet, turn);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
 template <typename T, int L, int E, bool LAYER>
 __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_back(NormArgs g) {
     using R = NormRows<T, L, E>;
-    constexpr int SUMS = LAYER ? 4 : 2;                // without a mean there are no biases, or they are given to no one
+    constexpr int SUMS = LAYER ? 4 : 2;
     __shared__ float meet[2][16][4];
     int turn = 0;
     const int c = R::column(), count = g.f - c < 0 ? 0 : (g.f - c > E ? E : g.f - c);
@@ -209,7 +209,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
                 s[1] += gw[e];
             }
             join_lanes<L>(s, meet, turn);
-            const float along = s[0] * inv_f, mean = LAYER ? s[1] * inv_f : 0.f;
+            const float along = s[0] * inv_f, mean = LAYER && g.layer ? s[1] * inv_f : 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) dx[e] = fmaf(now.st.w, gw[e] - fmaf(xh[e], along, mean), dx[e]);
         }
@@ -237,7 +237,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
             if (g.w_post || g.gate == 1) join_lanes<L>(s, meet, turn);
             if (g.dA && g.gate == 1 && c == 0 && there) ((T*)g.dA)[i * g.ldda] = (T)s[2];
             if (g.w_post) {
-                const float along = s[0] * inv_f, mean = LAYER ? s[1] * inv_f : 0.f;
+                const float along = s[0] * inv_f, mean = LAYER && g.layer ? s[1] * inv_f : 0.f;
 #pragma unroll
                 for (int e = 0; e < E; ++e) dx[e] = rstd_u * (dx[e] - fmaf(u[e], along, mean));
             }
@@ -526,7 +526,7 @@ static int norm_forward(const NormArgs& g, hipStream_t s) {
             using R = NormRows<T, L, E>;
             const int64_t groups = (g.n + R::ROWS - 1) / R::ROWS, most = cus * (2048 / R::THREADS);
             const dim3 grid((unsigned)(groups < most ? groups : most));
-            // a norm without mean and biases has a kernel of its own
+            // (LAYER: a mean or biases; the norm without either has a kernel of its own)
             if (g.layer || g.b_post || g.b_pre) hipLaunchKernelGGL((k_block_norm<T, L, E, true>), grid, dim3(R::THREADS), 0, s, g);
             else hipLaunchKernelGGL((k_block_norm<T, L, E, false>), grid, dim3(R::THREADS), 0, s, g);
         }

@@ -508,6 +508,39 @@ def test_block_norm_backward(type_, at):
     assert all(t is None or torch.equal(t, v[k]) for k, t in v2.items())
 
 
+@pytest.mark.parametrize("f", [6, 300, 4100, 9000])
+@pytest.mark.parametrize("layer", [False, True])
+def test_block_norm_biases_go_with_either_norm(f, layer):
+    """Biases with the root-mean-square norm, and a layer norm without any; forward, and backward by differentiation of the plain form."""
+    g = lib()
+    gen = gen_of("biases", f, layer)
+    n, kind = 7, g.NORM_LAYER if layer else g.NORM_RMS
+    X, U, A, C, E = (normal(gen, (n, f), "f32") for _ in range(5))
+    w, wp = (1 + 0.2 * torch.randn(f, generator=gen) for _ in range(2))
+    b, bp = (None, None) if layer else (0.3 * torch.randn(f, generator=gen) for _ in range(2))
+    leaf = {k: t.double().requires_grad_() for k, t in dict(X=X, U=U, A=A, w=w, wp=wp, b=b, bp=bp).items() if t is not None}
+
+    def unit(x):
+        x = x - x.mean(1, keepdim=True) if layer else x
+        return x / torch.sqrt((x * x).mean(1, keepdim=True) + NORM_EPS)
+    x = leaf["X"] + torch.sigmoid(leaf["A"]) * (unit(leaf["U"]) * leaf["wp"] + leaf.get("bp", 0))
+    h = unit(x) * leaf["w"] + leaf.get("b", 0)
+    want = dict(zip(leaf, torch.autograd.grad((C.double() * x).sum() + (E.double() * h).sum(), list(leaf.values()))))
+    dev = {k: t.cuda() for k, t in dict(X=X, U=U, A=A, w=w, wp=wp, b=b, bp=bp).items() if t is not None}
+    Xo, H, stats = torch.empty(n, f, device="cuda"), torch.empty(n, f, device="cuda"), torch.empty(n, 4, device="cuda")
+    g.gcn_block_norm_forward(dev["X"], dev["U"], Xo, H, w_pre=dev["w"], b_pre=dev.get("b"), A=dev["A"], w_post=dev["wp"], b_post=dev.get("bp"),
+                             stats=stats, kind=kind, eps=NORM_EPS)
+    size = 4 * DEPTH * EPS * (1 + f ** 0.5)                   # of numbers of about 1, in rows whose largest are some times that
+    check(Xo, x.detach(), torch.full((1, 1), size, dtype=torch.float64), "X'")
+    check(H, h.detach(), torch.full((1, 1), size, dtype=torch.float64), "H")
+    got = {k: torch.empty_like(t) for k, t in dev.items()}
+    g.gcn_block_norm_backward(dev["U"], Xo, stats, C.cuda(), E.cuda(), got["X"], got["U"], w_pre=dev["w"], A=dev["A"], dA=got["A"],
+                              w_post=dev["wp"], b_post=dev.get("bp"), dw_post=got["wp"], db_post=got.get("bp"), dw_pre=got["w"],
+                              db_pre=got.get("b"), kind=kind)
+    for k, t in want.items():
+        check(got[k], t, torch.full((1,) * t.dim(), 4 * size, dtype=torch.float64), "d" + k)
+
+
 @pytest.mark.parametrize("f", [48, 5000])
 def test_block_norm_gradients_of_one_side(f):
     """Only dX', only dH, and no block."""
