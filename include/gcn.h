@@ -317,7 +317,7 @@ int gcn_block_norm_backward(int64_t n, int32_t f, int type, int kind, const void
  *   G = grad_scale dloss/dZ
  * top: int32[n][k] (ld ldtop), the classes of the list; an index below 0 or from C on is no entry, and neither is one whose t is
  * -inf (a list shorter than k, a row that the teacher never saw: a row without entries adds nothing to the teacher's part).  An index that comes twice counts as
- * two entries.  t: n x k (ld ldt) and Z, G of element type `type`.  labels: int32[n] or NULL; a label outside [0, C) is none.  m: the divisor
+ * two entries.  A weight of 0 leaves its part out.  t: n x k (ld ldt) and Z, G of element type `type`.  labels: int32[n] or NULL; a label outside [0, C) is none.  m: the divisor
  * (host value, for instance the number of rows with a list or a label).  loss: fp32, written.  G: n x C or NULL; it may be Z.
  * Logits of -inf are classes that cannot be (q = 0); a row of them alone has no softmax, and gives NaN if it has a list or a label.  Exponentials
  * and row sums are fp32; the loss is added up in fp64 in a fixed order.  1 <= k <= min(C, GCN_DISTILL_MOST).  Rows up to

@@ -106,7 +106,7 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
             if (j < a.k) {
                 at = a.top[i * a.ldtop + j];
                 t = (float)((const T*)a.t)[i * a.ldt + j];
-                if (at >= a.C || t == -INFINITY) at = -1;
+                if (at >= a.C || t == -INFINITY || a.wt == 0.f) at = -1;       // (a part of weight 0 is none, whatever it is)
                 if (at >= 0) {
                     high[1] = fmaxf(high[1], t);
                     high[2] = 1.f;

@@ -790,6 +790,29 @@ def test_distill_rows_without_anything():
     assert math.isnan(float(loss)) and bool(torch.isnan(G[3]).all()) and bool(torch.isfinite(G[[0, 1, 2, 4]]).all())
 
 
+def test_distill_weight_zero_leaves_a_part_out():
+    """A part of weight 0 adds nothing, also where its own loss would be infinite."""
+    g = lib()
+    n, C = 3, 30
+    Z = torch.randn(n, C, device="cuda")
+    Z[0, 2] = float("-inf")                                   # impossible, and named by the list and by the label of row 0
+    top = torch.full((n, 1), 2, dtype=torch.int32, device="cuda")
+    y = torch.full((n,), 2, dtype=torch.int32, device="cuda")
+    t = torch.ones(n, 1, device="cuda")
+    G, loss = torch.empty(n, C, device="cuda"), torch.empty(1, device="cuda")
+    g.gcn_distill(Z, top, t, loss, G, labels=y, w_teacher=1.0, w_label=1.0)
+    assert math.isinf(float(loss))
+    y[0] = 5
+    G1, one = torch.empty_like(G), torch.empty_like(loss)
+    g.gcn_distill(Z, top, t, loss, G, labels=y, w_teacher=0.0, w_label=1.0)
+    g.gcn_distill(Z, torch.full_like(top, -1), t, one, G1, labels=y, w_teacher=1.0, w_label=1.0)
+    assert math.isfinite(float(loss)) and torch.equal(loss, one) and torch.equal(G, G1)
+    top[0], y[0] = 5, 2
+    g.gcn_distill(Z, top, t, loss, G, labels=y, w_teacher=1.0, w_label=0.0)
+    g.gcn_distill(Z, top, t, one, G1, labels=None, w_teacher=1.0, w_label=1.0)
+    assert math.isfinite(float(loss)) and torch.equal(loss, one) and torch.equal(G, G1)
+
+
 def test_distill_refusals():
     g = lib()
     Z, G, t, loss = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda"), torch.zeros(4, 3, device="cuda"), torch.zeros(1, device="cuda")
