@@ -74,15 +74,23 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int s
 #pragma unroll
             for (int e = 0; e < 4; ++e) mine[(t * 16 + r) * ROW + (quarter * 4 + e) * C + q] = acc[t][q][e];
     __syncthreads();
+    // a thread for each result; the sum takes the place of the first wavefront's, which no other thread reads
+    for (int i = threadIdx.x; i < RT * 16 * 16 * C; i += FEW_WAVES * 64) {
+        float* const at = (float*)lds + i / (16 * C) * ROW + i % (16 * C);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) sum += at[w * RT * 16 * ROW];
+        *at = sum;
+    }
+    __syncthreads();
     constexpr int PIECES = 16 * C / E;
     if constexpr (16 * C % E == 0) {
         for (int i = threadIdx.x; i < RT * 16 * PIECES; i += FEW_WAVES * 64) {
             const int row = i / PIECES, c = i % PIECES * E, count = a.N - n0 - c;
             if (row >= a.M || count <= 0) continue;
-            float d[E] = {};
-            for (int w = 0; w < FEW_WAVES; ++w)
+            float d[E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) d[e] += ((const float*)lds)[(w * RT * 16 + row) * ROW + c + e];
+            for (int e = 0; e < E; ++e) d[e] = ((const float*)lds)[row * ROW + c + e];
             if (a.part) {
                 float* const p = a.part + ((int64_t)blockIdx.y * a.M + row) * a.N + n0 + c;
 #pragma unroll
