@@ -1,7 +1,7 @@
 // Products of fp32 matrices on the bf16 matrix units.  An fp32 number is the sum of three bf16 numbers exactly (x = h + m + l: each the nearest bf16 number to
 // what is left, 8 + 8 + 8 bits), and the product of two such sums has nine products of bf16 numbers, which the matrix unit multiplies exactly and adds in fp32.  Three of the
 // nine, m l', l m' and l l', are at most 2^-26 of x x' each and left out, below the rounding of an fp32 product; the other six take 96 cycles for what the fp32 units
-// take 256 for.  4096 x 2048 x 4096: see choose_tiles for the rates.
+// take 256 for.  8192 x 8192 x 8192 takes 5.2 ms (210 TFLOP/s; on the fp32 units at most 157, the library's product 151), 232965 x 602 x 128 260 us.
 // Infinities and NaN have no such sum, nor have numbers that round to infinity as bf16: with them m, and with it the result, is NaN.  A workgroup that has such
 // results computes its tile again on the fp32 units, and takes these results from there (and no other, so that none depends on another row's numbers).  Numbers below
 // 2^-100 lose bits of m and l below the smallest bf16 number, 2^-133.
@@ -63,7 +63,9 @@ struct Thirds {
     }
 };
 
-// As k_linear_tile through registers, for any alignment; one stage in LDS, the next one in registers, and other workgroups on the compute unit meanwhile.
+// As k_linear_tile through registers, for any alignment; one stage in LDS (three planes of 32 k: 48 KB of a 128 x 128 tile), the next one in registers, and another
+// workgroup on the compute unit meanwhile.  Bound by the matrix units (96 products of 16 cycles a stage and wavefront) and beside them the vector instructions that
+// split: 22 for four numbers, as many cycles as half of the products take at 128 x 128.  (A look at every number for infinities made them as many: 180 TFLOP/s.)
 template <int BM, int BN, int WM, int WN, int LA, int LB>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, BK = 32, E = 4;

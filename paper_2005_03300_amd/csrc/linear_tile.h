@@ -1,4 +1,4 @@
-// Tiles of a matrix product for the matrix units: D (M x N) = A (M x K) B (K x N), of 32- or 16-bit elements, sums in 32 bits, with what a linear
+// Tiles of a matrix product for the matrix units: D (M x N) = A (M x K) B (K x N), of 32- (see linear_thirds.h) or 16-bit elements, sums in 32 bits, with what a linear
 // layer does to its result where a tile leaves.  One kernel serves the three products of a layer and its backward pass, which differ in which of
 // their dimensions lies contiguous in memory:
 //   forward  X W      A by k, B by n
@@ -373,10 +373,14 @@ __device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[F
     }
 }
 
-// BM x BN results of a workgroup of WM x WN wavefronts, 128 bytes of k at a time (64 values of 16 bits, 32 of 32), two such stages in LDS: one is
+// D = A B for 16-bit elements: BM x BN results of a workgroup of WM x WN wavefronts, 128 bytes of k (64 values) at a time, two such stages in LDS: one is
 // fetched while the other is multiplied.  A wavefront's results are the transpose of what the matrix unit is given (B's columns as its rows), so that a lane
 // holds four neighbouring columns of one row.
-// DIRECT: rows of both operands at 16-byte addresses in whole pieces.
+// Bound by the matrix units for large products: 16384 x 4096 x 4096 in bf16 435 to 475 us (1.16 to 1.27 PFLOP/s) in each of the three directions.  A 256 x 256 tile reads
+// each operand half as often from L2 as 128 x 128 and LDS as often per product as its wavefronts' 128 x 64 results ask for (the units take 2048 cycles of a stage, LDS
+// 1536); 128 x 128 has two workgroups on a compute unit, so that one's end overlaps the other's products (1.05 PFLOP/s), and 64 x 64 is for results too small to fill
+// the chip otherwise.  128 bytes of k are a cache line of a row, and one barrier for 64 (256 x 256) products of a wavefront.
+// DIRECT: rows of both operands at 16-byte addresses in whole pieces: memory to LDS without registers.
 template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT>
 __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, E = Elem<T>::E, BK = 8 * E;
