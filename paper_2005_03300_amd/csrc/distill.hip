@@ -136,12 +136,12 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
                     if (POWER != 1) sum[1] *= plain_power<POWER>(by, m, now);
                     m = now;
                 }
-                if (m == -INFINITY) continue;
+                const float from = m == -INFINITY ? 0.f : m;     // (nothing yet: -inf adds 0, and NaN is not lost)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const float et = power((float)v[e], m, cT);
+                    const float et = power((float)v[e], from, cT);
                     sum[0] += et;
-                    if (POWER != 1) sum[1] += plain_power<POWER>(et, (float)v[e], m);
+                    if (POWER != 1) sum[1] += plain_power<POWER>(et, (float)v[e], from);
                 }
             }
         }
@@ -158,8 +158,8 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
                     sum[0] += et;
                     if (POWER != 1) sum[1] += plain_power<POWER>(et, (float)held[p][e], zh);
                 }
-        } else if (m == -INFINITY) {                             // nothing in it: 0, and NaN where the whole row is so
-            sum[0] = sum[1] = zh == -INFINITY ? NAN : 0.f;
+        } else if (m == -INFINITY) {                             // nothing in it: 0 (or NaN), and NaN where the whole row is so
+            if (zh == -INFINITY) sum[0] = sum[1] = NAN;
         } else {
             const float by = power(m, zh, cT);
             sum[0] *= by;

@@ -790,6 +790,25 @@ def test_distill_rows_without_anything():
     assert math.isnan(float(loss)) and bool(torch.isnan(G[3]).all()) and bool(torch.isfinite(G[[0, 1, 2, 4]]).all())
 
 
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0])
+@pytest.mark.parametrize("C", [40, 3000, 40000])
+def test_distill_nan_makes_its_row_nan(C, T, type_):
+    """A few NaN among a row's logits, also where a thread meets nothing else at first; the other rows keep their results."""
+    g = lib()
+    gen = gen_of("nan", C)
+    Z = normal(gen, (3, C), type_).cuda()
+    top, t = torch.tensor([[1, C - 1]] * 3, dtype=torch.int32, device="cuda"), normal(gen, (3, 2), type_).cuda()
+    y = torch.full((3,), 9, dtype=torch.int32, device="cuda")
+    want, G, loss = torch.empty_like(Z), torch.empty_like(Z), torch.empty(1, device="cuda")
+    g.gcn_distill(Z, top, t, loss, want, labels=y, temperature=T, w_teacher=0.5, w_label=0.5)
+    assert math.isfinite(float(loss))
+    Z[1, 16:24] = float("nan")
+    g.gcn_distill(Z, top, t, loss, G, labels=y, temperature=T, w_teacher=0.5, w_label=0.5)
+    assert math.isnan(float(loss)) and bool(torch.isnan(G[1]).all())
+    assert torch.equal(G[0], want[0]) and torch.equal(G[2], want[2])
+
+
 def test_distill_weight_zero_leaves_a_part_out():
     """A part of weight 0 adds nothing, also where its own loss would be infinite."""
     g = lib()
