@@ -266,7 +266,7 @@ int gcn_softmax_nll_masked(int64_t n, int32_t C, const float* Z, int64_t ldz, co
  * fp32, and bias, activation and residual applied to the fp32 sum; Z and Y are rounded once.  Products of fp32 elements are exact to 2^-26
  * of themselves (each number enters the matrix units as the sum of three bf16 numbers), with the infinities and NaN of fp32 products; numbers
  * below 2^-100 lose bits below 2^-133.  GELU of 16-bit elements is off by 2e-7 |Z| at most before it is rounded.  Y may be R (same address and leading dimension); no other output may overlap an input or another output.
- * Sums have a fixed order: repeated calls give the same bits.  Widths go up to 2^30 (RANGE).  Rows and leading dimensions of any alignment are taken; rows at
+ * Sums have a fixed order: repeated calls give the same bits.  Widths go up to 2^27 (RANGE).  Rows and leading dimensions of any alignment are taken; rows at
  * 16-byte addresses (and widths of whole 16 bytes) are faster.
  * backward, with G = dL/dY given as dY:
  *   dZ = dY (Hadamard) act'(Z),  dX = dZ W^T,  dW = X^T dZ,  dbias = column sums of dZ (before it is rounded),  dR = rho dY
@@ -297,7 +297,7 @@ int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const 
  *   dX = dXout + dN/dX'(dH);  dA, dscale, dw_post, db_post, dU from dX through the block's side; dw_pre, db_pre from dH.
  * Each output may be NULL.  dA has the shape of A (with one gate per row a sum over it).  The vectors' gradients are fp32 sums over all
  * rows in a fixed order.  dX, dU and dA may each be U, A, Xout, dXout or dH (same address, leading dimension and width).
- * Rows of up to 8192 elements are held in registers; longer ones are read several times.
+ * Rows of up to 8192 elements are held in registers; longer ones, up to 2^26 (RANGE), are read several times.
  * ----------------------------------------------------------------------------------------- */
 int gcn_block_norm_forward(int64_t n, int32_t f, int type, int kind, float eps, const void* X, int64_t ldx, const void* U,
                            int64_t ldu, const void* A, int32_t gate_cols, int64_t lda, const float* scale,
@@ -320,8 +320,8 @@ int gcn_block_norm_backward(int64_t n, int32_t f, int type, int kind, const void
  * two entries.  A weight of 0 leaves its part out.  t: n x k (ld ldt) and Z, G of element type `type`.  labels: int32[n] or NULL; a label outside [0, C) is none.  m: the divisor
  * (host value, for instance the number of rows with a list or a label).  loss: fp32, written.  G: n x C or NULL; it may be Z.
  * Logits of -inf are classes that cannot be (q = 0); a row of them alone has no softmax, and gives NaN if it has a list or a label.  Exponentials
- * and row sums are fp32; the loss is added up in fp64 in a fixed order.  1 <= k <= min(C, GCN_DISTILL_MOST).  Rows up to
- * 256 KB are read once.
+ * and row sums are fp32; the loss is added up in fp64 in a fixed order.  1 <= k <= min(C, GCN_DISTILL_MOST); C up to 2^30 (RANGE).
+ * Rows up to 16 KB are read once.
  * ----------------------------------------------------------------------------------------- */
 int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_t ldz, int32_t k, const int32_t* top, int64_t ldtop,
                 const void* t, int64_t ldt, const int32_t* labels, float temperature, float w_teacher, float w_label,

@@ -628,6 +628,7 @@ static int norm_checks(const char* who, int64_t n, int32_t f, int type, int kind
     if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
     if (kind != GCN_NORM_RMS && kind != GCN_NORM_LAYER) return fail(GCN_ERR_BADARG, "%s: unknown norm %d", who, kind);
     if (n <= 0 || f <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (f > (1 << 26)) return fail(GCN_ERR_RANGE, "%s: rows go up to 2^26", who);   // (a launch has 64 threads for a column, and less than 2^32 of them)
     if (A && gate_cols != 1 && gate_cols != f) return fail(GCN_ERR_BADARG, "%s: the gate has 1 or f columns", who);
     if (A && lda < gate_cols) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     return GCN_OK;

@@ -283,6 +283,7 @@ extern "C" int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_
     if (!Z || !top || !t || !loss) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
     if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
     if (n <= 0 || C <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (C > (1 << 30)) return fail(GCN_ERR_RANGE, "%s: there are up to 2^30 classes", who);
     if (k <= 0 || k > C || k > GCN_DISTILL_MOST) return fail(GCN_ERR_BADARG, "%s: a list has 1 to %d entries, and no more than there are classes", who, GCN_DISTILL_MOST);
     if (ldz < C || ldtop < k || ldt < k || (G && ldg < C)) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(GCN_ERR_BADARG, "%s: the temperature must be positive", who);

@@ -4,8 +4,8 @@
 namespace gcn {
 
 // dZ = dY * act'(Z), dR = rho dY, and the column sums of dZ (the bias gradient, of the unrounded products): one pass over the matrices for the elementwise
-// part, bound by memory (8192 x 4096 in fp16 with SiLU: 201 MB in 44 to 49 us).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two such sets on their way, and a share of the rows; the four row sets are
-// added in order.
+// part, bound by memory (8192 x 4096 in fp16 with SiLU: 201 MB in 44 to 49 us).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two such sets on their way,
+// and a share of the rows; the four row sets are added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int64_t rows_per_block, const T* Z, int64_t ldz,
                                                       const T* dY, int64_t lddy, int act, float rho, T* dZ, int64_t lddz, T* dR,
@@ -13,8 +13,8 @@ __global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int6
     constexpr int E = Elem<T>::E, SETS = 4, AHEAD = 2;
     __shared__ float sums[SETS][64][E + 1];
     const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
-    const int64_t c = ((int64_t)blockIdx.y * 64 + lane) * E;
-    const int64_t rb = (int64_t)blockIdx.x * rows_per_block, re = rb + rows_per_block < n ? rb + rows_per_block : n;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E;
+    const int64_t rb = (int64_t)blockIdx.y * rows_per_block, re = rb + rows_per_block < n ? rb + rows_per_block : n;
     const int count = c >= N ? 0 : N - c < E ? (int)(N - c) : E;
     float sum[E] = {};
     auto row = [&](int64_t i, Vec<T> y, Vec<T> z) {
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int6
         for (int e = 0; e < E; ++e) sum[e] += sums[w][lane][e];
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        if (e < count) part[(int64_t)blockIdx.x * N + c + e] = sum[e];
+        if (e < count) part[(int64_t)blockIdx.y * N + c + e] = sum[e];
 }
 
 template <typename T>
@@ -85,7 +85,7 @@ static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const 
     ScratchLease lease;
     void* part = dbias;                                           // the sums of a single share of the rows are the result
     if (dbias && blocks > 1) GCN_TRY(lease.get(&part, (size_t)blocks * N * 4, s));
-    hipLaunchKernelGGL(k_linear_slope<T>, dim3((unsigned)blocks, (unsigned)across), dim3(256), 0, s, n, N, per, (const T*)Z, ldz,
+    hipLaunchKernelGGL(k_linear_slope<T>, dim3((unsigned)across, (unsigned)blocks), dim3(256), 0, s, n, N, per, (const T*)Z, ldz,
                        (const T*)dY, lddy, act, rho, (T*)dZ, lddz, (T*)dR, lddr, (float*)part);
     GCN_LAUNCH_CHECK();
     if (dbias && blocks > 1) return vector_sums_launch((const float*)part, (int)blocks, N, dbias, s);
@@ -96,6 +96,7 @@ static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const 
 
 using namespace gcn;
 
+constexpr int32_t MOST = 1 << 27;                                 // a launch has up to 16 threads for a column, and less than 2^32 of them
 static bool known_act(int act) { return act >= GCN_ACT_NONE && act <= GCN_ACT_SILU; }
 
 extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W,
@@ -106,7 +107,7 @@ extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int ty
     if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
     if (!known_act(act)) return fail(GCN_ERR_BADARG, "%s: unknown activation %d", who, act);
     if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
-    if (f_in > (1 << 30) || f_out > (1 << 30)) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^30", who);
+    if (f_in > MOST || f_out > MOST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
     if (ldx < f_in || ldw < f_out || ldy < f_out || (R && ldr < f_out) || (Z && ldz < f_out))
         return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     const size_t b = elem_bytes(type);
@@ -133,7 +134,7 @@ extern "C" int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int t
     if (curved && (products || dbias || dZ) && !Z) return fail(GCN_ERR_BADARG, "%s: the activation's derivative needs Z", who);
     if (curved && products && !dZ) return fail(GCN_ERR_BADARG, "%s: the products need dZ as workspace", who);
     if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
-    if (f_in > (1 << 30) || f_out > (1 << 30)) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^30", who);
+    if (f_in > MOST || f_out > MOST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
     if (lddy < f_out || (X && ldx < f_in) || (W && ldw < f_out) || (Z && ldz < f_out) || (dZ && lddz < f_out) || (dX && lddx < f_in) ||
         (dW && lddw < f_out) || (dR && lddr < f_out))
         return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);

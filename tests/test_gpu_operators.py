@@ -856,6 +856,33 @@ def test_distill_refusals():
     assert L.gcn_distill(4, 8, 0, p(Z), 8, 0, p(top), 3, p(t), 3, None, 1.0, 1.0, 0.0, 4, 1.0, p(loss), p(G), 8, 0) == -1
 
 
+# ---- sizes ----------------------------------------------------------------------------------------------------------
+def test_widths_beyond_the_range_are_refused():
+    """By every entry point, before anything is launched or read."""
+    L, x = lib().lib(), torch.zeros(64, device="cuda")
+    p = [x[8 * i:].data_ptr() for i in range(8)]
+    far = (1 << 31) - 1
+    assert L.gcn_linear_forward(1, 1, (1 << 27) + 1, 0, p[0], far, p[1], far, None, 0, None, 0, 0.0, None, 0, p[2], far, 0) == -2
+    assert L.gcn_linear_backward(1, 1, (1 << 27) + 1, 0, p[0], far, p[1], far, None, 0, p[2], far, 0, 0.0, None, 0, None, 0, None, 0, p[3], None, 0, 0) == -2
+    for f in ((1 << 26) + 1, far):
+        assert L.gcn_block_norm_forward(1, f, 0, 0, 1e-5, p[0], far, None, 0, None, 0, 0, None, None, None, p[1], None, None, 0, p[2], far, None, 0) == -2
+        assert L.gcn_block_norm_backward(1, f, 0, 0, None, 0, None, 0, 0, None, None, None, p[0], p[1], far, p[2], None, 0, p[3], far, p[4], far,
+                                         None, 0, None, 0, None, None, None, None, None, 0) == -2
+    for C in ((1 << 30) + 1, far):
+        assert L.gcn_distill(1, C, 0, p[0], far, 1, p[1], 1, p[2], 1, None, 1.0, 1.0, 0.0, 1, 1.0, p[3], None, 0, 0) == -2
+
+
+@pytest.mark.parametrize("type_", ["f32", "f16"])
+def test_linear_backward_of_one_very_wide_row(type_):
+    """One row: the bias's gradient is dY act'(Z), and dR is rho dY, both exact for ReLU; more columns than a launch has rows of workgroups."""
+    g = lib()
+    N = (1 << 25) + 3
+    dY, Z = torch.empty(1, N, device="cuda", dtype=TYPES[type_]).normal_(), torch.empty(1, N, device="cuda", dtype=TYPES[type_]).normal_()
+    db, dR, dZ = torch.empty(N, device="cuda"), torch.empty_like(dY), torch.empty_like(dY)
+    g.gcn_linear_backward(None, None, Z, dY, dZ, dbias=db, dR=dR, act=g.ACT_RELU, rho=0.5)
+    assert torch.equal(dZ, dY * (Z > 0)) and torch.equal(db, dZ[0].float()) and torch.equal(dR, (0.5 * dY.float()).to(dY.dtype))
+
+
 # ---- streams and graphs ---------------------------------------------------------------------------------------------
 def test_operators_on_a_stream_of_the_callers_and_in_a_graph():
     """A training step of a block on a side stream, and the same one captured and replayed with new inputs: the eager results bit by bit."""
