@@ -108,7 +108,7 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
             if (j < a.k) {
                 at = a.top[i * a.ldtop + j];
                 t = (float)((const T*)a.t)[i * a.ldt + j];
-                if (at >= a.C || t == -INFINITY || a.wt == 0.f) at = -1;       // (a part of weight 0 is none, whatever it is)
+                if (at >= a.C || t == -INFINITY) at = -1;
                 if (at >= 0) {
                     high[1] = fmaxf(high[1], t);
                     high[2] = 1.f;
@@ -293,8 +293,8 @@ extern "C" int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_
     if ((g.meets(z) && (G != Z || ldg != ldz)) || g.meets(at) || g.meets(tt) || g.meets(y) || l.meets(z) || l.meets(g) || l.meets(at) || l.meets(tt) || l.meets(y))
         return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
     DistillArgs a;
-    a.n = n; a.C = C; a.k = k; a.Z = Z; a.ldz = ldz; a.G = G; a.ldg = ldg; a.top = top; a.ldtop = ldtop; a.t = t; a.ldt = ldt;
-    a.labels = w_label != 0.f ? labels : nullptr;
+    a.n = n; a.C = C; a.k = w_teacher != 0.f ? k : 0; a.Z = Z; a.ldz = ldz; a.G = G; a.ldg = ldg; a.top = top; a.ldtop = ldtop; a.t = t; a.ldt = ldt;
+    a.labels = w_label != 0.f ? labels : nullptr;                 // (a part of weight 0 is none, whatever it is: not multiplied away)
     a.inv_T = 1.f / temperature;
     a.wt = w_teacher * temperature * temperature;
     a.wl = w_label;
