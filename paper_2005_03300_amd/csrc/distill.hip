@@ -3,7 +3,7 @@
 //   loss = 1/m sum over rows [ wt T^2 sum over S of p (log p - log q) - wl log softmax(z)_y ]
 //   G    = 1/m [ wt T (q - p) where S is not empty, + wl (softmax(z) - onehot(y)) where y >= 0 ]
 // A row of up to 16 KB is read once, held in registers in its own type, and its gradient written once: bound by memory and, where rows are short, by the chain of a row
-// (its list, two joins, the list again): 232965 x 41 in fp32 35 us, x 128 55 us (4.3 TB/s).  Longer rows: 4096 x 100,000 in bf16 406 us, 3 x 819 MB from and to
+// (its list, two joins, the list again): 232965 x 41 in fp32 35 us, x 128 55 us (4.3 TB/s).  Longer rows: 4096 x 100,000 in bf16 403 us, 3 x 819 MB from and to
 // memory and caches.
 #include <type_traits>
 

@@ -4,7 +4,7 @@
 namespace gcn {
 
 // dZ = dY * act'(Z), dR = rho dY, and the column sums of dZ (the bias gradient, of the unrounded products): one pass over the matrices for the elementwise
-// part, bound by memory (8192 x 4096 in fp16 with SiLU: 201 MB in 44 to 49 us).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two such sets on their way,
+// part, bound by memory (8192 x 4096 in fp16 with SiLU: 201 MB in 45 us, 4.5 TB/s).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two such sets on their way,
 // and a share of the rows; the four row sets are added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int64_t rows_per_block, const T* Z, int64_t ldz,

@@ -9,7 +9,7 @@ constexpr int FEW_STRIPS = 48;
 template <typename T, int C, int RT>
 constexpr size_t few_lds() { return (size_t)FEW_WAVES * RT * 16 * (16 * C + 4) * 4; }
 
-// Y's rows are few, so the product is bound by reading W (and by about 4 us of start and end): 4096 x 4096 in bf16 for 16 rows 13.8 us, in fp32 for one row 14.5 us (4.6
+// Y's rows are few, so the product is bound by reading W (and by about 4 us of start and end): 4096 x 4096 in bf16 for 16 rows 13.5 us, in fp32 for one row 14.5 us (4.6
 // TB/s), 4096 x 16384 in bf16 26 us (5 TB/s).
 // A workgroup has a strip of 16 C columns; its wavefronts take the 4 E values of k of a step in turn, straight from memory into the operands of the matrix unit: a
 // lane loads C neighbouring columns of E rows of W and has with them C fragments of E values of k.  Up to 16 RT rows of X, whose fragments are 16
