@@ -2,9 +2,9 @@
 // what is left, 8 + 8 + 8 bits), and the product of two such sums has nine products of bf16 numbers, which the matrix unit multiplies exactly and adds in fp32.  Three of the
 // nine, m l', l m' and l l', are at most 2^-26 of x x' each and left out, below the rounding of an fp32 product; the other six take 96 cycles for what the fp32 units
 // take 256 for.  8192 x 8192 x 8192 takes 5.2 ms (210 TFLOP/s; on the fp32 units at most 157, the library's product 151), 232965 x 602 x 128 260 us.
-// Infinities and NaN have no such sum, nor have numbers that round to infinity as bf16: with them m, and with it the result, is NaN.  A workgroup that has such
-// results computes its tile again on the fp32 units, and takes these results from there (and no other, so that none depends on another row's numbers).  Numbers below
-// 2^-100 lose bits of m and l below the smallest bf16 number, 2^-133.
+// Infinities and NaN have no such sum, nor have numbers that round to infinity as bf16: with them m, and with it the result, is NaN; and a finite product of
+// numbers whose h are rounded up can become infinite.  A workgroup that has results that are not finite computes its tile again on the fp32 units, and takes these
+// results from there (and no other, so that none depends on another row's numbers).  Numbers below 2^-100 lose bits of m and l below the smallest bf16 number, 2^-133.
 #pragma once
 #include "linear_tile.h"
 
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) lost |= acc[i][j][e] != acc[i][j][e];
+            for (int e = 0; e < 4; ++e) lost |= !(fabsf(acc[i][j][e]) < INFINITY);
     if (__syncthreads_or(lost)) {
         v4f plain[FM][FN] = {};
         run([&](const Vec<float>(&va)[OpA::PER], const Vec<float>(&vb)[OpB::PER]) {
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
             for (int j = 0; j < FN; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (acc[i][j][e] != acc[i][j][e]) acc[i][j][e] = plain[i][j][e];
+                    if (!(fabsf(acc[i][j][e]) < INFINITY)) acc[i][j][e] = plain[i][j][e];
     }
     constexpr int PHASES = (BM * BN * 4 + STAGE - 1) / STAGE, PART = BM / WM / PHASES * (BN / WN) * 4;
     static_assert(WM * WN * PART <= STAGE && (BM + BN) * 128 <= STAGE, "results and plain stages have room");

@@ -1,0 +1,48 @@
+"""The operators of residual networks at the ends of what they take: magnitudes, widths, places of operands, tiles.
+
+Tolerances are derived as in test_gpu_operators.py."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from test_gpu_operators import ALL, EPS, TINY, TYPES, UNIT, check, code, gen_of, lib, normal
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- fp32 products --------------------------------------------------------------------------------------------------
+def outer_products(g, x, w):
+    """x w^T of two vectors by each of a layer's three products, none of them with a sum: the forward pass, dX and dW."""
+    X, W = x.reshape(-1, 1).contiguous().cuda(), w.reshape(1, -1).contiguous().cuda()
+    n, N = X.shape[0], W.shape[1]
+    Y, dX, dW = (torch.empty(n, N, device="cuda") for _ in range(3))
+    g.gcn_linear_forward(X, W, Y)
+    g.gcn_linear_backward(None, W.t().contiguous(), None, X, dX=dX)
+    g.gcn_linear_backward(X.t().contiguous(), None, None, W, dW=dW)
+    return dict(forward=Y, dX=dX, dW=dW)
+
+
+def test_linear_fp32_products_next_to_the_largest_number():
+    """Finite where the product is, though both factors are rounded up on their way, and infinite of the right sign where it is not."""
+    g = lib()
+    x = torch.full((70,), 1.9999 * 2.0 ** 63)
+    x[1::2] *= -1
+    x[3], x[4] = 1.0, 2.0 ** 65
+    w = torch.full((45,), 1.9999 * 2.0 ** 63)
+    w[2::5] *= -1
+    ref = x.double()[:, None] * w.double()[None]
+    most = torch.finfo(torch.float32).max
+    ref = torch.where(ref.abs() > most, ref.sign() * math.inf, ref)
+    assert bool(torch.isfinite(ref[0]).all()) and bool(torch.isinf(ref[4]).all())
+    for name, got in outer_products(g, x, w).items():
+        check(got, ref, 3 * EPS * ref.abs(), name)
+        assert torch.equal(got.cpu().sign().double(), ref.sign()), name
+    # the same product in a sum of two
+    X, W = torch.stack([x, torch.full_like(x, -1.0)], 1), torch.stack([w, torch.full_like(w, 2.0 ** 100)], 0)
+    Y = torch.empty(70, 45, device="cuda")
+    g.gcn_linear_forward(X.cuda(), W.cuda(), Y)
+    fine = torch.isfinite(ref)
+    want = torch.where(fine, ref - 2.0 ** 100, ref)
+    check(Y, want, 4 * EPS * (ref.abs() + 2.0 ** 100), "sum of two")
