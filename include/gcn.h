@@ -263,9 +263,9 @@ int gcn_softmax_nll_masked(int64_t n, int32_t C, const float* Z, int64_t ldz, co
  *   Z = X W + 1 bias^T,   Y = rho R + act(Z)
  * X: n x f_in, W: f_in x f_out, R, Z, Y: n x f_out, all of element type `type` (GCN_F32, GCN_BF16, GCN_F16); bias: fp32[f_out].  bias and R
  * may be NULL; Z (the argument of act, which backward needs unless act is GCN_ACT_NONE) may be NULL.  Products are summed in
- * fp32, and bias, activation and residual applied to the fp32 sum; Z and Y are rounded once.  Products of fp32 elements are exact to 2^-26
- * of themselves (each number enters the matrix units as the sum of three bf16 numbers), with the infinities and NaN of fp32 products; numbers
- * below 2^-100 lose bits below 2^-133.  GELU of 16-bit elements is off by 2e-7 |Z| at most before it is rounded.  Y may be R (same address and leading dimension); no other output may overlap an input or another output.
+ * fp32, and bias, activation and residual applied to the fp32 sum; Z and Y are rounded once.  Products of fp32 elements are exact to 2^-24
+ * of themselves, as rounded ones are (each number enters the matrix units as the sum of three bf16 numbers), with the infinities and NaN of fp32 products;
+ * numbers below 2^-100 lose bits below 2^-133.  GELU of 16-bit elements is off by 2e-7 |Z| at most before it is rounded.  Y may be R (same address and leading dimension); no other output may overlap an input or another output.
  * Sums have a fixed order: repeated calls give the same bits.  Widths go up to 2^27 (RANGE).  Rows and leading dimensions of any alignment are taken; rows at
  * 16-byte addresses (and widths of whole 16 bytes) are faster.
  * backward, with G = dL/dY given as dY:

@@ -1,6 +1,7 @@
 // Products of fp32 matrices on the bf16 matrix units.  An fp32 number is the sum of three bf16 numbers exactly (x = h + m + l: each the nearest bf16 number to
 // what is left, 8 + 8 + 8 bits), and the product of two such sums has nine products of bf16 numbers, which the matrix unit multiplies exactly and adds in fp32.  Three of the
-// nine, m l', l m' and l l', are at most 2^-26 of x x' each and left out, below the rounding of an fp32 product; the other six take 96 cycles for what the fp32 units
+// nine are left out: m l' and l m', at most 2^-25 of x x' each, and l l', at most 2^-34; together they are up to 2^-24 of it, as the rounding of an fp32 product is, and
+// 2^-27.5 in the root mean square over random mantissas.  The other six take 96 cycles for what the fp32 units
 // take 256 for.  8192 x 8192 x 8192 takes 5.2 ms (210 TFLOP/s; on the fp32 units at most 157, the library's product 151), 232965 x 602 x 128 260 us.
 // Infinities and NaN have no such sum, nor have numbers that round to infinity as bf16: with them m, and with it the result, is NaN; and a finite product of
 // numbers whose h are rounded up can become infinite.  A workgroup that has results that are not finite computes its tile again on the fp32 units, and takes these

@@ -46,3 +46,17 @@ def test_linear_fp32_products_next_to_the_largest_number():
     fine = torch.isfinite(ref)
     want = torch.where(fine, ref - 2.0 ** 100, ref)
     check(Y, want, 4 * EPS * (ref.abs() + 2.0 ** 100), "sum of two")
+
+
+def test_linear_fp32_products_whose_parts_are_largest():
+    """Mantissas whose second and third parts are as large as they can be: what is left out of their product is 2^-24 of it, and the sum of what is kept is
+    rounded as an fp32 product is."""
+    g = lib()
+    x = 1 + 2.0 ** -8 - 2.0 ** -17 - 2.0 ** -23
+    x = torch.full((70,), x) * torch.exp2(torch.arange(70).float() - 35)
+    w = torch.full((45,), float(x[35]))
+    w[1::2] = -w[1::2]
+    assert float(x[35]) == 1 + 2.0 ** -8 - 2.0 ** -17 - 2.0 ** -23
+    ref = x.double()[:, None] * w.double()[None]
+    for name, got in outer_products(g, x, w).items():
+        check(got, ref, 3 * EPS * ref.abs(), name)
