@@ -4,6 +4,7 @@
 #include <initializer_list>
 #include <type_traits>
 
+#include "launch_rules.h"
 #include "rows.h"
 #include "sum_parts.h"
 
@@ -474,31 +475,34 @@ struct NormVectors {
     const float *scale, *w_post, *b_post;
     float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
 };
-// Sixteen columns by 64 shares of the workgroups, the shares in order.
+// Sixteen columns at a time by 64 shares of the workgroups, the shares in order.
 __global__ __launch_bounds__(1024) void k_block_norm_vectors(NormArgs g, int blocks, NormVectors v) {
     __shared__ float shares[4][64][17];
-    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
-    const int64_t c = (int64_t)blockIdx.x * 16 + col;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (g.at[k] >= 0) shares[k][share][col] = c < g.f ? strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, share, 64, blocks) : 0.f;
-    __syncthreads();
-    // (sum, column) of a thread; the others are done
     __shared__ float total[4][16];
-    if (threadIdx.x < 64) {
-        float s = 0.f;
-        if (g.at[share] >= 0)
-            for (int w = 0; w < 64; ++w) s += shares[share][w][col];
-        total[share][col] = s;
+    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
+    for (int64_t c0 = (int64_t)blockIdx.x * 16; c0 < g.f; c0 += (int64_t)gridDim.x * 16) {
+        const int64_t c = c0 + col;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (g.at[k] >= 0) shares[k][share][col] = c < g.f ? strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, share, 64, blocks) : 0.f;
+        __syncthreads();
+        // (sum, column) of a thread
+        if (threadIdx.x < 64) {
+            float s = 0.f;
+            if (g.at[share] >= 0)
+                for (int w = 0; w < 64; ++w) s += shares[share][w][col];
+            total[share][col] = s;
+        }
+        __syncthreads();
+        if (threadIdx.x < 16 && c < g.f) {                        // (the next columns' totals are written behind another barrier)
+            const float s0 = total[0][col], s1 = total[1][col], sc = v.scale ? v.scale[c] : 1.f;
+            if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], s0, v.b_post ? v.b_post[c] * s1 : 0.f) : s0;
+            if (v.dw_post) v.dw_post[c] = sc * s0;
+            if (v.db_post) v.db_post[c] = sc * s1;
+            if (v.dw_pre) v.dw_pre[c] = total[2][col];
+            if (v.db_pre) v.db_pre[c] = total[3][col];
+        }
     }
-    __syncthreads();
-    if (threadIdx.x >= 16 || c >= g.f) return;
-    const float s0 = total[0][col], s1 = total[1][col], sc = v.scale ? v.scale[c] : 1.f;
-    if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], s0, v.b_post ? v.b_post[c] * s1 : 0.f) : s0;
-    if (v.dw_post) v.dw_post[c] = sc * s0;
-    if (v.db_post) v.db_post[c] = sc * s1;
-    if (v.dw_pre) v.dw_pre[c] = total[2][col];
-    if (v.db_pre) v.db_pre[c] = total[3][col];
 }
 
 __global__ __launch_bounds__(1024) void k_vector_sums(const float* __restrict__ part, int parts, int64_t count, float* __restrict__ out) {
@@ -507,7 +511,7 @@ __global__ __launch_bounds__(1024) void k_vector_sums(const float* __restrict__ 
 }
 
 int vector_sums_launch(const float* part, int parts, int64_t count, float* out, hipStream_t s) {
-    hipLaunchKernelGGL(k_vector_sums, dim3((unsigned)((count + 63) / 64)), dim3(1024), 0, s, part, parts, count, out);
+    hipLaunchKernelGGL(k_vector_sums, dim3((unsigned)column_sum_groups(count)), dim3(1024), 0, s, part, parts, count, out);
     GCN_LAUNCH_CHECK();
     return GCN_OK;
 }
@@ -573,7 +577,7 @@ static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
         }
         GCN_LAUNCH_CHECK();
         if (g.sums) {
-            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)((g.f + 15) / 16)), dim3(1024), 0, s, g, blocks, v);
+            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)norm_vector_groups(g.f)), dim3(1024), 0, s, g, blocks, v);
             GCN_LAUNCH_CHECK();
         }
         return GCN_OK;
@@ -628,7 +632,7 @@ static int norm_checks(const char* who, int64_t n, int32_t f, int type, int kind
     if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
     if (kind != GCN_NORM_RMS && kind != GCN_NORM_LAYER) return fail(GCN_ERR_BADARG, "%s: unknown norm %d", who, kind);
     if (n <= 0 || f <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
-    if (f > (1 << 26)) return fail(GCN_ERR_RANGE, "%s: rows go up to 2^26", who);   // (a launch has 64 threads for a column, and less than 2^32 of them)
+    if (f > NORM_WIDEST) return fail(GCN_ERR_RANGE, "%s: rows go up to 2^26", who);
     if (A && gate_cols != 1 && gate_cols != f) return fail(GCN_ERR_BADARG, "%s: the gate has 1 or f columns", who);
     if (A && lda < gate_cols) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     return GCN_OK;

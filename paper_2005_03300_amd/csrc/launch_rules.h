@@ -88,4 +88,11 @@ inline bool short_copy_pays(int64_t rows, int64_t pitch, int64_t nnz, int64_t ro
     return rows * pitch <= (3 << 20) || 2 * rows * pitch <= 5 * nnz || rows_of_16 * 32 < rows;
 }
 
+// The widest rows that gcn_linear_* and gcn_block_norm_* take.  A launch has fewer than 2^32 threads along a dimension: that is what bounds the first, whose
+// columns have up to 16 threads each; an index of 32 bits for a column and the elements of a step behind it bounds both.
+constexpr int32_t LINEAR_WIDEST = 1 << 27, NORM_WIDEST = 1 << 26;
+// Workgroups of 1024 threads: for 64 of `count` column sums each; for 16 columns at a time of a norm's vectors, any number of times.
+constexpr int64_t column_sum_groups(int64_t count) { return (count + 63) / 64; }
+constexpr int64_t norm_vector_groups(int64_t f) { return f < (1 << 20) ? (f + 15) / 16 : (1 << 16); }
+
 }  // namespace gcn

@@ -1,4 +1,5 @@
 // A linear layer with what follows it: Y = rho R + act(X W + 1 bias^T), and its gradients, on 32- and 16-bit elements.
+#include "launch_rules.h"
 #include "linear_tile.h"
 
 namespace gcn {
@@ -96,7 +97,6 @@ static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const 
 
 using namespace gcn;
 
-constexpr int32_t MOST = 1 << 27;                                 // a launch has up to 16 threads for a column, and less than 2^32 of them
 static bool known_act(int act) { return act >= GCN_ACT_NONE && act <= GCN_ACT_SILU; }
 
 extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W,
@@ -107,7 +107,7 @@ extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int ty
     if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
     if (!known_act(act)) return fail(GCN_ERR_BADARG, "%s: unknown activation %d", who, act);
     if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
-    if (f_in > MOST || f_out > MOST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
+    if (f_in > LINEAR_WIDEST || f_out > LINEAR_WIDEST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
     if (ldx < f_in || ldw < f_out || ldy < f_out || (R && ldr < f_out) || (Z && ldz < f_out))
         return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     const size_t b = elem_bytes(type);
@@ -134,7 +134,7 @@ extern "C" int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int t
     if (curved && (products || dbias || dZ) && !Z) return fail(GCN_ERR_BADARG, "%s: the activation's derivative needs Z", who);
     if (curved && products && !dZ) return fail(GCN_ERR_BADARG, "%s: the products need dZ as workspace", who);
     if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
-    if (f_in > MOST || f_out > MOST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
+    if (f_in > LINEAR_WIDEST || f_out > LINEAR_WIDEST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
     if (lddy < f_out || (X && ldx < f_in) || (W && ldw < f_out) || (Z && ldz < f_out) || (dZ && lddz < f_out) || (dX && lddx < f_in) ||
         (dW && lddw < f_out) || (dR && lddr < f_out))
         return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);

@@ -60,3 +60,23 @@ def test_linear_fp32_products_whose_parts_are_largest():
     ref = x.double()[:, None] * w.double()[None]
     for name, got in outer_products(g, x, w).items():
         check(got, ref, 3 * EPS * ref.abs(), name)
+
+
+# ---- the widest rows ------------------------------------------------------------------------------------------------
+def test_block_norm_of_the_widest_row():
+    """One row of 2^26 elements through the norms and back.  The root mean square of ones and minus ones is 1 (eps 0) and the gradients are exact."""
+    g = lib()
+    f = 1 << 26
+    X = torch.ones(1, f, dtype=torch.bfloat16, device="cuda")
+    X[0, ::3] = -1
+    w = torch.full((f,), 2.0, device="cuda")
+    H, stats = torch.empty_like(X), torch.empty(1, 4, device="cuda")
+    g.gcn_block_norm_forward(X, H=H, w_pre=w, stats=stats, eps=0.0)
+    assert torch.equal(H, 2 * X) and stats[0].tolist() == [0, 0, 0, 1]
+    # a gradient at right angles to the row: dX = dH w, and the weights' gradient is dH x^
+    dH = torch.zeros_like(X)
+    dH[0, 0], dH[0, 1], dH[0, f - 2], dH[0, f - 1] = 1.0, 1.0, 3.0, 3.0
+    assert float((dH.float() * X.float()).sum()) == 0
+    dX, dw, db = torch.empty_like(X), torch.full((f,), 9.0, device="cuda"), torch.full((f,), 9.0, device="cuda")
+    g.gcn_block_norm_backward(None, X, stats, None, dH, dX, w_pre=w, dw_pre=dw, db_pre=db)
+    assert torch.equal(dX, 2 * dH) and torch.equal(dw, (dH * X)[0].float()) and torch.equal(db, dH[0].float())

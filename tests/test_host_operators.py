@@ -30,3 +30,27 @@ def test_what_fp32_products_leave_out():
     said = re.search(r"Products of fp32 elements are exact to 2\^-(\d+)", open(os.path.join(ROOT, "include", "gcn.h")).read())
     bound = 2.0 ** -int(said.group(1))
     assert left.max() <= bound and left[0] > bound / 2
+
+
+def test_launches_for_the_widest_rows_are_launchable(tmp_path):
+    """Fewer than 2^32 threads along a dimension, and all columns in some workgroup, at the widths where these counts change and at the widest."""
+    r = run_cpp(tmp_path, """
+        #include <cstdio>
+        #include <initializer_list>
+        #include "launch_rules.h"
+        using namespace gcn;
+        int main() {
+            const int64_t most = (int64_t)1 << 32;
+            for (int64_t f : {int64_t(1), int64_t(16), int64_t(17), int64_t(1 << 20) - 1, int64_t(1 << 20), int64_t(1 << 20) + 1, int64_t(NORM_WIDEST) - 16,
+                              int64_t(NORM_WIDEST) - 15, int64_t(NORM_WIDEST)}) {
+                const int64_t groups = norm_vector_groups(f);
+                // below the bound every column has a workgroup of its own; from it on a workgroup goes on behind the last one
+                if (groups * 1024 >= most || groups < 1 || (f < (1 << 20) && groups * 16 < f)) return printf("norm vectors of %lld: %lld\\n", (long long)f, (long long)groups), 1;
+            }
+            for (int64_t N : {int64_t(1), int64_t(64), int64_t(65), int64_t(LINEAR_WIDEST)}) {
+                const int64_t groups = column_sum_groups(N);
+                if (groups * 1024 >= most || groups * 64 < N) return printf("column sums of %lld\\n", (long long)N), 1;
+            }
+        }
+    """)
+    assert r.returncode == 0, r.stdout
