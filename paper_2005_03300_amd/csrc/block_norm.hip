@@ -443,10 +443,6 @@ __global__ __launch_bounds__(1024) void k_block_norm_back_long(NormArgs g) {
             join_lanes<1024>(s, meet, turn);
         }
         const float ualong = s[0] * inv_f, umean = g.layer ? s[1] * inv_f : 0.f;
-        if (g.dA && g.gate == 1) {
-            __syncthreads();                                     // dA may take the place of A: all lanes have read the row's gate
-            if (threadIdx.x == 0) ((T*)g.dA)[i * g.ldda] = (T)s[2];
-        }
         each([&](float(&dx)[E], float(&xh)[E], float(&gh)[E], float(&)[E], int64_t c, int count) {
             float uh[E], d[E], da[E], gv[E];
             if (g.U) block(dx, c, count, uh, d, da, gv);
@@ -466,6 +462,8 @@ __global__ __launch_bounds__(1024) void k_block_norm_back_long(NormArgs g) {
                 for (int e = 0; e < E; ++e) gv[e] = st.y * (gv[e] - fmaf(uh[e], ualong, umean));
             store_vec_part((T*)g.dU + i * g.lddu + c, from_floats<T>(gv), count);
         });
+        // dA may take the place of A, which all lanes have read before the join, and of a row of one element, which is this thread's
+        if (g.dA && g.gate == 1 && threadIdx.x == 0) ((T*)g.dA)[i * g.ldda] = (T)s[2];
     }
 }
 

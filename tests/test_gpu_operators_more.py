@@ -80,3 +80,21 @@ def test_block_norm_of_the_widest_row():
     dX, dw, db = torch.empty_like(X), torch.full((f,), 9.0, device="cuda"), torch.full((f,), 9.0, device="cuda")
     g.gcn_block_norm_backward(None, X, stats, None, dH, dX, w_pre=w, dw_pre=dw, db_pre=db)
     assert torch.equal(dX, 2 * dH) and torch.equal(dw, (dH * X)[0].float()) and torch.equal(db, dH[0].float())
+
+
+def test_gradient_of_a_gate_in_place_of_a_row_of_one_element():
+    """Rows of one element: the gate is as wide as they are, so its gradient may take the place of any of the row's operands."""
+    g = lib()
+    n = 5
+    gen = gen_of("one")
+    u, a, xo, c, d = (normal(gen, (n, 1), "f32").cuda() for _ in range(5))
+    w = torch.tensor([1.5], device="cuda")
+    stats = torch.rand(n, 4, generator=gen).cuda() + 0.5
+    e = lambda: torch.empty(n, 1, device="cuda")
+    want = [e(), e(), e()]
+    g.gcn_block_norm_backward(u, xo, stats, c, d, *want[:2], w_pre=w, w_post=w, A=a, dA=want[2], kind=g.NORM_LAYER)
+    for name in ("U", "A", "Xout", "dXout", "dH"):
+        o = dict(U=u.clone(), A=a.clone(), Xout=xo.clone(), dXout=c.clone(), dH=d.clone())
+        dX, dU = e(), e()
+        g.gcn_block_norm_backward(o["U"], o["Xout"], stats, o["dXout"], o["dH"], dX, dU, w_pre=w, w_post=w, A=o["A"], dA=o[name], kind=g.NORM_LAYER)
+        assert torch.equal(dX, want[0]) and torch.equal(dU, want[1]) and torch.equal(o[name], want[2]), name
