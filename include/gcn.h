@@ -298,6 +298,7 @@ int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const 
  * Each output may be NULL.  dA has the shape of A (with one gate per row a sum over it).  The vectors' gradients are fp32 sums over all
  * rows in a fixed order.  dX, dU and dA may each be U, A, Xout, dXout or dH (same address, leading dimension and width).
  * Rows of up to 8192 elements are held in registers; longer ones, up to 2^26 (RANGE), are read several times.
+ * Scratch of backward: the partial sums of the vectors' gradients, up to 34 MB and 16 f bytes, with rows of over 8192 or under 4 elements also 24 n bytes.
  * ----------------------------------------------------------------------------------------- */
 int gcn_block_norm_forward(int64_t n, int32_t f, int type, int kind, float eps, const void* X, int64_t ldx, const void* U,
                            int64_t ldu, const void* A, int32_t gate_cols, int64_t lda, const float* scale,

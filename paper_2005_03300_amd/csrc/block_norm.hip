@@ -25,7 +25,8 @@ struct NormArgs {
     int64_t lddxo = 0, lddh = 0, lddx = 0, lddu = 0, ldda = 0;
     const void *dXout = nullptr, *dH = nullptr;
     void *dX = nullptr, *dU = nullptr, *dA = nullptr;
-    float* part = nullptr;         // partial sums: of each workgroup `sums` vectors of f
+    struct RowSums* rows = nullptr;    // rows longer than the registers hold, or shorter than a lane's elements
+    float* part = nullptr;         // partial sums: of each workgroup (or share of the rows) `sums` vectors of f
     int sums = 0;
     int at[4] = {-1, -1, -1, -1};  // which of them are sum dX' a u^, sum dX' a, sum dH x^, sum dH
 };
@@ -362,108 +363,183 @@ __global__ __launch_bounds__(1024) void k_block_norm_long(NormArgs g) {
     }
 }
 
-// Likewise; a workgroup's sums over its rows grow in its partial results, where each thread has its own columns.
+// Their gradients: what a row's elements have to know of the whole row is found by a workgroup, which then has the rest of the row too where no vector's gradient is
+// wanted.  With these the rest is a launch of its own, in strips of columns, where a thread keeps its columns' sums over the rows in registers: a workgroup's sums over
+// whole rows would be as long as the rows (four of 2^24 columns from 256 workgroups 64 GB), and in memory.  Three readings of the operands either way,
+// the last one from the caches only in the one launch: 4096 x 16384 in bf16 382 us without the vectors (564 in two launches), 617 with them (a copy of as
+// many bytes takes 224).
+struct RowSums {
+    float along, mean;             // of g x^ and g over the row: mean(g x^), and mean(g) for the layer norm
+    float along_u, mean_u;         // likewise of e u^ and e
+    float gate, dgate;             // with one gate per row: sigmoid(A), and dA
+};
+// dX of E elements from column c of row i on, with x^ and dH, zeros behind the row's end
+template <typename T, int E>
+__device__ __forceinline__ void long_stream_side(const NormArgs& g, int64_t i, int64_t c, int count, const f4u& st, const float (&w_pre)[E], float along, float mean,
+                                                 float (&dx)[E], float (&xh)[E], float (&dh)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) dx[e] = xh[e] = dh[e] = 0.f;
+    if (g.dXout) to_floats<T>(load_vec_part((const T*)g.dXout + i * g.lddxo + c, count), dx);
+    if (!g.dH) return;
+    to_floats<T>(load_vec_part((const T*)g.Xout + i * g.ldxo + c, count), xh);
+    to_floats<T>(load_vec_part((const T*)g.dH + i * g.lddh + c, count), dh);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        xh[e] = e < count ? (xh[e] - st.z) * st.w : 0.f;
+        dx[e] = fmaf(st.w, dh[e] * w_pre[e] - fmaf(xh[e], along, mean), dx[e]);
+    }
+}
+// The block's side from it: u^, d = dX sigmoid(A), dA, and e = d scale w_post
+template <typename T, int E>
+__device__ __forceinline__ void long_block_side(const NormArgs& g, int64_t i, int64_t c, int count, const f4u& st, float row_gate, const float (&scale)[E],
+                                                const float (&w_post)[E], const float (&b_post)[E], const float (&dx)[E], float (&uh)[E], float (&d)[E],
+                                                float (&da)[E], float (&de)[E]) {
+    float a[E];
+    to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count), uh);
+    if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count), a);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if (g.w_post) uh[e] = e < count ? (uh[e] - st.x) * st.y : 0.f;
+        const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+        d[e] = e < count ? dx[e] * gate : 0.f;
+        da[e] = d[e] * scale[e] * fmaf(uh[e], w_post[e], b_post[e]) * (1.f - gate);
+        de[e] = d[e] * scale[e] * w_post[e];
+    }
+}
+// The gradients of E elements of the matrices.  What is written may take the place of what has been read; dA of one gate per row, of a row of one element, too.
+template <typename T, int E>
+__device__ __forceinline__ void long_matrices(const NormArgs& g, int64_t i, int64_t c, int count, const f4u& st, const RowSums& r, const float (&dx)[E],
+                                              const float (&uh)[E], const float (&da)[E], float (&de)[E]) {
+    if (g.dX) store_vec_part((T*)g.dX + i * g.lddx + c, from_floats<T>(dx), count);
+    if (!g.U) return;
+    if (g.dA && g.gate > 1) store_vec_part((T*)g.dA + i * g.ldda + c, from_floats<T>(da), count);
+    if (g.dA && g.gate == 1 && c == 0) ((T*)g.dA)[i * g.ldda] = (T)r.dgate;
+    if (!g.dU) return;
+    if (g.w_post)
+#pragma unroll
+        for (int e = 0; e < E; ++e) de[e] = st.y * (de[e] - fmaf(uh[e], r.along_u, r.mean_u));
+    store_vec_part((T*)g.dU + i * g.lddu + c, from_floats<T>(de), count);
+}
+template <int E>
+__device__ __forceinline__ void long_vectors(const NormArgs& g, int64_t c, int count, float (&scale)[E], float (&w_post)[E], float (&b_post)[E]) {
+    load_floats<E>(g.scale, c, count, 1.f, scale);
+    load_floats<E>(g.w_post, c, count, 1.f, w_post);
+    load_floats<E>(g.b_post, c, count, 0.f, b_post);
+}
+
 template <typename T>
-__global__ __launch_bounds__(1024) void k_block_norm_back_long(NormArgs g) {
+__global__ __launch_bounds__(1024) void k_block_norm_back_rows(NormArgs g) {
     constexpr int E = Elem<T>::E, STEP = 1024 * E;
     __shared__ float meet[2][16][4];
     int turn = 0;
     const float inv_f = 1.f / (float)g.f;
     for (int64_t i = blockIdx.x; i < g.n; i += gridDim.x) {
-        const bool first = i == (int64_t)blockIdx.x;
         const f4u st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
-        const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
-        float along = 0.f, mean = 0.f;
-        auto grow = [&](int k, int64_t c, float v) {
-            if (g.at[k] < 0) return;
-            float* const p = g.part + ((int64_t)blockIdx.x * g.sums + g.at[k]) * g.f + c;
-            *p = first ? v : *p + v;
-        };
-        // dX of the thread's columns, and what goes into the sums over the row on the way
-        auto each = [&](auto f) {
-            for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
-                const int count = g.f - c < E ? (int)(g.f - c) : E;
-                float dx[E] = {}, xh[E] = {}, gh[E] = {}, w[E] = {};
-                if (g.dXout) to_floats<T>(load_vec_part((const T*)g.dXout + i * g.lddxo + c, count), dx);
-                if (g.dH) {
-                    to_floats<T>(load_vec_part((const T*)g.Xout + i * g.ldxo + c, count), xh);
-                    to_floats<T>(load_vec_part((const T*)g.dH + i * g.lddh + c, count), gh);
-                    load_floats<E>(g.w_pre, c, count, 1.f, w);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        xh[e] = e < count ? (xh[e] - st.z) * st.w : 0.f;
-                        dx[e] = fmaf(st.w, gh[e] * w[e] - fmaf(xh[e], along, mean), dx[e]);
-                    }
-                }
-                f(dx, xh, gh, w, c, count);
-            }
-        };
+        RowSums r = {0.f, 0.f, 0.f, 0.f, 1.f, 0.f};
+        if (g.gate == 1) r.gate = gate_of((float)((const T*)g.A)[i * g.lda]);
         if (g.dH) {
             float s[2] = {0.f, 0.f};
-            each([&](float(&)[E], float(&xh)[E], float(&gh)[E], float(&w)[E], int64_t, int count) {
+            for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
+                const int count = g.f - c < E ? (int)(g.f - c) : E;
+                float dx[E], xh[E], dh[E], w_pre[E];
+                load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
+                long_stream_side<T, E>(g, i, c, count, st, w_pre, 0.f, 0.f, dx, xh, dh);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    s[0] = fmaf(gh[e] * w[e], xh[e], s[0]);
-                    s[1] += gh[e] * w[e];
+                    s[0] = fmaf(dh[e] * w_pre[e], xh[e], s[0]);
+                    s[1] += dh[e] * w_pre[e];
                 }
-            });
-            join_lanes<1024>(s, meet, turn);
-            along = s[0] * inv_f;
-            mean = g.layer ? s[1] * inv_f : 0.f;
-        }
-        // the block's side, from dX of the same columns
-        auto block = [&](const float(&dx)[E], int64_t c, int count, float(&uh)[E], float(&d)[E], float(&da)[E], float(&gv)[E]) {
-            float w[E], b[E], sc[E], a[E];
-            load_floats<E>(g.scale, c, count, 1.f, sc);
-            load_floats<E>(g.w_post, c, count, 1.f, w);
-            load_floats<E>(g.b_post, c, count, 0.f, b);
-            to_floats<T>(load_vec_part((const T*)g.U + i * g.ldu + c, count), uh);
-            if (g.gate > 1) to_floats<T>(load_vec_part((const T*)g.A + i * g.lda + c, count), a);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (g.w_post) uh[e] = e < count ? (uh[e] - st.x) * st.y : 0.f;
-                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
-                d[e] = e < count ? dx[e] * gate : 0.f;
-                da[e] = d[e] * sc[e] * fmaf(uh[e], w[e], b[e]) * (1.f - gate);
-                gv[e] = d[e] * sc[e] * w[e];
             }
-        };
-        float s[3] = {0.f, 0.f, 0.f};
+            join_lanes<1024>(s, meet, turn);
+            r.along = s[0] * inv_f;
+            r.mean = g.layer ? s[1] * inv_f : 0.f;
+        }
         if (g.U && (g.w_post || g.gate == 1)) {
-            each([&](float(&dx)[E], float(&)[E], float(&)[E], float(&)[E], int64_t c, int count) {
-                float uh[E], d[E], da[E], gv[E];
-                block(dx, c, count, uh, d, da, gv);
+            float s[3] = {0.f, 0.f, 0.f};
+            for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
+                const int count = g.f - c < E ? (int)(g.f - c) : E;
+                float dx[E], xh[E], dh[E], w_pre[E], scale[E], w_post[E], b_post[E], uh[E], d[E], da[E], de[E];
+                load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
+                long_vectors<E>(g, c, count, scale, w_post, b_post);
+                long_stream_side<T, E>(g, i, c, count, st, w_pre, r.along, r.mean, dx, xh, dh);
+                long_block_side<T, E>(g, i, c, count, st, r.gate, scale, w_post, b_post, dx, uh, d, da, de);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    s[0] = fmaf(gv[e], uh[e], s[0]);
-                    s[1] += gv[e];
+                    s[0] = fmaf(de[e], uh[e], s[0]);
+                    s[1] += de[e];
                     s[2] += da[e];
                 }
-            });
-            join_lanes<1024>(s, meet, turn);
-        }
-        const float ualong = s[0] * inv_f, umean = g.layer ? s[1] * inv_f : 0.f;
-        each([&](float(&dx)[E], float(&xh)[E], float(&gh)[E], float(&)[E], int64_t c, int count) {
-            float uh[E], d[E], da[E], gv[E];
-            if (g.U) block(dx, c, count, uh, d, da, gv);
-            for (int e = 0; e < count; ++e) {
-                grow(2, c + e, gh[e] * xh[e]);
-                grow(3, c + e, gh[e]);
-                if (!g.U) continue;
-                grow(0, c + e, d[e] * uh[e]);
-                grow(1, c + e, d[e]);
             }
-            if (g.dX) store_vec_part((T*)g.dX + i * g.lddx + c, from_floats<T>(dx), count);
-            if (!g.U) return;
-            if (g.dA && g.gate > 1) store_vec_part((T*)g.dA + i * g.ldda + c, from_floats<T>(da), count);
-            if (!g.dU) return;
-            if (g.w_post)
+            join_lanes<1024>(s, meet, turn);
+            r.along_u = s[0] * inv_f;
+            r.mean_u = g.layer ? s[1] * inv_f : 0.f;
+            r.dgate = s[2];
+        }
+        if (g.rows) {
+            if (threadIdx.x == 0) g.rows[i] = r;
+            continue;
+        }
+        for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {
+            const int count = g.f - c < E ? (int)(g.f - c) : E;
+            float dx[E], xh[E], dh[E], w_pre[E], scale[E], w_post[E], b_post[E], uh[E], d[E], da[E], de[E];
+            load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
+            long_stream_side<T, E>(g, i, c, count, st, w_pre, r.along, r.mean, dx, xh, dh);
+            if (g.U) {
+                long_vectors<E>(g, c, count, scale, w_post, b_post);
+                long_block_side<T, E>(g, i, c, count, st, r.gate, scale, w_post, b_post, dx, uh, d, da, de);
+            }
+            long_matrices<T, E>(g, i, c, count, st, r, dx, uh, da, de);
+        }
+    }
+}
+
+// 64 lanes of E columns by four rows at a time; a share of the rows, whose sums are the four row sets' in order.  What is written may take the place of what is read here.
+template <typename T>
+__global__ __launch_bounds__(256) void k_block_norm_back_columns(NormArgs g, int64_t rows_per_block) {
+    constexpr int E = Elem<T>::E, SETS = 4;
+    __shared__ float add[SETS][64][E + 1];
+    const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E;
+    const int64_t rb = (int64_t)blockIdx.y * rows_per_block, re = rb + rows_per_block < g.n ? rb + rows_per_block : g.n;
+    const int count = c >= g.f ? 0 : g.f - c < E ? (int)(g.f - c) : E;
+    float sum[4][E] = {};
+    if (count > 0) {
+        float w_pre[E], scale[E], w_post[E], b_post[E];
+        load_floats<E>(g.w_pre, c, count, 1.f, w_pre);
+        long_vectors<E>(g, c, count, scale, w_post, b_post);
+        for (int64_t i = rb + set; i < re; i += SETS) {
+            const f4u st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
+            RowSums r = {0.f, 0.f, 0.f, 0.f, 1.f, 0.f};
+            if (g.rows) r = g.rows[i];
+            float dx[E], xh[E], dh[E], uh[E], d[E], da[E], de[E];
+            long_stream_side<T, E>(g, i, c, count, st, w_pre, r.along, r.mean, dx, xh, dh);
+            if (g.U) long_block_side<T, E>(g, i, c, count, st, r.gate, scale, w_post, b_post, dx, uh, d, da, de);
 #pragma unroll
-                for (int e = 0; e < E; ++e) gv[e] = st.y * (gv[e] - fmaf(uh[e], ualong, umean));
-            store_vec_part((T*)g.dU + i * g.lddu + c, from_floats<T>(gv), count);
-        });
-        // dA may take the place of A, which all lanes have read before the join, and of a row of one element, which is this thread's
-        if (g.dA && g.gate == 1 && threadIdx.x == 0) ((T*)g.dA)[i * g.ldda] = (T)s[2];
+            for (int e = 0; e < E; ++e) {
+                sum[2][e] = fmaf(dh[e], xh[e], sum[2][e]);
+                sum[3][e] += dh[e];
+                if (!g.U) continue;
+                sum[0][e] = fmaf(d[e], uh[e], sum[0][e]);
+                sum[1][e] += d[e];
+            }
+            long_matrices<T, E>(g, i, c, count, st, r, dx, uh, da, de);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (g.at[k] < 0) continue;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) add[set][lane][e] = sum[k][e];
+        __syncthreads();
+        if (set) continue;
+        float* const out = g.part + ((int64_t)blockIdx.y * g.sums + g.at[k]) * g.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            float s = add[0][lane][e];
+            for (int w = 1; w < SETS; ++w) s += add[w][lane][e];
+            if (e < count) out[c + e] = s;
+        }
     }
 }
 
@@ -552,30 +628,40 @@ static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
     // (16-bit elements too by four: eight of them, with the sums, are more than a lane's 128 registers)
     return by_row<4>(g.f, [&](auto l, auto elements) -> int {
         constexpr int L = decltype(l)::value, E = decltype(elements)::value;
-        // as many workgroups as run at one time: each leaves partial sums, which are read again
-        int64_t groups = g.n, most = device_info().cus;
-        if constexpr (L != 0) {
-            using R = NormRows<T, L, E>;
-            groups = (g.n + R::ROWS - 1) / R::ROWS;
-            most *= 1024 / R::THREADS;
-        }
-        const int blocks = (int)(groups < most ? groups : most);
+        const int64_t cus = device_info().cus;
         ScratchLease lease;
-        if (g.sums) {
+        int64_t blocks = 0;
+        auto room = [&](size_t rows) -> int {                     // for `blocks` partial sums and, before them, what there is for each row
             void* mem = nullptr;
-            GCN_TRY(lease.get(&mem, (size_t)blocks * g.sums * g.f * 4, s));
-            g.part = (float*)mem;
-        }
+            const size_t bytes = rows + (size_t)blocks * g.sums * g.f * 4;      // (24 bytes for a row: the sums behind them are aligned)
+            if (bytes) GCN_TRY(lease.get(&mem, bytes, s));
+            if (rows) g.rows = (RowSums*)mem;
+            if (g.sums) g.part = (float*)((char*)mem + rows);
+            return GCN_OK;
+        };
         if constexpr (L == 0) {
-            hipLaunchKernelGGL((k_block_norm_back_long<T>), dim3((unsigned)blocks), dim3(1024), 0, s, g);
+            const int64_t across = (g.f + 64 * Elem<T>::E - 1) / (64 * Elem<T>::E);
+            const RowShares shares = row_shares(g.n, across, cus);
+            blocks = shares.count;
+            const bool rows = !g.sums || g.dH || g.w_post || g.gate == 1;
+            GCN_TRY(room(rows && g.sums ? (size_t)g.n * sizeof(RowSums) : 0));
+            if (rows) {
+                hipLaunchKernelGGL((k_block_norm_back_rows<T>), dim3((unsigned)(g.n < 2 * cus ? g.n : 2 * cus)), dim3(1024), 0, s, g);
+                GCN_LAUNCH_CHECK();
+            }
+            if (g.sums) hipLaunchKernelGGL((k_block_norm_back_columns<T>), dim3((unsigned)across, (unsigned)blocks), dim3(256), 0, s, g, shares.rows);
         } else {
+            // as many workgroups as run at one time: each leaves partial sums, which are read again
             using R = NormRows<T, L, E>;
+            const int64_t groups = (g.n + R::ROWS - 1) / R::ROWS, most = cus * (1024 / R::THREADS);
+            blocks = groups < most ? groups : most;
+            GCN_TRY(room(0));
             if (g.layer || g.b_post || v.db_post || v.db_pre) hipLaunchKernelGGL((k_block_norm_back<T, L, E, true>), dim3((unsigned)blocks), dim3(R::THREADS), 0, s, g);
             else hipLaunchKernelGGL((k_block_norm_back<T, L, E, false>), dim3((unsigned)blocks), dim3(R::THREADS), 0, s, g);
         }
         GCN_LAUNCH_CHECK();
         if (g.sums) {
-            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)norm_vector_groups(g.f)), dim3(1024), 0, s, g, blocks, v);
+            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)norm_vector_groups(g.f)), dim3(1024), 0, s, g, (int)blocks, v);
             GCN_LAUNCH_CHECK();
         }
         return GCN_OK;

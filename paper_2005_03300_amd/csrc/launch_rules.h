@@ -95,4 +95,17 @@ constexpr int32_t LINEAR_WIDEST = 1 << 27, NORM_WIDEST = 1 << 26;
 constexpr int64_t column_sum_groups(int64_t count) { return (count + 63) / 64; }
 constexpr int64_t norm_vector_groups(int64_t f) { return f < (1 << 20) ? (f + 15) / 16 : (1 << 16); }
 
+// Shares of n rows for a pass over matrices that is `across` workgroups wide: eight workgroups for each compute unit where there are rows enough for 16 each, in
+// multiples of four rows.  What the shares leave of sums over the rows, a number for each column, stays small: more columns take more workgroups and so fewer shares.
+struct RowShares {
+    int64_t rows, count;
+};
+inline RowShares row_shares(int64_t n, int64_t across, int64_t cus) {
+    int64_t count = (8 * cus + across - 1) / across;
+    if (count > (n + 15) / 16) count = (n + 15) / 16;
+    if (count > 1024) count = 1024;
+    const int64_t rows = ((n + count - 1) / count + 3) / 4 * 4;
+    return {rows, (n + rows - 1) / rows};
+}
+
 }  // namespace gcn

@@ -78,11 +78,8 @@ template <typename T>
 static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho, void* dZ,
                         int64_t lddz, void* dR, int64_t lddr, float* dbias, hipStream_t s) {
     const int64_t wide = 64 * Elem<T>::E, across = (N + wide - 1) / wide;
-    int64_t blocks = (8LL * device_info().cus + across - 1) / across;
-    if (blocks > (n + 15) / 16) blocks = (n + 15) / 16;
-    if (blocks > 1024) blocks = 1024;
-    const int64_t per = ((n + blocks - 1) / blocks + 3) / 4 * 4;
-    blocks = (n + per - 1) / per;
+    const RowShares shares = row_shares(n, across, device_info().cus);
+    const int64_t per = shares.rows, blocks = shares.count;
     ScratchLease lease;
     void* part = dbias;                                           // the sums of a single share of the rows are the result
     if (dbias && blocks > 1) GCN_TRY(lease.get(&part, (size_t)blocks * N * 4, s));

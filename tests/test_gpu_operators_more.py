@@ -7,7 +7,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_operators import ALL, EPS, TINY, TYPES, UNIT, check, code, gen_of, lib, normal
+from test_gpu_operators import ALL, DEPTH, EPS, TINY, TYPES, UNIT, check, gen_of, lib, norm64, normal, unit_gradient64
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +98,75 @@ def test_gradient_of_a_gate_in_place_of_a_row_of_one_element():
         dX, dU = e(), e()
         g.gcn_block_norm_backward(o["U"], o["Xout"], stats, o["dXout"], o["dH"], dX, dU, w_pre=w, w_post=w, A=o["A"], dA=o[name], kind=g.NORM_LAYER)
         assert torch.equal(dX, want[0]) and torch.equal(dU, want[1]) and torch.equal(o[name], want[2]), name
+
+
+# ---- rows longer than registers hold, and shorter than a lane's elements --------------------------------------------
+@pytest.mark.parametrize("type_", ALL)
+@pytest.mark.parametrize("n,f,gate,layer", [(70, 9001, "full", True), (133, 8200, "row", False), (37, 16384, None, True), (5000, 3, "row", True),
+                                            (3001, 2, "full", False), (257, 1, "row", False)])
+def test_block_norm_backward_of_many_rows(type_, n, f, gate, layer):
+    """Rows in several shares: every gradient against the formula in 64 bits, and the vectors' the same bits in every call."""
+    g = lib()
+    gen = gen_of("long", type_, n, f)
+    columns = {"full": f, "row": 1, None: 0}[gate]
+    U, Xo, C, D = (normal(gen, (n, f), type_, s).cuda() for s in (2.0, 1.3, 1.0, 1.0))
+    A = normal(gen, (n, columns), type_).cuda() if gate else None
+    vec = lambda c: (c + 0.2 * torch.randn(f, generator=gen, dtype=torch.float64)).float().cuda()
+    scale, wp, w = vec(0.3), vec(1.0), vec(1.0)
+    bp = vec(0.0) if layer else None
+    xo, u, c, d, sc, w2, wp2 = (t.double() for t in (Xo, U, C, D, scale, w, wp))
+    stats64 = torch.zeros(n, 4, dtype=torch.float64, device="cuda")
+    _, stats64[:, 0:1], stats64[:, 1:2], _ = norm64(u, wp2, None, layer)
+    _, stats64[:, 2:3], stats64[:, 3:4], _ = norm64(xo, w2, None, layer)
+    stats = stats64.float()
+    um, ur, xm, xr = stats.double().split(1, dim=1)
+    e = lambda *s: torch.full(s, 7.0, dtype=TYPES[type_], device="cuda")
+    v = lambda: torch.full((f,), 7.0, device="cuda")
+    out = dict(dX=e(n, f), dU=e(n, f), dA=e(n, columns) if gate else None, dscale=v(), dw_post=v(), db_post=v() if layer else None, dw_pre=v(), db_pre=v())
+    common = dict(w_pre=w, A=A, scale=scale, w_post=wp, b_post=bp, kind=g.NORM_LAYER if layer else g.NORM_RMS)
+    g.gcn_block_norm_backward(U, Xo, stats, C, D, **out, **common)
+    K, unit, tiny = 4 * DEPTH * EPS, UNIT[type_], TINY[type_]
+    xhat, xsize = (xo - xm) * xr, (xo.abs() + xm.abs()) * xr
+    dx = c + unit_gradient64(d * w2, xhat, xr, layer)[0]
+    size = c.abs() + unit_gradient64((d * w2).abs(), xsize, xr, True)[1]
+    s = torch.sigmoid(A.double()) if gate else torch.ones(n, 1, dtype=torch.float64, device="cuda")
+    b = bp.double() if layer else 0 * sc
+    uhat, usize = (u - um) * ur, (u.abs() + um.abs()) * ur
+    val, vsize = uhat * wp2 + b, usize * wp2.abs() + b.abs()
+    dv, dvsize = dx * sc * s, size * sc.abs() * s
+    du = unit_gradient64(dv * wp2, uhat, ur, layer)[0]
+    dusize = unit_gradient64(dvsize * wp2.abs(), usize, ur, True)[1]
+    check(out["dX"], dx.cpu(), (K * size + unit * dx.abs() + tiny).cpu(), "dX")
+    check(out["dU"], du.cpu(), (K * dusize + unit * du.abs() + tiny).cpu(), "dU")
+    if gate:
+        da, dasize = dx * sc * val * s * (1 - s), size * sc.abs() * vsize * s
+        if columns != f:
+            da, dasize = da.sum(1, keepdim=True), dasize.sum(1, keepdim=True)
+        check(out["dA"], da.cpu(), (K * dasize + unit * da.abs() + tiny).cpu(), "dA")
+    KV = K + (n + 2) * EPS
+    sums = dict(dscale=(dx * s * val, size * s * vsize), dw_post=(dv * uhat, dvsize * usize), db_post=(dv, dvsize), dw_pre=(d * xhat, d.abs() * xsize),
+                db_pre=(d, d.abs()))
+    for name, (terms, sizes) in sums.items():
+        if out[name] is not None:
+            check(out[name], terms.sum(0).cpu(), (KV * sizes.sum(0) + 1e-37).cpu(), name)
+    # again, in place of the inputs
+    again = {k: torch.empty_like(t) for k, t in out.items() if t is not None and t.dim() == 1}
+    place = dict(dX=U.clone(), dU=C.clone(), dA=A.clone() if gate else None)
+    g.gcn_block_norm_backward(place["dX"], Xo, stats, place["dU"], D, **place, **again, **dict(common, A=place["dA"]))
+    assert all(torch.equal(t, out[k]) for k, t in {**again, **place}.items() if t is not None)
+
+
+def test_scratch_of_a_norm_s_gradients_is_bounded():
+    """256 rows of 2^18 elements: the call keeps some tens of megabytes of partial sums, not a copy of its operands in fp32."""
+    g = lib()
+    n, f = 256, 1 << 18
+    e = lambda: torch.zeros(n, f, dtype=torch.bfloat16, device="cuda")
+    U, Xo, D, stats = e(), e(), e(), torch.ones(n, 4, device="cuda")
+    v = [torch.ones(f, device="cuda") for _ in range(6)]
+    torch.cuda.synchronize()
+    g.gcn_scratch_release()
+    before = torch.cuda.mem_get_info()[0]
+    g.gcn_block_norm_backward(U, Xo, stats, None, D, w_pre=v[0], w_post=v[1], dscale=v[2], dw_post=v[3], db_post=v[4], dw_pre=v[5], kind=g.NORM_LAYER)
+    torch.cuda.synchronize()
+    assert before - torch.cuda.mem_get_info()[0] < (64 << 20)
+    assert all(bool((t == 0).all()) for t in v[2:])

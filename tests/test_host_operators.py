@@ -54,3 +54,25 @@ def test_launches_for_the_widest_rows_are_launchable(tmp_path):
         }
     """)
     assert r.returncode == 0, r.stdout
+
+
+def test_scratch_of_sums_over_the_rows(tmp_path):
+    """Every row is in one share, and the partial sums of four vectors stay below 17 MB and four rows of fp32, for rows of any width."""
+    r = run_cpp(tmp_path, """
+        #include <cstdio>
+        #include <initializer_list>
+        #include "launch_rules.h"
+        using namespace gcn;
+        int main() {
+            for (int64_t wide : {256, 512})
+                for (int64_t f = 1; f <= NORM_WIDEST; f += f / 3 + 1)
+                    for (int64_t n = 1; n <= 3000000; n += n / 2 + 1) {
+                        const int64_t across = (f + wide - 1) / wide;
+                        const RowShares s = row_shares(n, across, 256);
+                        if (s.count < 1 || s.count > 65535 || s.rows % 4 || s.count * s.rows < n || (s.count - 1) * s.rows >= n)
+                            return printf("shares of %lld rows\\n", (long long)n), 1;
+                        if (s.count * f * 16 > 17000000 + 16 * f) return printf("%lld x %lld: %lld shares\\n", (long long)n, (long long)f, (long long)s.count), 1;
+                    }
+        }
+    """)
+    assert r.returncode == 0, r.stdout
