@@ -10,6 +10,8 @@
  *   - Every pointer named "device" is HIP device memory on the current device; "host" is host
  *     memory.  Dense matrices are row-major, with a leading dimension in elements: fp32, and in the calls that take an
  *     element type (gcn_linear_*, gcn_block_norm_*, gcn_distill) of that type.
+ *     In these calls operands that may not overlap may have no element in common; matrices whose rows take turns in one buffer
+ *     (halves of n x 2f) have none, an output beside an input among them.
  *   - Dense buffers are owned by the caller; the library neither frees nor keeps them after the
  *     work queued on `stream` has finished.  Only gcn_csr objects own device memory.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Compute calls only

@@ -673,7 +673,7 @@ static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
 using namespace gcn;
 
 // Whether outputs overlap inputs or each other otherwise than element by element: an output of the rows' size may be an input of that size
-// (same address and leading dimension).
+// (same address and, of several rows, leading dimension).
 struct Place {
     const void* p;
     int64_t cols, ld;
@@ -684,7 +684,7 @@ static bool misplaced(int64_t n, int32_t f, size_t b, std::initializer_list<Plac
     const Span st(stats, n, 4, 4, 4);
     for (const Place* o = out.begin(); o != out.end(); ++o) {
         for (const Place& i : in)
-            if (span(*o).meets(span(i)) && !(o->p == i.p && o->ld == i.ld && o->cols == i.cols)) return true;
+            if (span(*o).meets(span(i)) && !span(*o).is(span(i))) return true;
         for (const Place* q = out.begin(); q != o; ++q)
             if (span(*o).meets(span(*q))) return true;
         for (const void* v : vectors_in)

@@ -290,7 +290,7 @@ extern "C" int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_
     if (m <= 0) return fail(GCN_ERR_BADARG, "%s: m must be positive", who);
     const size_t b = elem_bytes(type);
     const Span z(Z, n, C, ldz, b), g(G, n, C, ldg, b), at(top, n, k, ldtop, 4), tt(t, n, k, ldt, b), y(labels, 1, n, n, 4), l(loss, 1, 1, 1, 4);
-    if ((g.meets(z) && (G != Z || ldg != ldz)) || g.meets(at) || g.meets(tt) || g.meets(y) || l.meets(z) || l.meets(g) || l.meets(at) || l.meets(tt) || l.meets(y))
+    if ((g.meets(z) && !g.is(z)) || g.meets(at) || g.meets(tt) || g.meets(y) || l.meets(z) || l.meets(g) || l.meets(at) || l.meets(tt) || l.meets(y))
         return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
     DistillArgs a;
     a.n = n; a.C = C; a.k = w_teacher != 0.f ? k : 0; a.Z = Z; a.ldz = ldz; a.G = G; a.ldg = ldg; a.top = top; a.ldtop = ldtop; a.t = t; a.ldt = ldt;

@@ -3,6 +3,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "places.h"
 
 namespace gcn {
 
@@ -147,17 +148,6 @@ int by_type(int type, const F& f) {
     return f(_Float16());
 }
 inline bool known_type(int type) { return type == GCN_F32 || type == GCN_BF16 || type == GCN_F16; }
-
-// Rows of `cols` elements of `bytes` each, `ld` apart, as a range of addresses.
-struct Span {
-    uintptr_t from = 0, to = 0;
-    Span(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t bytes) {
-        if (!p || rows <= 0) return;
-        from = (uintptr_t)p;
-        to = from + ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * bytes;
-    }
-    bool meets(const Span& o) const { return from < o.to && o.from < to; }
-};
 
 // `group`s of 64 results, each the sum of `parts` partial results in a fixed order (see sum_of_parts).
 int vector_sums_launch(const float* part, int parts, int64_t count, float* out, hipStream_t s);

@@ -110,7 +110,7 @@ extern "C" int gcn_linear_forward(int64_t n, int32_t f_in, int32_t f_out, int ty
     const size_t b = elem_bytes(type);
     const Span x(X, n, f_in, ldx, b), w(W, f_in, f_out, ldw, b), y(Y, n, f_out, ldy, b), z(Z, n, f_out, ldz, b), r(R, n, f_out, ldr, b);
     const Span v(bias, 1, f_out, f_out, 4);
-    if (y.meets(x) || y.meets(w) || z.meets(x) || z.meets(w) || z.meets(y) || z.meets(r) || y.meets(v) || z.meets(v) || (y.meets(r) && (R != Y || ldr != ldy)))
+    if (y.meets(x) || y.meets(w) || z.meets(x) || z.meets(w) || z.meets(y) || z.meets(r) || y.meets(v) || z.meets(v) || (y.meets(r) && !y.is(r)))
         return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
     TileArgs a;
     a.A = X; a.lda = ldx; a.B = W; a.ldb = ldw; a.M = n; a.N = f_out; a.K = f_in;
@@ -143,8 +143,8 @@ extern "C" int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int t
     for (int o = 0; o < 5; ++o) {
         for (int i = 0; i < 4; ++i) {
             // an element of dZ may take the place of the one of Z or dY that it is made of, one of dR that of dY
-            const bool same = (o == 0 && i == 2 && dZ == Z && lddz == ldz) || (o == 0 && i == 3 && dZ == dY && lddz == lddy) ||
-                              (o == 1 && i == 3 && dR == dY && lddr == lddy && (curved || !products));
+            const bool may = (o == 0 && (i == 2 || i == 3)) || (o == 1 && i == 3 && (curved || !products));
+            const bool same = may && out[o].is(in[i]);
             bad |= out[o].meets(in[i]) && !same;
         }
         for (int i = 0; i < o; ++i) bad |= out[o].meets(out[i]);

@@ -170,3 +170,102 @@ def test_scratch_of_a_norm_s_gradients_is_bounded():
     torch.cuda.synchronize()
     assert before - torch.cuda.mem_get_info()[0] < (64 << 20)
     assert all(bool((t == 0).all()) for t in v[2:])
+
+
+# ---- operands side by side ------------------------------------------------------------------------------------------
+def halves(n, left, right, dtype, mark=3.0):
+    """Two matrices whose rows take turns in one buffer."""
+    both = torch.full((n, left + right), mark, dtype=dtype, device="cuda")
+    return both[:, :left], both[:, left:]
+
+
+@pytest.mark.parametrize("type_", ALL)
+@pytest.mark.parametrize("n,K,N", [(5, 48, 40), (200, 65, 130)])
+def test_linear_operands_side_by_side(type_, n, K, N):
+    """Y beside Z, Y beside X, and the gradients beside what they are made of: the results of matrices by themselves."""
+    g = lib()
+    dt = TYPES[type_]
+    gen = gen_of("beside", type_, n)
+    x, W, dy = normal(gen, (n, K), type_).cuda(), normal(gen, (K, N), type_, K ** -0.5).cuda(), normal(gen, (n, N), type_).cuda()
+    e = lambda *s: torch.empty(*s, dtype=dt, device="cuda")
+    y0, z0 = e(n, N), e(n, N)
+    g.gcn_linear_forward(x, W, y0, act=g.ACT_SILU, Z=z0)
+    Y, Z = halves(n, N, N, dt)
+    g.gcn_linear_forward(x, W, Y, act=g.ACT_SILU, Z=Z)
+    assert torch.equal(Y, y0) and torch.equal(Z, z0)
+    X, Y = halves(n, K, N, dt)
+    X.copy_(x)
+    g.gcn_linear_forward(X, W, Y, act=g.ACT_SILU)
+    assert torch.equal(Y, y0) and torch.equal(X, x)
+    dz0, dx0, dw0 = e(n, N), e(n, K), e(K, N)
+    g.gcn_linear_backward(x, W, z0, dy, dz0, dX=dx0, dW=dw0, act=g.ACT_SILU)
+    Z, dZ = halves(n, N, N, dt)
+    Z.copy_(z0)
+    X, dX = halves(n, K, K, dt)
+    X.copy_(x)
+    V, dW = halves(K, N, N, dt)
+    V.copy_(W)
+    g.gcn_linear_backward(X, V, Z, dy, dZ, dX=dX, dW=dW, act=g.ACT_SILU)
+    assert torch.equal(dZ, dz0) and torch.equal(dX, dx0) and torch.equal(dW, dw0)
+    assert torch.equal(Z, z0) and torch.equal(X, x) and torch.equal(V, W)
+    # one element in common, at the end of a row and at the start of the next
+    wide = torch.zeros(n, 2 * N, dtype=dt, device="cuda")
+    for at in (N - 1, 1):
+        with pytest.raises(g.GcnError, match="overlaps"):
+            g.gcn_linear_forward(x, W, wide[:, :N], Z=wide[:, at:at + N])
+
+
+@pytest.mark.parametrize("type_", ALL)
+@pytest.mark.parametrize("f", [5, 130, 9001])
+def test_block_norm_operands_side_by_side(type_, f):
+    """U and A from one wide product, their gradients likewise, X' beside H."""
+    g = lib()
+    dt, n = TYPES[type_], 6
+    gen = gen_of("besidenorm", type_, f)
+    x, u, a, c, d = (normal(gen, (n, f), type_).cuda() for _ in range(5))
+    w = torch.ones(f, device="cuda")
+    e = lambda: torch.empty(n, f, dtype=dt, device="cuda")
+    xo, h, dx, du, da, stats = e(), e(), e(), e(), e(), torch.empty(n, 4, device="cuda")
+    g.gcn_block_norm_forward(x, u, xo, h, w_pre=w, w_post=w, A=a, stats=stats)
+    g.gcn_block_norm_backward(u, xo, stats, c, d, dx, du, w_pre=w, w_post=w, A=a, dA=da)
+    (U, A), (Xo, H), (dU, dA) = (halves(n, f, f, dt) for _ in range(3))
+    U.copy_(u), A.copy_(a)
+    g.gcn_block_norm_forward(x, U, Xo, H, w_pre=w, w_post=w, A=A)
+    assert torch.equal(Xo, xo) and torch.equal(H, h)
+    dX = e()
+    g.gcn_block_norm_backward(U, Xo, stats, c, d, dX, dU, w_pre=w, w_post=w, A=A, dA=dA)
+    assert torch.equal(dX, dx) and torch.equal(dU, du) and torch.equal(dA, da)
+    g.gcn_block_norm_backward(U, Xo, stats, c, d, dX, U, w_pre=w, w_post=w, A=A, dA=A)      # each in the place of its own operand
+    assert torch.equal(U, du) and torch.equal(A, da)
+    with pytest.raises(g.GcnError, match="overlaps"):
+        wide = torch.zeros(n, 2 * f, dtype=dt, device="cuda")
+        g.gcn_block_norm_forward(x, u, wide[:, :f], wide[:, f - 1:2 * f - 1], w_pre=w)
+
+
+def test_one_row_in_place_whatever_its_leading_dimension():
+    """A single row has no other: its place is its address and width."""
+    g = lib()
+    f = 40
+    x = torch.randn(1, f, device="cuda")
+    w, want, place = torch.ones(f, device="cuda"), torch.empty_like(x), x.clone()
+    g.gcn_block_norm_forward(x, H=want, w_pre=w)
+    L, p = g.lib(), place.data_ptr()
+    rc = L.gcn_block_norm_forward(1, f, g.F32, g.NORM_RMS, 1e-5, p, f, None, 0, None, 0, 0, None, None, None, w.data_ptr(), None, None, 0, p, 2 * f, None,
+                                  g.binding._now())
+    assert rc == 0 and torch.equal(place, want)
+
+
+@pytest.mark.parametrize("type_", ALL)
+@pytest.mark.parametrize("C", [41, 700, 20001])
+def test_distill_gradient_beside_the_logits(type_, C):
+    g = lib()
+    dt, n, k = TYPES[type_], 5, 3
+    gen = gen_of("besidekd", type_, C)
+    z, t = normal(gen, (n, C), type_).cuda(), normal(gen, (n, k), type_).cuda()
+    top = torch.stack([torch.randperm(C, generator=gen)[:k] for _ in range(n)]).int().cuda()
+    g0, loss0, loss = torch.empty_like(z), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    g.gcn_distill(z, top, t, loss0, g0)
+    Z, G = halves(n, C, C, dt)
+    Z.copy_(z)
+    g.gcn_distill(Z, top, t, loss, G)
+    assert torch.equal(G, g0) and torch.equal(loss, loss0) and torch.equal(Z, z)

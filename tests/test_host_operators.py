@@ -76,3 +76,47 @@ def test_scratch_of_sums_over_the_rows(tmp_path):
         }
     """)
     assert r.returncode == 0, r.stdout
+
+
+def test_matrices_meet_where_they_have_a_byte_in_common(tmp_path):
+    """Against the bytes of both, one by one: random matrices in a small buffer, contiguous and strided, at equal and at different pitches."""
+    r = run_cpp(tmp_path, """
+        #include <cstdio>
+        #include <random>
+        #include <set>
+        #include "places.h"
+        using namespace gcn;
+        int main() {
+            std::mt19937 rng(5);
+            auto upto = [&](int n) { return (int)(rng() % (unsigned)(n + 1)); };
+            static char buffer[4096];
+            int met = 0, same = 0, between = 0;
+            for (int round = 0; round < 200000; ++round) {
+                struct M { int at, rows, cols, ld, bytes; } m[2];
+                for (M& x : m) {
+                    x.bytes = 2 << upto(1);
+                    x.rows = 1 + upto(4); x.cols = 1 + upto(4); x.ld = x.cols + (upto(2) ? upto(6) : 0); x.at = 2 * upto(40);
+                }
+                if (upto(1)) { m[1].ld = m[0].ld < m[1].cols ? m[1].ld : m[0].ld; m[1].bytes = m[0].bytes; }
+                if (!upto(9)) m[1] = m[0];
+                std::set<int> have[2];
+                for (int k = 0; k < 2; ++k)
+                    for (int i = 0; i < m[k].rows; ++i)
+                        for (int b = 0; b < m[k].cols * m[k].bytes; ++b) have[k].insert(m[k].at + i * m[k].ld * m[k].bytes + b);
+                bool meet = false;
+                for (int b : have[0]) meet |= have[1].count(b) > 0;
+                const Span p(buffer + m[0].at, m[0].rows, m[0].cols, m[0].ld, m[0].bytes), q(buffer + m[1].at, m[1].rows, m[1].cols, m[1].ld, m[1].bytes);
+                if (p.meets(q) != meet || q.meets(p) != meet) {
+                    for (const M& x : m) printf("%d: %d x %d, %d apart, of %d bytes\\n", x.at, x.rows, x.cols, x.ld, x.bytes);
+                    return 1;
+                }
+                if (m[0].rows == m[1].rows && m[0].bytes == m[1].bytes && p.is(q) != (have[0] == have[1] && m[0].cols == m[1].cols)) return printf("the same place\\n"), 1;
+                met += meet; same += p.is(q);
+                between += !meet && *have[0].begin() < *have[1].rbegin() && *have[1].begin() < *have[0].rbegin();
+            }
+            const Span none(nullptr, 3, 3, 3, 4), some(buffer, 3, 3, 3, 4);
+            if (none.meets(some) || some.meets(none)) return printf("nothing meets something\\n"), 1;
+            return met > 1000 && same > 1000 && between > 1000 ? 0 : (printf("%d %d %d\\n", met, same, between), 1);
+        }
+    """)
+    assert r.returncode == 0, r.stdout
