@@ -108,4 +108,44 @@ inline RowShares row_shares(int64_t n, int64_t across, int64_t cus) {
     return {rows, (n + rows - 1) / rows};
 }
 
+// The tiles of a product: their edge, and in how many shares the sum over k is cut.
+struct TileChoice {
+    int edge, splits;
+};
+struct TileKind {
+    int edge, most;         // most: workgroups that a compute unit has room for
+    double full, way;             // share of the matrix units' rate with that many; microseconds that a stage takes to come from memory
+};
+// The choice with the least estimated time.  A stage takes what the products of all workgroups of a compute unit do, at a rate that grows with the tiles
+// (16384 x 4096 x 4096 in bf16: 1.2 PFLOP/s at 256 x 256, 1.05 at 128 x 128, 0.73 at 64 x 64; 8192 x 8192 x 8192 in fp32: 210 and 155 TFLOP/s at 128 and 64), but no
+// less than a stage's way from memory, which is longer through registers.  Splits fill the chip where there are few tiles, and cost partial results written and
+// read again and a launch.
+inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, bool direct, int64_t cus) {
+    static const TileKind KINDS16[] = {{256, 1, 1.0, 1.2}, {128, 2, 0.88, 0.8}, {64, 5, 0.61, 0.6}};
+    static const TileKind KINDS32[] = {{128, 2, 1.0, 1.1}, {64, 3, 0.74, 0.5}};               // (larger ones win nothing, and there are fewer of them)
+    const double rate = fp32 ? 0.82e6 : 4.7e6;                    // FLOP per microsecond of one compute unit
+    const int64_t depth = fp32 ? 32 : 64, stages = (K + depth - 1) / depth;
+    TileChoice best{64, 1};
+    double least = 1e300;
+    for (int i = 0; i < (fp32 ? 2 : 3); ++i) {
+        const TileKind& kind = fp32 ? KINDS32[i] : KINDS16[i];
+        const int64_t tiles = ((M + kind.edge - 1) / kind.edge) * ((N + kind.edge - 1) / kind.edge);
+        const double way = kind.way * (direct ? 1.0 : 1.5);
+        for (int64_t splits = 1; splits <= 512; splits += splits < 4 ? 1 : splits / 2) {
+            const int64_t share = (stages + splits - 1) / splits;
+            if (splits > 1 && (share < 2 || tiles * (splits - 1) > 4 * cus)) break;
+            const int64_t count = tiles * splits, each = (count + cus - 1) / cus;      // of one compute unit
+            const int64_t rounds = (each + kind.most - 1) / kind.most, together = each < kind.most ? each : kind.most;
+            const double products = together * 2.0 * kind.edge * kind.edge * depth / (rate * kind.full);
+            double us = rounds * (share * (products > way ? products : way) + 1.5);
+            if (splits > 1) us += 3.0 + splits * (double)M * N * 8 / 4.0e6;
+            if (us < least) {
+                least = us;
+                best = {kind.edge, (int)splits};
+            }
+        }
+    }
+    return best;
+}
+
 }  // namespace gcn

@@ -4,6 +4,7 @@ import re
 
 import numpy as np
 
+from linear_tiles import PRODUCTS
 from test_host_parts import ROOT, run_cpp
 
 
@@ -120,3 +121,22 @@ def test_matrices_meet_where_they_have_a_byte_in_common(tmp_path):
         }
     """)
     assert r.returncode == 0, r.stdout
+
+
+def test_every_tile_of_a_product_is_tested(tmp_path):
+    """The sizes that the GPU tests take stand for the tile and the split that the rule gives them, and for all that there are."""
+    for kind, whole, edge, splits, M, N, K in PRODUCTS:
+        assert M % edge and N % edge and K % 64 and (not whole or (M % 8 == 0 and N % 8 == 0))
+    calls = "".join(f'say({M}, {N}, {K}, {int(kind == "f32")}, {int(whole)});' for kind, whole, _, _, M, N, K in PRODUCTS)
+    r = run_cpp(tmp_path, """
+        #include <cstdio>
+        #include "launch_rules.h"
+        void say(int64_t M, int64_t N, int64_t K, int fp32, int direct) {
+            const gcn::TileChoice c = gcn::choose_tiles(M, N, K, fp32, direct, 256);
+            printf("%%d %%d\\n", c.edge, c.splits);
+        }
+        int main() { %s }
+    """ % calls)
+    assert [tuple(map(int, line.split())) for line in r.stdout.splitlines()] == [p[2:4] for p in PRODUCTS]
+    assert {(p[0], p[1], p[2], p[3] > 1) for p in PRODUCTS} == {("16", w, e, s) for w in (False, True) for e in (256, 128, 64) for s in (False, True)} | {
+        ("f32", False, e, s) for e in (128, 64) for s in (False, True)}
