@@ -31,15 +31,6 @@ struct NormArgs {
     int at[4] = {-1, -1, -1, -1};  // which of them are sum dX' a u^, sum dX' a, sum dH x^, sum dH
 };
 
-// (by the instructions for a power of 2 and a reciprocal: off by a few 2^-24)
-__device__ __forceinline__ float gate_of(float a) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -1.4426950408889634f));
-#else
-    return 0.f;
-#endif
-}
-
 // L lanes (a power of two, up to 1024) hold a row, E neighbouring elements each; a workgroup has as many rows at a time as make 512 threads.  All of them
 // go through the same number of steps, with zeros for a row that is not there.  A lane keeps its columns for all its rows, and what the vectors
 // hold for them; columns behind the row's end have zeros there, which keeps what is computed for them out of every sum.
@@ -127,10 +118,10 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm(
                 for (int e = 0; e < E; ++e) u[e] = (u[e] - st.x) * st.y;
             }
             if (g.gate > 1) floats(now.a, a);
-            const float row_gate = g.gate == 1 ? gate_of(now.gate) : 1.f;
+            const float row_gate = g.gate == 1 ? sigmoid<T>(now.gate) : 1.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+                const float gate = g.gate > 1 ? sigmoid<T>(a[e]) : row_gate;
                 x[e] = fmaf(gate, LAYER ? fmaf(u[e], sw[e], sb[e]) : u[e] * sw[e], x[e]);
             }
             if (g.Xout && i < g.n) store_elems<E>((T*)g.Xout + i * g.ldxo + c, x, count);
@@ -226,7 +217,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
         }
         if (g.dX && there) store_elems<E>((T*)g.dX + i * g.lddx + c, dx, count);
         if (g.U) {
-            const float row_gate = g.gate == 1 ? gate_of(now.gate) : 1.f;
+            const float row_gate = g.gate == 1 ? sigmoid<T>(now.gate) : 1.f;
             const float mean_u = g.w_post ? now.st.x : 0.f, rstd_u = g.w_post ? now.st.y : 1.f;
             float u[E], a[E], s[3] = {0.f, 0.f, 0.f};
             floats(now.u, u);
@@ -234,7 +225,7 @@ __global__ __launch_bounds__((NormRows<T, L, E>::THREADS), 4) void k_block_norm_
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 u[e] = (u[e] - mean_u) * rstd_u;
-                const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+                const float gate = g.gate > 1 ? sigmoid<T>(a[e]) : row_gate;
                 const float d = dx[e] * gate;
                 sum[0][e] = fmaf(d, u[e], sum[0][e]);
                 if (LAYER) sum[2][e] += d;
@@ -294,7 +285,7 @@ __global__ __launch_bounds__(1024) void k_block_norm_long(NormArgs g) {
     for (int64_t i = blockIdx.x; i < g.n; i += gridDim.x) {
         const T* const X = (const T*)g.X + i * g.ldx;
         const T* const U = g.U ? (const T*)g.U + i * g.ldu : nullptr;
-        const float row_gate = g.gate == 1 ? gate_of((float)((const T*)g.A)[i * g.lda]) : 1.f;
+        const float row_gate = g.gate == 1 ? sigmoid<T>((float)((const T*)g.A)[i * g.lda]) : 1.f;
         float umean = 0.f, urstd = 0.f, xmean = 0.f, xrstd = 0.f;
         // each(value, column, elements there) for the thread's columns of U, then of X'
         auto each_u = [&](auto f) {
@@ -320,7 +311,7 @@ __global__ __launch_bounds__(1024) void k_block_norm_long(NormArgs g) {
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
                         const float v = g.w_post ? fmaf((u[e] - umean) * urstd, w[e], b[e]) : u[e];
-                        x[e] = fmaf(sc[e] * (g.gate > 1 ? gate_of(a[e]) : row_gate), v, x[e]);
+                        x[e] = fmaf(sc[e] * (g.gate > 1 ? sigmoid<T>(a[e]) : row_gate), v, x[e]);
                     }
                 }
                 f(x, c, count);
@@ -400,7 +391,7 @@ __device__ __forceinline__ void long_block_side(const NormArgs& g, int64_t i, in
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         if (g.w_post) uh[e] = e < count ? (uh[e] - st.x) * st.y : 0.f;
-        const float gate = g.gate > 1 ? gate_of(a[e]) : row_gate;
+        const float gate = g.gate > 1 ? sigmoid<T>(a[e]) : row_gate;
         d[e] = e < count ? dx[e] * gate : 0.f;
         da[e] = d[e] * scale[e] * fmaf(uh[e], w_post[e], b_post[e]) * (1.f - gate);
         de[e] = d[e] * scale[e] * w_post[e];
@@ -436,7 +427,7 @@ __global__ __launch_bounds__(1024) void k_block_norm_back_rows(NormArgs g) {
     for (int64_t i = blockIdx.x; i < g.n; i += gridDim.x) {
         const f4u st = *reinterpret_cast<const f4u*>(g.stats + 4 * i);
         RowSums r = {0.f, 0.f, 0.f, 0.f, 1.f, 0.f};
-        if (g.gate == 1) r.gate = gate_of((float)((const T*)g.A)[i * g.lda]);
+        if (g.gate == 1) r.gate = sigmoid<T>((float)((const T*)g.A)[i * g.lda]);
         if (g.dH) {
             float s[2] = {0.f, 0.f};
             for (int64_t c = (int64_t)threadIdx.x * E; c < g.f; c += STEP) {

@@ -140,6 +140,35 @@ __device__ __forceinline__ void floats_of(Elems<T, COUNT> x, float (&v)[COUNT]) 
 #pragma unroll
     for (int e = 0; e < COUNT; ++e) v[e] = (float)x[e];
 }
+// 2^x and 1/x by the instructions, each off by a unit in the last place.
+constexpr float LOG2E = (float)1.4426950408889634, LOG2E_LOW = (float)(1.4426950408889634 - (double)LOG2E);
+__device__ __forceinline__ float power_of_2(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_exp2f(x);
+#else
+    return 0.f;
+#endif
+}
+__device__ __forceinline__ float inverse(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_rcpf(x);
+#else
+    return 0.f;
+#endif
+}
+// e^x for elements T.  The argument times log2(e) is rounded, which the power feels as 2^-24 of itself for each unit of the argument: nothing to 16-bit elements, but
+// 2^-18 of an fp32 result at -80.  For fp32 elements therefore with what was lost: 2^(t + l) = 2^t (1 + l ln 2) for the small l.  Beyond 2^200 nothing is left of
+// it, and infinities have no such rest; NaN stays NaN.  SiLU of 65536 x 128 x 256 in fp32 82.4 us, without the rest 81.1, with expf 84.2; the norms around a block of
+// 232965 x 128 118.5, 118.4 and 119.1.
+template <typename T>
+__device__ __forceinline__ float exp_for(float x) {
+    const float t = x * LOG2E;
+    if (sizeof(T) == 2) return power_of_2(t);
+    const float low = fmaf(x, LOG2E_LOW, fmaf(x, LOG2E, -t));
+    return power_of_2(t) * fmaf(fabsf(t) > 200.f ? 0.f : low, 0.69314718055994531f, 1.f);
+}
+template <typename T>
+__device__ __forceinline__ float sigmoid(float z) { return inverse(1.f + exp_for<T>(-z)); }
 // Calls f with a value of the element type.
 template <typename F>
 int by_type(int type, const F& f) {

@@ -30,22 +30,6 @@ struct TileArgs {
     int act = GCN_ACT_NONE;
 };
 
-// e^x and 1/x by the instructions (2 to a power; a reciprocal), each off by a unit in the last place, the power also by 2^-24 for each unit of its argument.
-__device__ __forceinline__ float fast_exp(float x) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
-#else
-    return 0.f;
-#endif
-}
-__device__ __forceinline__ float fast_inverse(float x) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_rcpf(x);
-#else
-    return 0.f;
-#endif
-}
-__device__ __forceinline__ float sigmoid(float z) { return fast_inverse(1.f + fast_exp(-z)); }
 // The normal distribution function Phi(z) and its density.  For 16-bit elements erfc by Abramowitz and Stegun's formula 7.1.26, off by 1.5e-7 at most, whose
 // exponential is the density's (erff's way through its ranges made the activation of 16384 x 4096 elements 100 us).
 template <typename T>
@@ -54,7 +38,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& density) {
         density = 0.39894228040143268f * expf(-0.5f * z * z);
         return 0.5f * (1.f + erff(z * 0.70710678118654752f));
     }
-    const float g = fast_exp(-0.5f * z * z), t = fast_inverse(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
+    const float g = exp_for<T>(-0.5f * z * z), t = inverse(fmaf(0.3275911f * 0.70710678118654752f, fabsf(z), 1.f));
     float p = fmaf(1.061405429f, t, -1.453152027f);
     p = fmaf(p, t, 1.421413741f);
     p = fmaf(p, t, -0.284496736f);
@@ -71,7 +55,7 @@ __device__ __forceinline__ float act_of(float z, int act) {
         float density;
         return z * normal_cdf<T>(z, density);
     }
-    if (act == GCN_ACT_SILU) return z * sigmoid(z);
+    if (act == GCN_ACT_SILU) return z * sigmoid<T>(z);
     return z;
 }
 template <typename T>
@@ -83,7 +67,7 @@ __device__ __forceinline__ float slope_of(float z, int act) {
         return fmaf(z, density, phi);
     }
     if (act == GCN_ACT_SILU) {
-        const float s = sigmoid(z);
+        const float s = sigmoid<T>(z);
         return s * fmaf(z, 1.f - s, 1.f);
     }
     return 1.f;

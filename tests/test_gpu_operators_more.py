@@ -269,3 +269,69 @@ def test_distill_gradient_beside_the_logits(type_, C):
     Z.copy_(z)
     g.gcn_distill(Z, top, t, loss, G)
     assert torch.equal(G, g0) and torch.equal(loss, loss0) and torch.equal(Z, z)
+
+
+# ---- exponentials of fp32 elements ----------------------------------------------------------------------------------
+# A power of e off by 2 units in the last place (4 EPS), 1 added, a reciprocal off by one (2 EPS), and up to three products.
+POWERS = 12 * EPS
+
+
+def far():
+    return torch.cat([torch.linspace(-85, 85, 3401), torch.tensor([0.0, -0.5, 1e-6, -1e-6])])
+
+
+def test_silu_of_fp32_far_from_zero():
+    """The activation relative to itself; its slope, whose two terms cancel where it is 0, relative to them."""
+    g = lib()
+    z = far()
+    n = z.numel()
+    X, W = z.reshape(n, 1).cuda(), torch.ones(1, 1, device="cuda")
+    Y = torch.empty(n, 1, device="cuda")
+    g.gcn_linear_forward(X, W, Y, act=g.ACT_SILU)
+    s = torch.sigmoid(z.double())
+    check(Y[:, 0], z.double() * s, POWERS * (z.double() * s).abs() + 1e-37, "silu")
+    few = torch.empty(5, 1, device="cuda")
+    g.gcn_linear_forward(X[:5], W, few, act=g.ACT_SILU)
+    assert torch.equal(few, Y[:5])
+    dZ = torch.empty(n, 1, device="cuda")
+    g.gcn_linear_backward(None, None, X, torch.ones(n, 1, device="cuda"), dZ, act=g.ACT_SILU)
+    # (1 - s) is off by what s is off, relative to 1
+    check(dZ[:, 0], s * (1 + z.double() * (1 - s)), 2 * POWERS * s * (1 + z.double().abs()) + 1e-37, "slope")
+
+
+@pytest.mark.parametrize("f", [3405, 20430])
+@pytest.mark.parametrize("per_row", [False, True])
+def test_gate_of_fp32_far_from_zero(f, per_row):
+    """X' = sigmoid(A) for U = 1 and X = 0, in rows of registers and in longer ones; dU = sigmoid(A) dX'."""
+    g = lib()
+    a = far().repeat(f // 3405)
+    n = 7 if per_row else 1
+    A = a[::500][:n].reshape(n, 1) if per_row else a.reshape(1, f)
+    X, U, Xo = torch.zeros(n, f, device="cuda"), torch.ones(n, f, device="cuda"), torch.empty(n, f, device="cuda")
+    g.gcn_block_norm_forward(X, U, Xo, A=A.cuda())
+    s = torch.sigmoid(A.double()).expand(n, f)
+    check(Xo, s, POWERS * s, "gate")
+    dU = torch.empty(n, f, device="cuda")
+    g.gcn_block_norm_backward(U, None, torch.zeros(n, 4, device="cuda"), U, None, None, dU, A=A.cuda())
+    check(dU, s, POWERS * s, "dU")
+
+
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0, 4.0])
+@pytest.mark.parametrize("C", [41, 700, 20001])
+def test_distill_of_fp32_logits_far_apart(C, T):
+    """The gradient of classes far below the largest, relative to itself: the exponential is off by 2^-23 for each unit of its exponent, and its constant, which 1 / T and
+    log2(e) are rounded into, by as much again at the most."""
+    g = lib()
+    d = torch.linspace(0, 80, C)
+    Z = (-d * T).reshape(1, C)
+    top, t = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, device="cuda")
+    G, loss = torch.empty(1, C, device="cuda"), torch.empty(1, device="cuda")
+    g.gcn_distill(Z.cuda(), top, t, loss, G, temperature=T)
+    z = Z.double() / T
+    q = torch.softmax(z, 1)
+    # the sum of the row is off by its additions; the first column's gradient is q - 1
+    tol = T * (POWERS + 40 * EPS + 4 * EPS * z.abs()) * q
+    tol[0, 0] += 4 * EPS * T
+    ref = T * q
+    ref[0, 0] -= T
+    check(G, ref, tol, "G")
