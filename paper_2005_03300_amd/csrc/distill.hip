@@ -30,7 +30,9 @@ struct DistillArgs {
 // unit d of the exponent.  In a row's sum, which is 1 at least, that is at most d e^-d 2^-23 of it, less than an fp32 rounding; what is relative to itself is the gradient of a
 // class far below the largest.  (With the lost bits, as exp_for has them for fp32 elements, 232965 x 41 took 34.0 us, without 31.0.)
 __device__ __forceinline__ float power(float x, float high, float c) { return power_of_2((x - high) * c); }
-// e^(x - high) from et = e^((x - high) / T): powers of it at the temperatures 1, 2 and 4 (POWER), else a second exponential.
+// e^(x - high) from et = e^((x - high) / T): itself at the temperature 1, its square at 2 and that one's at 4 (POWER), else a second exponential.  Microseconds at 1, 2, 4 and, with
+// a second one, 3: 4096 x 100,000 in bf16 399, 404, 422, 458 (exponentials of a quarter of the vector rate, twice for each element, beside the memory); 65536 x 1000 in bf16 70, 74, 75, 77;
+// 232965 x 41 in fp32 30.2, 31.3, 31.0, 31.8.  Further whole powers would take as many products as a second exponential takes.
 template <int POWER>
 __device__ __forceinline__ float plain_power(float et, float x, float high) {
     if (POWER == 1) return et;
@@ -256,7 +258,10 @@ static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream
         return launch(l, p, std::integral_constant<int, 0>());
     };
     // The fewest lanes that hold a row with four pieces each: more lanes have less to do between the same number of joins (65536 x 1000 in bf16 with 64 lanes 101 us,
-    // with 32 68; 65536 x 2000 in fp32 with 256 442, with 128 296).  Rows of over 16 KB are read twice; the longer, the more lanes: the rows in work at one
+    // with 32 68; 65536 x 2000 in fp32 with 256 442, with 128 296).  Short rows are rather bound by what a lane does one piece after the other, and by their lists, of which a
+    // lane of few has more: up to 16 pieces eight lanes with two (232965 x 41 in fp32 31.4 us, with four of four 34.8, with eight of four 40.6; x 64 in bf16 39.5, 39.9 and
+    // 55; but x 32 in fp32 25.4 and 24.9 with four of four), up to four pieces four lanes with one (232965 x 16 in fp32 17.6, with eight of two 24.4, in bf16 x 32 19.6 and 32.5).
+    // Rows of over 16 KB are read twice; the longer, the more lanes: the rows in work at one
     // time, as many as workgroups fit, stay in the caches until they are read again (4096 x 100,000 in bf16 with 512 lanes 493 us, with 1024 431).
     const int64_t pieces = (a.C + Elem<T>::E - 1) / Elem<T>::E;
 #define GCN_LANES(L, P) if (pieces <= (int64_t)(L) * (P)) return with(std::integral_constant<int, L>(), std::integral_constant<int, P>())
