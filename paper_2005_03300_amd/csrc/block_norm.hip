@@ -570,17 +570,6 @@ __global__ __launch_bounds__(1024) void k_block_norm_vectors(NormArgs g, int blo
     }
 }
 
-__global__ __launch_bounds__(1024) void k_vector_sums(const float* __restrict__ part, int parts, int64_t count, float* __restrict__ out) {
-    __shared__ float s_sum[16][64];
-    sum_of_parts(blockIdx.x, 1, (int32_t)count, parts, 0, part, 16, s_sum, [&](int, int c, float s) { out[c] = s; });
-}
-
-int vector_sums_launch(const float* part, int parts, int64_t count, float* out, hipStream_t s) {
-    hipLaunchKernelGGL(k_vector_sums, dim3((unsigned)column_sum_groups(count)), dim3(1024), 0, s, part, parts, count, out);
-    GCN_LAUNCH_CHECK();
-    return GCN_OK;
-}
-
 // The fewest lanes that hold a row with E elements each, a workgroup's 1024 with twice as many for longer rows; call(lanes, elements), or call(0, 0) for rows longer than
 // that or shorter than E.
 template <int E, typename F>

@@ -11,25 +11,21 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 
 template <typename T> struct Elem;
 template <> struct Elem<float> {
-    static constexpr int TYPE = GCN_F32, E = 4;                  // E: elements of 16 bytes
+    static constexpr int E = 4;                                  // elements of 16 bytes
     typedef float V __attribute__((ext_vector_type(4)));
     struct __attribute__((packed, aligned(4))) Loose { uint32_t w[4]; };
-    struct __attribute__((packed, aligned(4))) Loose4 { uint32_t w[4]; };   // four elements
 };
 template <> struct Elem<__bf16> {
-    static constexpr int TYPE = GCN_BF16, E = 8;
+    static constexpr int E = 8;
     typedef __bf16 V __attribute__((ext_vector_type(8)));
     struct __attribute__((packed, aligned(2))) Loose { uint32_t w[4]; };
-    struct __attribute__((packed, aligned(2))) Loose4 { uint32_t w[2]; };
 };
 template <> struct Elem<_Float16> {
-    static constexpr int TYPE = GCN_F16, E = 8;
+    static constexpr int E = 8;
     typedef _Float16 V __attribute__((ext_vector_type(8)));
     struct __attribute__((packed, aligned(2))) Loose { uint32_t w[4]; };
-    struct __attribute__((packed, aligned(2))) Loose4 { uint32_t w[2]; };
 };
 template <typename T> using Vec = typename Elem<T>::V;
-template <typename T> using Vec4 = T __attribute__((ext_vector_type(4)));
 
 template <typename T>
 __device__ __forceinline__ Vec<T> load_vec(const T* p) {
@@ -43,14 +39,6 @@ typedef float v4f_loose __attribute__((ext_vector_type(4), aligned(2)));
 template <typename T>
 __device__ __forceinline__ void stream_vec(T* p, Vec<T> v) {       // past the caches
     __builtin_nontemporal_store((v4f_loose)__builtin_bit_cast(v4f, v), reinterpret_cast<v4f_loose*>(p));
-}
-template <typename T>
-__device__ __forceinline__ v4f load4(const T* p) {
-    return __builtin_convertvector(__builtin_bit_cast(Vec4<T>, *reinterpret_cast<const typename Elem<T>::Loose4*>(p)), v4f);
-}
-template <typename T>
-__device__ __forceinline__ void store4(T* p, v4f v) {             // rounds to nearest, ties to even
-    *reinterpret_cast<typename Elem<T>::Loose4*>(p) = __builtin_bit_cast(typename Elem<T>::Loose4, __builtin_convertvector(v, Vec4<T>));
 }
 // The first `count` elements of 16 bytes; the others are zero.
 template <typename T>
@@ -177,8 +165,5 @@ int by_type(int type, const F& f) {
     return f(_Float16());
 }
 inline bool known_type(int type) { return type == GCN_F32 || type == GCN_BF16 || type == GCN_F16; }
-
-// `group`s of 64 results, each the sum of `parts` partial results in a fixed order (see sum_of_parts).
-int vector_sums_launch(const float* part, int parts, int64_t count, float* out, hipStream_t s);
 
 }  // namespace gcn

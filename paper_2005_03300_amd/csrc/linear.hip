@@ -1,6 +1,7 @@
 // A linear layer with what follows it: Y = rho R + act(X W + 1 bias^T), and its gradients, on 32- and 16-bit elements.
 #include "launch_rules.h"
 #include "linear_tile.h"
+#include "sum_parts.h"
 
 namespace gcn {
 
@@ -74,6 +75,12 @@ __global__ __launch_bounds__(256) void k_linear_slope(int64_t n, int32_t N, int6
         if (e < count) part[(int64_t)blockIdx.y * N + c + e] = sum[e];
 }
 
+// The partial results of the shares of the rows, added in order (see sum_of_parts): 64 columns for each workgroup.
+__global__ __launch_bounds__(1024) void k_vector_sums(const float* __restrict__ part, int parts, int32_t count, float* __restrict__ out) {
+    __shared__ float s_sum[16][64];
+    sum_of_parts(blockIdx.x, 1, count, parts, 0, part, 16, s_sum, [&](int, int c, float s) { out[c] = s; });
+}
+
 template <typename T>
 static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho, void* dZ,
                         int64_t lddz, void* dR, int64_t lddr, float* dbias, hipStream_t s) {
@@ -86,7 +93,10 @@ static int slope_launch(int64_t n, int32_t N, const void* Z, int64_t ldz, const 
     hipLaunchKernelGGL(k_linear_slope<T>, dim3((unsigned)across, (unsigned)blocks), dim3(256), 0, s, n, N, per, (const T*)Z, ldz,
                        (const T*)dY, lddy, act, rho, (T*)dZ, lddz, (T*)dR, lddr, (float*)part);
     GCN_LAUNCH_CHECK();
-    if (dbias && blocks > 1) return vector_sums_launch((const float*)part, (int)blocks, N, dbias, s);
+    if (dbias && blocks > 1) {
+        hipLaunchKernelGGL(k_vector_sums, dim3((unsigned)column_sum_groups(N)), dim3(1024), 0, s, (const float*)part, (int)blocks, N, dbias);
+        GCN_LAUNCH_CHECK();
+    }
     return GCN_OK;
 }
 

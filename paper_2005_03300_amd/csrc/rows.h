@@ -9,7 +9,7 @@ namespace gcn {
 
 template <typename T, int L, int P>
 struct Rows {
-    static constexpr int E = Elem<T>::E, THREADS = L <= 64 ? 256 : L, ROWS = THREADS / L, WAVES = L <= 64 ? 1 : L / 64;
+    static constexpr int E = Elem<T>::E, THREADS = L <= 64 ? 256 : L, ROWS = THREADS / L;
     __device__ static int column(int p) { return (p * L + (int)(threadIdx.x % L)) * E; }
     // of the E elements from column c on, how many a row of f has
     __device__ static int there(int c, int32_t f) { return f - c < 0 ? 0 : (f - c > E ? E : f - c); }
