@@ -540,34 +540,32 @@ struct NormVectors {
     const float *scale, *w_post, *b_post;
     float *dscale, *dw_post, *db_post, *dw_pre, *db_pre;
 };
-// Sixteen columns at a time by 64 shares of the workgroups, the shares in order.
+// Sixteen columns by 64 shares of the workgroups, the shares in order.  (A second dimension of workgroups for more columns than one has threads for: a loop over the
+// columns took 1 us longer.)
 __global__ __launch_bounds__(1024) void k_block_norm_vectors(NormArgs g, int blocks, NormVectors v) {
     __shared__ float shares[4][64][17];
-    __shared__ float total[4][16];
     const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
-    for (int64_t c0 = (int64_t)blockIdx.x * 16; c0 < g.f; c0 += (int64_t)gridDim.x * 16) {
-        const int64_t c = c0 + col;
+    const int64_t c = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16 + col;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (g.at[k] >= 0) shares[k][share][col] = c < g.f ? strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, share, 64, blocks) : 0.f;
-        __syncthreads();
-        // (sum, column) of a thread
-        if (threadIdx.x < 64) {
-            float s = 0.f;
-            if (g.at[share] >= 0)
-                for (int w = 0; w < 64; ++w) s += shares[share][w][col];
-            total[share][col] = s;
-        }
-        __syncthreads();
-        if (threadIdx.x < 16 && c < g.f) {                        // (the next columns' totals are written behind another barrier)
-            const float s0 = total[0][col], s1 = total[1][col], sc = v.scale ? v.scale[c] : 1.f;
-            if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], s0, v.b_post ? v.b_post[c] * s1 : 0.f) : s0;
-            if (v.dw_post) v.dw_post[c] = sc * s0;
-            if (v.db_post) v.db_post[c] = sc * s1;
-            if (v.dw_pre) v.dw_pre[c] = total[2][col];
-            if (v.db_pre) v.db_pre[c] = total[3][col];
-        }
+    for (int k = 0; k < 4; ++k)
+        if (g.at[k] >= 0) shares[k][share][col] = c < g.f ? strided_sum(g.part + (int64_t)g.at[k] * g.f + c, (int64_t)g.sums * g.f, share, 64, blocks) : 0.f;
+    __syncthreads();
+    // (sum, column) of a thread; the others are done
+    __shared__ float total[4][16];
+    if (threadIdx.x < 64) {
+        float s = 0.f;
+        if (g.at[share] >= 0)
+            for (int w = 0; w < 64; ++w) s += shares[share][w][col];
+        total[share][col] = s;
     }
+    __syncthreads();
+    if (threadIdx.x >= 16 || c >= g.f) return;
+    const float s0 = total[0][col], s1 = total[1][col], sc = v.scale ? v.scale[c] : 1.f;
+    if (v.dscale) v.dscale[c] = v.w_post ? fmaf(v.w_post[c], s0, v.b_post ? v.b_post[c] * s1 : 0.f) : s0;
+    if (v.dw_post) v.dw_post[c] = sc * s0;
+    if (v.db_post) v.db_post[c] = sc * s1;
+    if (v.dw_pre) v.dw_pre[c] = total[2][col];
+    if (v.db_pre) v.db_pre[c] = total[3][col];
 }
 
 // The fewest lanes that hold a row with E elements each, a workgroup's 1024 with twice as many for longer rows; call(lanes, elements), or call(0, 0) for rows longer than
@@ -641,7 +639,8 @@ static int norm_backward(NormArgs g, const NormVectors& v, hipStream_t s) {
         }
         GCN_LAUNCH_CHECK();
         if (g.sums) {
-            hipLaunchKernelGGL(k_block_norm_vectors, dim3((unsigned)norm_vector_groups(g.f)), dim3(1024), 0, s, g, (int)blocks, v);
+            const LaunchGroups groups = norm_vector_groups(g.f);
+            hipLaunchKernelGGL(k_block_norm_vectors, dim3(groups.x, groups.y), dim3(1024), 0, s, g, (int)blocks, v);
             GCN_LAUNCH_CHECK();
         }
         return GCN_OK;

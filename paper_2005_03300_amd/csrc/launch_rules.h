@@ -91,9 +91,15 @@ inline bool short_copy_pays(int64_t rows, int64_t pitch, int64_t nnz, int64_t ro
 // The widest rows that gcn_linear_* and gcn_block_norm_* take.  A launch has fewer than 2^32 threads along a dimension: that is what bounds the first, whose
 // columns have up to 16 threads each; an index of 32 bits for a column and the elements of a step behind it bounds both.
 constexpr int32_t LINEAR_WIDEST = 1 << 27, NORM_WIDEST = 1 << 26;
-// Workgroups of 1024 threads: for 64 of `count` column sums each; for 16 columns at a time of a norm's vectors, any number of times.
+// Workgroups of 1024 threads: for 64 of `count` column sums each, and for 16 columns each of a norm's vectors, in two dimensions where one has not threads enough.
 constexpr int64_t column_sum_groups(int64_t count) { return (count + 63) / 64; }
-constexpr int64_t norm_vector_groups(int64_t f) { return f < (1 << 20) ? (f + 15) / 16 : (1 << 16); }
+struct LaunchGroups {
+    uint32_t x, y;
+};
+constexpr LaunchGroups norm_vector_groups(int64_t f) {
+    const int64_t groups = (f + 15) / 16, most = 1 << 16;
+    return {(uint32_t)(groups < most ? groups : most), (uint32_t)((groups + most - 1) / most)};
+}
 
 // Shares of n rows for a pass over matrices that is `across` workgroups wide: eight workgroups for each compute unit where there are rows enough for 16 each, in
 // multiples of four rows.  What the shares leave of sums over the rows, a number for each column, stays small: more columns take more workgroups and so fewer shares.

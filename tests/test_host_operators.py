@@ -44,9 +44,9 @@ def test_launches_for_the_widest_rows_are_launchable(tmp_path):
             const int64_t most = (int64_t)1 << 32;
             for (int64_t f : {int64_t(1), int64_t(16), int64_t(17), int64_t(1 << 20) - 1, int64_t(1 << 20), int64_t(1 << 20) + 1, int64_t(NORM_WIDEST) - 16,
                               int64_t(NORM_WIDEST) - 15, int64_t(NORM_WIDEST)}) {
-                const int64_t groups = norm_vector_groups(f);
-                // below the bound every column has a workgroup of its own; from it on a workgroup goes on behind the last one
-                if (groups * 1024 >= most || groups < 1 || (f < (1 << 20) && groups * 16 < f)) return printf("norm vectors of %lld: %lld\\n", (long long)f, (long long)groups), 1;
+                const LaunchGroups g = norm_vector_groups(f);
+                if (g.x < 1 || g.y < 1 || g.x * int64_t(1024) >= most || g.y > 65535 || (int64_t)g.x * g.y * 16 < f)
+                    return printf("norm vectors of %lld: %u x %u\\n", (long long)f, g.x, g.y), 1;
             }
             for (int64_t N : {int64_t(1), int64_t(64), int64_t(65), int64_t(LINEAR_WIDEST)}) {
                 const int64_t groups = column_sum_groups(N);
