@@ -2,9 +2,10 @@
 // q = softmax over all classes of z / T,
 //   loss = 1/m sum over rows [ wt T^2 sum over S of p (log p - log q) - wl log softmax(z)_y ]
 //   G    = 1/m [ wt T (q - p) where S is not empty, + wl (softmax(z) - onehot(y)) where y >= 0 ]
-// A row of up to 16 KB is read once, held in registers in its own type, and its gradient written once: bound by memory and, where rows are short, by the chain of a row
-// (its list, two joins, the list again): 232965 x 41 in fp32 35 us, x 128 55 us (4.3 TB/s).  Longer rows: 4096 x 100,000 in bf16 403 us, 3 x 819 MB from and to
-// memory and caches.
+// A row of up to 16 KB is read once, held in registers in its own type, and its gradient written once: bound by memory and, where rows are short, by the instructions of a row
+// (its list, two joins, the list again; vector instructions are issued in 83 % of the cycles): 232965 x 41 in fp32 35 us, x 128 55 us (4.3 TB/s).  Longer rows: 4096 x 100,000 in bf16
+// 403 us, 3 x 819 MB from and to memory and caches, with vector instructions in 75 % of the cycles.  Double entries are looked for by every entry in the whole list, which long
+// lists feel: 4096 rows of 100,000 with 1500 entries 2.0 ms, without a gradient 0.24.
 #include <type_traits>
 
 #include "rows.h"

@@ -1,4 +1,4 @@
-// A linear layer over few rows: one pass over the weights, whose reading is all the time it takes.
+// A linear layer over few rows: one pass over the weights, whose reading is most of the time it takes.
 #pragma once
 #include "linear_tile.h"
 
@@ -14,7 +14,8 @@ template <typename T, int C, int RT>
 constexpr size_t few_lds() { return (size_t)FEW_WAVES * RT * 16 * (16 * C + 4) * 4; }
 
 // Y's rows are few, so the product is bound by reading W (and by about 4 us of start and end): 4096 x 4096 in bf16 for 16 rows 13.5 us, in fp32 for one row 14.5 us (4.6
-// TB/s), 4096 x 16384 in bf16 26 us (5 TB/s).
+// TB/s), 4096 x 16384 in bf16 26 to 28 us (4.8 to 5 TB/s).  What is left where strips are narrow: a wavefront waits for its two steps before it multiplies them and sends for the next two
+// after, so at 4096 x 4096 in bf16, two bytes to a load, the weights come at 2.5 TB/s.
 // A workgroup has a strip of 16 C columns; its wavefronts take the 4 E values of k of a step in turn, straight from memory into the operands of the matrix unit: a
 // lane loads C neighbouring columns of E rows of W and has with them C fragments of E values of k.  Up to 16 RT rows of X, whose fragments are 16
 // bytes of a row.  The wavefronts' results are added in order in LDS, and what the layer does with them follows.  Neighbouring strips run on the same XCD, since

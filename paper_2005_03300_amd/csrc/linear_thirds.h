@@ -2,7 +2,7 @@
 // what is left, 8 + 8 + 8 bits), and the product of two such sums has nine products of bf16 numbers, which the matrix unit multiplies exactly and adds in fp32.  Three of the
 // nine are left out: m l' and l m', at most 2^-25 of x x' each, and l l', at most 2^-34; together they are up to 2^-24 of it, as the rounding of an fp32 product is, and
 // 2^-27.5 in the root mean square over random mantissas.  The other six take 96 cycles for what the fp32 units
-// take 256 for.  8192 x 8192 x 8192 takes 5.2 ms (210 TFLOP/s; on the fp32 units at most 157, the library's product 151), 232965 x 602 x 128 260 us.
+// take 256 for.  8192 x 8192 x 8192 takes 5.2 ms (210 TFLOP/s; on the fp32 units at most 157, the library's product 151), 232965 x 602 x 128 270 us.
 // Infinities and NaN have no such sum, nor have numbers that round to infinity as bf16: with them m, and with it the result, is NaN; and a finite product of
 // numbers whose h are rounded up can become infinite.  A workgroup that has results that are not finite computes its tile again on the fp32 units, and takes these
 // results from there (and no other, so that none depends on another row's numbers).  Numbers below 2^-100 lose bits of m and l below the smallest bf16 number, 2^-133.
@@ -65,8 +65,9 @@ struct Thirds {
 };
 
 // As k_linear_tile through registers, for any alignment; one stage in LDS (three planes of 32 k: 48 KB of a 128 x 128 tile), the next one in registers, and another
-// workgroup on the compute unit meanwhile.  Bound by the matrix units (96 products of 16 cycles a stage and wavefront) and beside them the vector instructions that
-// split: 22 for four numbers, as many cycles as half of the products take at 128 x 128.  (A look at every number for infinities made them as many: 180 TFLOP/s.)
+// workgroup on the compute unit meanwhile.  Of the compute units' cycles the matrix units are busy in 40 % at 232965 x 602 x 128 (96 products of 16 cycles a stage and wavefront), and
+// vector instructions are issued in 40 %: 22 split four numbers.  (A look at every number for infinities made them as many as the products take: 180 TFLOP/s.)  The second set of
+// results for those that are not finite costs 16 and 18 spilled registers of the 128 x 128 forms whose B lies along n.
 template <int BM, int BN, int WM, int WN, int LA, int LB>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, BK = 32, E = 4;

@@ -360,11 +360,13 @@ __device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[F
 // D = A B for 16-bit elements: BM x BN results of a workgroup of WM x WN wavefronts, 128 bytes of k (64 values) at a time, two such stages in LDS: one is
 // fetched while the other is multiplied.  A wavefront's results are the transpose of what the matrix unit is given (B's columns as its rows), so that a lane
 // holds four neighbouring columns of one row.
-// Bound by the matrix units for large products: 16384 x 4096 x 4096 in bf16 435 to 475 us (1.16 to 1.27 PFLOP/s) in each of the three directions.  A 256 x 256 tile reads
+// Large products: 16384 x 4096 x 4096 in bf16 435 to 475 us (1.16 to 1.27 PFLOP/s, the library's rate) in each of the three directions; the matrix units are busy in 47 % of the
+// cycles, epilogue included, in the library's product of 8192 x 8192 x 8192 in 73 % at a lower clock.  A 256 x 256 tile reads
 // each operand half as often from L2 as 128 x 128 and LDS as often per product as its wavefronts' 128 x 64 results ask for (the units take 2048 cycles of a stage, LDS
 // 1536); 128 x 128 has two workgroups on a compute unit, so that one's end overlaps the other's products (1.05 PFLOP/s), and 64 x 64 is for results too small to fill
 // the chip otherwise.  128 bytes of k are a cache line of a row, and one barrier for 64 (256 x 256) products of a wavefront.
-// DIRECT: rows of both operands at 16-byte addresses in whole pieces: memory to LDS without registers.
+// DIRECT: rows of both operands at 16-byte addresses in whole pieces: memory to LDS without registers.  (Through registers the 256 x 256 tile spills 23 of them forward and
+// 60 for dW.)
 template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT>
 __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, E = Elem<T>::E, BK = 8 * E;
