@@ -325,7 +325,8 @@ int gcn_block_norm_backward(int64_t n, int32_t f, int type, int kind, const void
  * (host value, for instance the number of rows with a list or a label).  loss: fp32, written.  G: n x C or NULL; it may be Z.
  * Logits of -inf are classes that cannot be (q = 0); a row of them alone has no softmax, and gives NaN if it has a list or a label.  Exponentials
  * and row sums are fp32, an exponential off by 2^-23 of itself for each unit of its exponent (the logit's distance from the row's largest over T), which its row's sum does
- * not feel; the loss is added up in fp64 in a fixed order.  1 <= k <= min(C, GCN_DISTILL_MOST); C up to 2^30 (RANGE).
+ * not feel; the loss is added up in fp64 in a fixed order.  1 <= k <= min(C, GCN_DISTILL_MOST); C up to 2^30, temperatures from 2^-126 on (RANGE).  A row's sum over the list is
+ * of fp32 terms: at high temperatures, where it is small, T^2 times its rounding is what the loss is off by, a few 2^-24 T^2.
  * Rows up to 16 KB are read once.
  * ----------------------------------------------------------------------------------------- */
 int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_t ldz, int32_t k, const int32_t* top, int64_t ldtop,

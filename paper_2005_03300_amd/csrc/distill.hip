@@ -22,7 +22,7 @@ struct DistillArgs {
     const int32_t* top = nullptr;
     const void* t = nullptr;
     const int32_t* labels = nullptr;
-    float inv_T = 1, wt = 0, wl = 0;          // wt, wl: of the loss
+    float inv_T = 1, wt = 0, wl = 0;          // wt, wl: of the loss over T, which joins 1 / m: w_teacher T, w_label / T
     float gt = 0, gl = 0;                     // of the gradient: grad_scale / m times wt T and wl
     double* part = nullptr;
 };
@@ -230,9 +230,9 @@ __global__ __launch_bounds__((Rows<T, L, P>::THREADS), P == 0 ? 8 : 4) void k_di
     }
 }
 
-__global__ __launch_bounds__(256) void k_distill_loss(int64_t parts, const double* __restrict__ part, double inv_m, float* __restrict__ loss) {
+__global__ __launch_bounds__(256) void k_distill_loss(int64_t parts, const double* __restrict__ part, double scale, float* __restrict__ loss) {
     __shared__ double s[256];
-    sum_of_losses(part, parts, inv_m, loss, s);
+    sum_of_losses(part, parts, scale, loss, s);
 }
 
 template <typename T>
@@ -248,7 +248,7 @@ static int distill_of(DistillArgs a, int64_t m, float T_, float* loss, hipStream
         a.part = (double*)part;
         launch_lds<k_distill<T, L, P, decltype(power)::value>>(dim3((unsigned)blocks), R::THREADS, (size_t)R::ROWS * (a.k + 1) * 12, s, a);
         GCN_LAUNCH_CHECK();
-        hipLaunchKernelGGL(k_distill_loss, dim3(1), dim3(256), 0, s, (int64_t)blocks, (const double*)part, 1.0 / (double)m, loss);
+        hipLaunchKernelGGL(k_distill_loss, dim3(1), dim3(256), 0, s, (int64_t)blocks, (const double*)part, (double)T_ / (double)m, loss);
         GCN_LAUNCH_CHECK();
         return GCN_OK;
     };
@@ -287,6 +287,7 @@ extern "C" int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_
     if (k <= 0 || k > C || k > GCN_DISTILL_MOST) return fail(GCN_ERR_BADARG, "%s: a list has 1 to %d entries, and no more than there are classes", who, GCN_DISTILL_MOST);
     if (ldz < C || ldtop < k || ldt < k || (G && ldg < C)) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
     if (!(temperature > 0.f) || !(temperature < INFINITY)) return fail(GCN_ERR_BADARG, "%s: the temperature must be positive", who);
+    if (temperature < 0x1p-126f) return fail(GCN_ERR_RANGE, "%s: temperatures begin at 2^-126", who);
     if (m <= 0) return fail(GCN_ERR_BADARG, "%s: m must be positive", who);
     const size_t b = elem_bytes(type);
     const Span z(Z, n, C, ldz, b), g(G, n, C, ldg, b), at(top, n, k, ldtop, 4), tt(t, n, k, ldt, b), y(labels, 1, n, n, 4), l(loss, 1, 1, 1, 4);
@@ -296,8 +297,8 @@ extern "C" int gcn_distill(int64_t n, int32_t C, int type, const void* Z, int64_
     a.n = n; a.C = C; a.k = w_teacher != 0.f ? k : 0; a.Z = Z; a.ldz = ldz; a.G = G; a.ldg = ldg; a.top = top; a.ldtop = ldtop; a.t = t; a.ldt = ldt;
     a.labels = w_label != 0.f ? labels : nullptr;                 // (a part of weight 0 is none, whatever it is: not multiplied away)
     a.inv_T = 1.f / temperature;
-    a.wt = w_teacher * temperature * temperature;
-    a.wl = w_label;
+    a.wt = w_teacher * temperature;                               // (T^2 in fp32 is 0 below 2^-75, and infinite from 2^64 on)
+    a.wl = w_label / temperature;
     const double scale = (double)grad_scale / (double)m;
     a.gt = (float)(scale * w_teacher * temperature);
     a.gl = (float)(scale * w_label);

@@ -335,3 +335,29 @@ def test_distill_of_fp32_logits_far_apart(C, T):
     ref = T * q
     ref[0, 0] -= T
     check(G, ref, tol, "G")
+
+
+# ---- temperatures ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("T", [2.0 ** -126, 1e-25, 1e-12, 1e12])
+def test_distill_at_the_ends_of_the_temperatures(T):
+    """One entry, one below the row's largest logit of two: the loss is T^2 log(1 + e^(1/T)), or T at low temperatures, and T (q - p) the gradient."""
+    g = lib()
+    Z, t = torch.tensor([[0.0, 1.0]], device="cuda"), torch.zeros(1, 1, device="cuda")
+    top = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    G, loss = torch.empty(1, 2, device="cuda"), torch.empty(1, device="cuda")
+    T = float(torch.tensor(T))                                 # as the call takes it
+    g.gcn_distill(Z, top, t, loss, G, temperature=T)
+    low = 1 / T > 80
+    want = T if low else T * T * math.log1p(math.exp(1 / T))
+    assert abs(float(loss) - want) <= 8 * EPS * want
+    q = 1.0 if low else 1 / (1 + math.exp(-1 / T))
+    for got, ref in zip(G[0].tolist(), (-T * q, T * q)):
+        assert abs(got - ref) <= 16 * EPS * T + 2.0 ** -149
+
+
+def test_distill_refuses_temperatures_without_an_inverse():
+    g = lib()
+    Z, t, loss = torch.zeros(1, 2, device="cuda"), torch.zeros(1, 1, device="cuda"), torch.zeros(1, device="cuda")
+    top = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    with pytest.raises(g.GcnError, match="temperatures"):
+        g.gcn_distill(Z, top, t, loss, temperature=2.0 ** -140)
