@@ -9,7 +9,7 @@
  * Conventions for every call
  *   - Every pointer named "device" is HIP device memory on the current device; "host" is host
  *     memory.  Dense matrices are row-major, with a leading dimension in elements: fp32, and in the calls that take an
- *     element type (gcn_linear_*, gcn_block_norm_*, gcn_distill) of that type.
+ *     element type (gcn_linear_*, gcn_gated_*, gcn_checkpoint_*, gcn_linear4_*, gcn_block_norm_*, gcn_distill) of that type.
  *     In these calls operands that may not overlap may have no element in common; matrices whose rows take turns in one buffer
  *     (halves of n x 2f) have none, an output beside an input among them.
  *   - Dense buffers are owned by the caller; the library neither frees nor keeps them after the
@@ -26,7 +26,7 @@
  *   - A matrix that gcn_csr_create symmetrised and did not normalise by rows equals its transpose bit by bit: it is
  *     stored once, and gcn_csr_arrays gives the same arrays for both.
  *   - Library-owned scratch exists only for the stand-alone gcn_gemm (ta = 1), gcn_softmax_nll*, the gradients of
- *     gcn_layer_backward, gcn_linear_* , gcn_block_norm_backward and gcn_distill: a buffer per (device, stream), grown on demand by the first call that needs more (an
+ *     gcn_layer_backward, gcn_linear_*, gcn_gated_*, gcn_checkpoint_linear_backward, gcn_linear4_forward, gcn_block_norm_backward and gcn_distill: a buffer per (device, stream), grown on demand by the first call that needs more (an
  *     allocation), never shared between streams, nor between calls that threads make on one stream at the same time: these get
  *     buffers of their own.  gcn_scratch_release frees all of them.  The epoch calls keep these partial sums in the caller's
  *     workspace instead.
@@ -73,10 +73,10 @@ extern "C" {
 
 #define GCN_ACT_NONE 0
 #define GCN_ACT_RELU 1
-#define GCN_ACT_GELU 2 /* z/2 (1 + erf(z / sqrt 2)); gcn_linear_* only, as the next */
+#define GCN_ACT_GELU 2 /* z/2 (1 + erf(z / sqrt 2)); gcn_linear_*, gcn_gated_*, gcn_checkpoint_linear_backward and gcn_linear4_forward only, as the next */
 #define GCN_ACT_SILU 3 /* z / (1 + exp(-z)) */
 
-/* element types of gcn_linear_*, gcn_block_norm_* and gcn_distill; sums, statistics and vectors are fp32 with each of them */
+/* element types of gcn_linear_*, gcn_gated_*, gcn_checkpoint_*, gcn_linear4_*, gcn_block_norm_* and gcn_distill; sums, statistics and vectors are fp32 with each of them */
 #define GCN_F32 0
 #define GCN_BF16 1
 #define GCN_F16 2
@@ -84,6 +84,8 @@ extern "C" {
 /* norms of gcn_block_norm_* */
 #define GCN_NORM_RMS 0   /* x / sqrt(mean(x^2) + eps) */
 #define GCN_NORM_LAYER 1 /* (x - mean(x)) / sqrt(var(x) + eps), var the mean squared deviation */
+
+#define GCN_CHECKPOINT_GROUP 64 /* neighbours of a row that share a scale in gcn_checkpoint_* */
 
 #define GCN_DISTILL_MOST 4096 /* entries of a teacher's list in gcn_distill */
 
@@ -285,6 +287,64 @@ int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const 
                         int64_t ldw, const void* Z, int64_t ldz, const void* dY, int64_t lddy, int act, float rho,
                         void* dZ, int64_t lddz, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias, void* dR,
                         int64_t lddr, void* stream);
+
+/* -------------------------------------------------------------------------------------------
+ * A gated block over the rows of X: both projections, the activation and their product.
+ *   Z = X W + 1 bias^T  with W: f_in x 2 f_out (the gate's columns, then the others),  H = act(Z[:, :f_out]) (Hadamard) Z[:, f_out:]
+ * X: n x f_in, H: n x f_out, Z: n x 2 f_out, of element type `type`; bias: fp32[2 f_out] or NULL; Z (what backward needs) may be NULL.  Elements, sums, roundings, activations, alignment
+ * and reproducibility as gcn_linear_forward; f_in up to 2^27, f_out up to 2^26 (RANGE).  No output may overlap an input or another output.
+ * backward, with dL/dH given as dH:
+ *   dZ = [dH (Hadamard) Z[:, f_out:] (Hadamard) act'(Z[:, :f_out]),  dH (Hadamard) act(Z[:, :f_out])],  dX = dZ W^T,  dW = X^T dZ,
+ *   dbias = column sums of dZ (before it is rounded),  H as above (which then need not be kept for the next layer's dW)
+ * Any of dX, dW, dbias, H may be NULL, and is then not computed; X is read for dW and W for dX only.  dZ (n x 2 f_out) is workspace that the call fills, needed for dX and dW; it is rounded
+ * to the element type, as in gcn_linear_backward.  dZ may be Z, and H may be dH (same address and leading dimension).
+ * x_scales, z_scales: NULL, or X (Z) is a checkpoint, X the codes (int8, ldx apart) and x_scales their scales (see below; Z's groups are of its rows of 2 f_out).
+ * ----------------------------------------------------------------------------------------- */
+int gcn_gated_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                      const float* bias, int act, void* Z, int64_t ldz, void* H, int64_t ldh, void* stream);
+int gcn_gated_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const uint16_t* x_scales, int64_t ldxs,
+                       const void* W, int64_t ldw, const void* Z, int64_t ldz, const uint16_t* z_scales, int64_t ldzs, const void* dH,
+                       int64_t lddh, int act, void* dZ, int64_t lddz, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias, void* H,
+                       int64_t ldh, void* stream);
+
+/* -------------------------------------------------------------------------------------------
+ * Checkpoints: activations held in 8 bits between the forward and the backward pass, 1.03 bytes an element.  Each GCN_CHECKPOINT_GROUP neighbours of a row (the last group of a row may be shorter) share a
+ * scale s, the smallest bf16 number (2^-126 at least) with 127 s >= |x| for all of them; x is held as the whole number c nearest to x / s (of two as near the even one),
+ * off by s / 2 at most.  It stands for s c, rounded to the element type.  A group with an infinity or NaN has the scale NaN, and stands for NaN.
+ * (In fp16 the largest scale is 512, in the others 2^121: numbers beyond 65024, or 127 2^121, are held as that.)
+ * codes: int8, n x f, ldc >= f apart; scales: bf16, n x ceil(f / GCN_CHECKPOINT_GROUP), lds apart; X: n x f elements; any alignment; widths up to 2^27 (RANGE).
+ * pack writes codes and scales, unpack X; no output may overlap an input or another output.
+ * gcn_checkpoint_linear_backward: gcn_linear_backward from checkpoints.  x_scales, z_scales: NULL, or X (Z) is a checkpoint, X the codes (int8, ldx apart) and x_scales their scales; the rest as
+ * there, except that dZ may not be the codes.
+ * ----------------------------------------------------------------------------------------- */
+int gcn_checkpoint_pack(int64_t n, int32_t f, int type, const void* X, int64_t ldx, int8_t* codes, int64_t ldc, uint16_t* scales, int64_t lds,
+                        void* stream);
+int gcn_checkpoint_unpack(int64_t n, int32_t f, int type, const int8_t* codes, int64_t ldc, const uint16_t* scales, int64_t lds, void* X,
+                          int64_t ldx, void* stream);
+int gcn_checkpoint_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const uint16_t* x_scales,
+                                   int64_t ldxs, const void* W, int64_t ldw, const void* Z, int64_t ldz, const uint16_t* z_scales, int64_t ldzs,
+                                   const void* dY, int64_t lddy, int act, float rho, void* dZ, int64_t lddz, void* dX, int64_t lddx, void* dW,
+                                   int64_t lddw, float* dbias, void* dR, int64_t lddr, void* stream);
+
+/* -------------------------------------------------------------------------------------------
+ * A linear layer or a gated block whose weights are held in 4 bits, for answering:
+ *   Y = rho R + act(X W + 1 bias^T),  or with `gated`  Y = rho R + act(Z[:, :f_out]) (Hadamard) Z[:, f_out:],  Z = X W + 1 bias^T of 2 f_out columns
+ * Each `group` (32, 64 or 128) neighbours of a column of W (the last group may be shorter) share a scale s, the smallest bf16 number (2^-126 at least) with 6 s >= |w| for all of them; w is held as the
+ * nearest of +-s {0, 1/2, 1, 3/2, 2, 3, 4, 6} (of two as near the one with the even place in this list), off by s at most.  Its code has the sign in bit 3, the place in bits 0 to 2.
+ * A group with an infinity or NaN has the scale NaN, and stands for NaN.  (The largest scale is 1.328125 2^13 in fp16, where weights beyond 65280 are held as that, else 1.328125 2^125.)
+ * Q: words, ceil(f_in / 8) x cols, ldq apart; word (j, c) holds the codes of W[8 j .. 8 j + 7, c], the first in its lowest bits; those beyond f_in are 0.  S: bf16, ceil(f_in / group) x cols, lds
+ * apart.  cols: the columns of W, f_out or, gated, 2 f_out; a block of columns of Q and S at the same leading dimensions holds that block of columns of W.
+ * pack: W, f_in x cols of element type `type`, to Q and S; unpack: back, each weight rounded to the type; no output may overlap an input or another output.
+ * forward: the weights enter the products as they are held, without a rounding: sums over a group in fp32, times the scale, added in fp32 in a fixed order.  bias: fp32[cols] or NULL; R may be
+ * NULL; Y may be R (same address and leading dimension) and may overlap no other input.  Roundings, activations and alignment as gcn_linear_forward; f_in and cols up to 2^27 (RANGE).
+ * ----------------------------------------------------------------------------------------- */
+int gcn_linear4_pack(int32_t f_in, int32_t cols, int type, const void* W, int64_t ldw, int group, uint32_t* Q, int64_t ldq, uint16_t* S,
+                     int64_t lds, void* stream);
+int gcn_linear4_unpack(int32_t f_in, int32_t cols, int type, const uint32_t* Q, int64_t ldq, const uint16_t* S, int64_t lds, int group, void* W,
+                       int64_t ldw, void* stream);
+int gcn_linear4_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const uint32_t* Q, int64_t ldq,
+                        const uint16_t* S, int64_t lds, int group, int gated, const float* bias, int act, const void* R, int64_t ldr, float rho,
+                        void* Y, int64_t ldy, void* stream);
 
 /* -------------------------------------------------------------------------------------------
  * The norms around a block of a residual network, with the block's gate and residual scale, in one pass:

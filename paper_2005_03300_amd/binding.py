@@ -15,6 +15,7 @@ ORDER_AUTO, ORDER_GEMM_FIRST, ORDER_SPMM_FIRST = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_SILU = 0, 1, 2, 3
 F32, BF16, F16 = 0, 1, 2
 NORM_RMS, NORM_LAYER = 0, 1
+CHECKPOINT_GROUP = 64
 CFG_SPMM_ALGO, CFG_TIMING, CFG_SPMM_BLOCKS, CFG_SWEEP_HEAVY, CFG_SWEEP_WAVES, CFG_PATTERN_SPMM, CFG_HUB_MB, CFG_HUB_DMIN, CFG_HUB_BLOCK_COLS, CFG_SPLIT_LDS_KB, CFG_FUSED_LAST_LAYER = 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11
 
 _lib = None
@@ -70,15 +71,24 @@ def lib():
         L.gcn_epoch_preaggregated.argtypes = L.gcn_epoch_masked.argtypes
         L.gcn_linear_forward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i, p, i64, f32, p, i64, p, i64, p]
         L.gcn_linear_backward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i64, p, i64, i, f32, p, i64, p, i64, p, i64, p, p, i64, p]
+        L.gcn_gated_forward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i, p, i64, p, i64, p]
+        L.gcn_gated_backward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i64, p, i64, p, i64, p, i64, i, p, i64, p, i64, p, i64, p, p, i64, p]
+        L.gcn_checkpoint_pack.argtypes = [i64, i32, i, p, i64, p, i64, p, i64, p]
+        L.gcn_checkpoint_unpack.argtypes = L.gcn_checkpoint_pack.argtypes
+        L.gcn_checkpoint_linear_backward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i64, p, i64, p, i64, p, i64, i, f32, p, i64, p, i64, p, i64, p,
+                                                     p, i64, p]
+        L.gcn_linear4_pack.argtypes = [i32, i32, i, p, i64, i, p, i64, p, i64, p]
+        L.gcn_linear4_unpack.argtypes = [i32, i32, i, p, i64, p, i64, i, p, i64, p]
+        L.gcn_linear4_forward.argtypes = [i64, i32, i32, i, p, i64, p, i64, p, i64, i, i, p, i, p, i64, f32, p, i64, p]
         L.gcn_block_norm_forward.argtypes = [i64, i32, i, i, f32, p, i64, p, i64, p, i32, i64, p, p, p, p, p, p, i64, p, i64, p, p]
         L.gcn_block_norm_backward.argtypes = [i64, i32, i, i, p, i64, p, i32, i64, p, p, p, p, p, i64, p, p, i64, p, i64, p, i64, p,
                                               i64, p, i64, p, p, p, p, p, p]
         L.gcn_distill.argtypes = [i64, i32, i, p, i64, i32, p, i64, p, i64, p, f32, f32, f32, i64, f32, p, p, i64, p]
-        global _raw_stream, _device, _f32, _i32, _types
+        global _raw_stream, _device, _f32, _i32, _i8, _bf16, _types
         import torch
         _types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
         _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-        _f32, _i32 = torch.float32, torch.int32
+        _f32, _i32, _i8, _bf16 = torch.float32, torch.int32, torch.int8, torch.bfloat16
         _lib = L
     return _lib
 
@@ -373,6 +383,124 @@ def gcn_linear_backward(X, W, Z, dY, dZ=None, dX=None, dW=None, dbias=None, act:
                                *_mat(dR, out, dt), _raw_stream(_device()))
     if rc:
         _check(rc)
+
+
+def _kept(t, shape, dtype):
+    """Address and leading dimension of a matrix that was kept, and of its scales: of a tensor (no scales), or of a checkpoint, the pair of its codes
+    and scales."""
+    if not isinstance(t, tuple):
+        return *_mat(t, shape, dtype), 0, 0
+    codes, scales = t
+    return *_mat(codes, shape, _i8), *_mat(scales, (shape[0], -(-shape[1] // CHECKPOINT_GROUP)), _bf16)
+
+
+def gcn_gated_forward(X, W, H, bias=None, act: int = ACT_SILU, Z=None):
+    """H = act(Z[:, :m]) Z[:, m:] with Z = X W + 1 bias^T of 2 m columns, which Z receives."""
+    L = _lib or lib()
+    dt, out = X.dtype, H.shape
+    n, f_in = X.shape
+    m = out[1]
+    both = (n, 2 * m)
+    rc = L.gcn_gated_forward(n, f_in, m, _type_of(dt), *_mat(X, (n, f_in), dt), *_mat(W, (f_in, 2 * m), dt), _vec(bias, (2 * m,)), act,
+                             *_mat(Z, both, dt), *_mat(H, (n, m), dt), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+    return H
+
+
+def gcn_gated_backward(X, W, Z, dH, dZ=None, dX=None, dW=None, dbias=None, act: int = ACT_SILU, H=None):
+    """The gradients that are given a place, and H again; dZ is workspace of the size of Z.  X and Z: tensors or checkpoints (pairs of codes and
+    scales).  X may be None without dW, W without dX."""
+    L = _lib or lib()
+    dt, out = dH.dtype, dH.shape
+    n, m = out
+    both = (n, 2 * m)
+    f_in = (X[0] if isinstance(X, tuple) else X).shape[1] if X is not None else W.shape[0] if W is not None else 1
+    rows, weights = (n, f_in), (f_in, 2 * m)
+    rc = L.gcn_gated_backward(n, f_in, m, _type_of(dt), *_kept(X, rows, dt), *_mat(W, weights, dt), *_kept(Z, both, dt), *_mat(dH, out, dt), act,
+                              *_mat(dZ, both, dt), *_mat(dX, rows, dt), *_mat(dW, weights, dt), _vec(dbias, (2 * m,)), *_mat(H, out, dt),
+                              _raw_stream(_device()))
+    if rc:
+        _check(rc)
+
+
+def gcn_checkpoint_pack(X, codes, scales):
+    """X in 8 bits: its codes (int8, as many) and scales (bf16, one for CHECKPOINT_GROUP neighbours of a row)."""
+    L = _lib or lib()
+    dt, shape = X.dtype, X.shape
+    n, f = shape
+    rc = L.gcn_checkpoint_pack(n, f, _type_of(dt), *_mat(X, shape, dt), *_kept((codes, scales), shape, dt), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+    return codes, scales
+
+
+def gcn_checkpoint_unpack(codes, scales, X):
+    """The matrix that a checkpoint stands for."""
+    L = _lib or lib()
+    dt, shape = X.dtype, X.shape
+    n, f = shape
+    rc = L.gcn_checkpoint_unpack(n, f, _type_of(dt), *_kept((codes, scales), shape, dt), *_mat(X, shape, dt), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+    return X
+
+
+def gcn_checkpoint_linear_backward(X, W, Z, dY, dZ=None, dX=None, dW=None, dbias=None, act: int = ACT_NONE, dR=None, rho: float = 1.0):
+    """gcn_linear_backward whose X and Z may each be a checkpoint (the pair of its codes and scales)."""
+    L = _lib or lib()
+    dt, out = dY.dtype, dY.shape
+    n, f_out = out
+    f_in = (X[0] if isinstance(X, tuple) else X).shape[1] if X is not None else W.shape[0] if W is not None else 1
+    rows, weights = (n, f_in), (f_in, f_out)
+    rc = L.gcn_checkpoint_linear_backward(n, f_in, f_out, _type_of(dt), *_kept(X, rows, dt), *_mat(W, weights, dt), *_kept(Z, out, dt),
+                                          *_mat(dY, out, dt), act, rho, *_mat(dZ, out, dt), *_mat(dX, rows, dt), *_mat(dW, weights, dt),
+                                          _vec(dbias, (f_out,)), *_mat(dR, out, dt), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+
+
+def _weights4(Q, S, f_in, cols, group):
+    return *_mat(Q, (-(-f_in // 8), cols), _i32), *_mat(S, (-(-f_in // group), cols), _bf16)
+
+
+def gcn_linear4_pack(W, Q, S, group: int = 64):
+    """W in 4 bits: eight codes of a column in each word of Q (int32), a scale for `group` neighbours of a column in S (bf16)."""
+    L = _lib or lib()
+    dt, shape = W.dtype, W.shape
+    f_in, cols = shape
+    assert group > 0
+    rc = L.gcn_linear4_pack(f_in, cols, _type_of(dt), *_mat(W, shape, dt), group, *_weights4(Q, S, f_in, cols, group), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+    return Q, S
+
+
+def gcn_linear4_unpack(Q, S, W, group: int = 64):
+    """The weights that Q and S stand for."""
+    L = _lib or lib()
+    dt, shape = W.dtype, W.shape
+    f_in, cols = shape
+    assert group > 0
+    rc = L.gcn_linear4_unpack(f_in, cols, _type_of(dt), *_weights4(Q, S, f_in, cols, group), group, *_mat(W, shape, dt), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+    return W
+
+
+def gcn_linear4_forward(X, Q, S, Y, group: int = 64, bias=None, act: int = ACT_NONE, R=None, rho: float = 1.0, gated: bool = False):
+    """Y = rho R + act(X W + 1 bias^T), or with `gated` the gated block, W held in 4 bits by Q and S."""
+    L = _lib or lib()
+    dt = X.dtype
+    n, f_in = X.shape
+    f_out = Y.shape[1]
+    cols, out = 2 * f_out if gated else f_out, (n, f_out)
+    assert group > 0
+    rc = L.gcn_linear4_forward(n, f_in, f_out, _type_of(dt), *_mat(X, (n, f_in), dt), *_weights4(Q, S, f_in, cols, group), group, 1 if gated else 0,
+                               _vec(bias, (cols,)), act, *_mat(R, out, dt), rho, *_mat(Y, out, dt), _raw_stream(_device()))
+    if rc:
+        _check(rc)
+    return Y
 
 
 def gcn_block_norm_forward(X, U=None, Xout=None, H=None, w_pre=None, b_pre=None, A=None, scale=None, w_post=None, b_post=None,

@@ -1,0 +1,185 @@
+// Checkpoints of activations in 8 bits: stored, restored, and read by the backward pass of a linear layer.
+#include "slope.h"
+
+namespace gcn {
+
+// The largest of the bits of L lanes' numbers without their signs (NaN and infinities are the largest).
+template <int L>
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {
+    auto with = [&](float p) {
+        const uint32_t o = __builtin_bit_cast(uint32_t, p);
+        v = v > o ? v : o;
+    };
+    with(partner<1>(__builtin_bit_cast(float, v)));
+    with(partner<2>(__builtin_bit_cast(float, v)));
+    with(partner<4>(__builtin_bit_cast(float, v)));
+    if constexpr (L == 16) with(partner<8>(__builtin_bit_cast(float, v)));
+    return v;
+}
+
+// 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.
+template <typename T>
+__global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* C, int64_t ldc, uint16_t* S, int64_t lds) {
+    constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E;
+    const int64_t groups = groups_of(f, CHECKPOINT_GROUP), all = n * groups;
+    for (int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L; t < all; t += (int64_t)gridDim.x * (256 / L)) {
+        const int64_t i = t / groups, g = t % groups, c = g * CHECKPOINT_GROUP + (int)(threadIdx.x % L) * E;
+        const int count = f - c < 0 ? 0 : f - c < E ? (int)(f - c) : E;
+        float v[E];
+        to_floats<T>(count > 0 ? load_vec_part(X + i * ldx + c, count) : Vec<T>{}, v);
+        uint32_t most = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
+            most = most > b ? most : b;
+        }
+        const uint32_t bits = scale_of<T>(most_of_lanes<L>(most), CHECKPOINT_TOP);
+        const float s = scale_value(bits), inv = inverse(s);
+        uint32_t code[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) code[e] = checkpoint_code<T>(v[e], s, inv) & 255u;
+        int8_t* const to = C + i * ldc + c;
+        if (count == E) {
+            LooseCodes<E> x;
+#pragma unroll
+            for (int w = 0; w < E / 4; ++w) x.w[w] = code[4 * w] | code[4 * w + 1] << 8 | code[4 * w + 2] << 16 | code[4 * w + 3] << 24;
+            *reinterpret_cast<LooseCodes<E>*>(to) = x;
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e < count) to[e] = (int8_t)code[e];
+        }
+        if (threadIdx.x % L == 0) S[i * lds + g] = (uint16_t)bits;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f, const int8_t* C, int64_t ldc, const uint16_t* S, int64_t lds, T* X, int64_t ldx) {
+    constexpr int E = Elem<T>::E;
+    const int64_t pieces = groups_of(f, E), all = n * pieces;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all; t += (int64_t)gridDim.x * 256) {
+        const int64_t i = t / pieces, c = t % pieces * E;
+        const Codes<E> q = load_codes<E>(C + i * ldc, c, f);
+        const float s = scale_value(S[i * lds + c / CHECKPOINT_GROUP]);
+        float v[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = s * code_value<E>(q, e);
+        store_vec_part(X + i * ldx + c, from_floats<T>(v), f - c < E ? (int)(f - c) : E);
+    }
+}
+
+static unsigned passes(int64_t items, int64_t each) {             // workgroups of a pass over `items`, `each` at a time for one
+    const int64_t blocks = (items + each - 1) / each, most = 32 * (int64_t)device_info().cus;
+    return (unsigned)(blocks < most ? blocks : most);
+}
+
+template <typename T>
+static int unpack_launch(int64_t n, int32_t f, const Kept& k, void* X, int64_t ldx, hipStream_t s) {
+    hipLaunchKernelGGL(k_checkpoint_unpack<T>, dim3(passes(n * groups_of(f, Elem<T>::E), 256)), dim3(256), 0, s, n, f, (const int8_t*)k.p, k.ld, k.scales, k.lds, (T*)X, ldx);
+    GCN_LAUNCH_CHECK();
+    return GCN_OK;
+}
+
+int back_products(int type, const BackProducts& b, hipStream_t s) {
+    return by_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        TileArgs a;
+        if (b.dX) {
+            a.A = b.G; a.lda = b.ldg; a.B = b.W; a.ldb = b.ldw; a.M = b.n; a.N = b.f_in; a.K = b.cols; a.Y = b.dX; a.ldy = b.lddx;
+            GCN_TRY(linear_dx_of<T>(a, s));
+        }
+        if (b.dW) {
+            const void* X = b.X.p;
+            int64_t ldx = b.X.ld;
+            ScratchLease lease;
+            if (b.X.scales) {
+                void* p = nullptr;
+                ldx = groups_of(b.f_in, Elem<T>::E) * Elem<T>::E;
+                GCN_TRY(lease.get(&p, (size_t)b.n * ldx * sizeof(T), s));
+                GCN_TRY(unpack_launch<T>(b.n, b.f_in, b.X, p, ldx, s));
+                X = p;
+            }
+            a.A = X; a.lda = ldx; a.B = b.G; a.ldb = b.ldg; a.M = b.f_in; a.N = b.cols; a.K = b.n; a.Y = b.dW; a.ldy = b.lddw;
+            GCN_TRY(linear_dw_of<T>(a, s));
+        }
+        return GCN_OK;
+    });
+}
+
+}  // namespace gcn
+
+using namespace gcn;
+
+static int check_pack(const char* who, int64_t n, int32_t f, int type, const void* X, int64_t ldx, const Kept& k) {
+    if (!X || !k.p || !k.scales) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
+    if (n <= 0 || f <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (f > LINEAR_WIDEST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
+    if (ldx < f || k.ld < f || k.lds < groups_of(f, CHECKPOINT_GROUP)) return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    const Span x(X, n, f, ldx, elem_bytes(type)), c = span_of(k, n, f, 1), s = scales_of(k, n, f);
+    if (x.meets(c) || x.meets(s) || c.meets(s)) return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    return GCN_OK;
+}
+
+extern "C" int gcn_checkpoint_pack(int64_t n, int32_t f, int type, const void* X, int64_t ldx, int8_t* codes, int64_t ldc, uint16_t* scales, int64_t lds, void* stream) {
+    GCN_TRY(check_pack("gcn_checkpoint_pack", n, f, type, X, ldx, {codes, ldc, scales, lds}));
+    return by_type(type, [&](auto t) -> int {
+        using T = decltype(t);
+        hipLaunchKernelGGL(k_checkpoint_pack<T>, dim3(passes(n * groups_of(f, CHECKPOINT_GROUP), 256 / (CHECKPOINT_GROUP / Elem<T>::E))), dim3(256), 0, (hipStream_t)stream, n, f,
+                           (const T*)X, ldx, codes, ldc, scales, lds);
+        GCN_LAUNCH_CHECK();
+        return GCN_OK;
+    });
+}
+
+extern "C" int gcn_checkpoint_unpack(int64_t n, int32_t f, int type, const int8_t* codes, int64_t ldc, const uint16_t* scales, int64_t lds, void* X, int64_t ldx, void* stream) {
+    const Kept k{codes, ldc, scales, lds};
+    GCN_TRY(check_pack("gcn_checkpoint_unpack", n, f, type, X, ldx, k));
+    return by_type(type, [&](auto t) { return unpack_launch<decltype(t)>(n, f, k, X, ldx, (hipStream_t)stream); });
+}
+
+extern "C" int gcn_checkpoint_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const uint16_t* x_scales, int64_t ldxs, const void* W,
+                                              int64_t ldw, const void* Z, int64_t ldz, const uint16_t* z_scales, int64_t ldzs, const void* dY, int64_t lddy, int act, float rho, void* dZ,
+                                              int64_t lddz, void* dX, int64_t lddx, void* dW, int64_t lddw, float* dbias, void* dR, int64_t lddr, void* stream) {
+    static const char* const who = "gcn_checkpoint_linear_backward";
+    const hipStream_t s = (hipStream_t)stream;
+    if (!dY || (dW && !X) || (dX && !W)) return fail(GCN_ERR_BADARG, "%s: NULL argument", who);
+    if (!known_type(type)) return fail(GCN_ERR_BADARG, "%s: unknown element type %d", who, type);
+    if (!known_act(act)) return fail(GCN_ERR_BADARG, "%s: unknown activation %d", who, act);
+    const bool curved = act != GCN_ACT_NONE, products = dX || dW;
+    if (curved && (products || dbias || dZ) && !Z) return fail(GCN_ERR_BADARG, "%s: the activation's derivative needs Z", who);
+    if (curved && products && !dZ) return fail(GCN_ERR_BADARG, "%s: the products need dZ as workspace", who);
+    if (n <= 0 || f_in <= 0 || f_out <= 0) return fail(GCN_ERR_BADARG, "%s: sizes must be positive", who);
+    if (f_in > LINEAR_WIDEST || f_out > LINEAR_WIDEST) return fail(GCN_ERR_RANGE, "%s: widths go up to 2^27", who);
+    const Kept x{X, ldx, X ? x_scales : nullptr, ldxs}, z{curved ? Z : nullptr, ldz, curved && Z ? z_scales : nullptr, ldzs};
+    if (lddy < f_out || (x.p && ldx < f_in) || (x.scales && ldxs < groups_of(f_in, CHECKPOINT_GROUP)) || (W && ldw < f_out) || (z.p && ldz < f_out) ||
+        (z.scales && ldzs < groups_of(f_out, CHECKPOINT_GROUP)) || (curved && dZ && lddz < f_out) || (dX && lddx < f_in) || (dW && lddw < f_out) || (dR && lddr < f_out))
+        return fail(GCN_ERR_BADARG, "%s: leading dimension below the width", who);
+    const size_t b = elem_bytes(type);
+    if (!curved) dZ = nullptr;
+    const Span in[] = {span_of(x, n, f_in, b), scales_of(x, n, f_in), Span(W, f_in, f_out, ldw, b), span_of(z, n, f_out, b), scales_of(z, n, f_out), Span(dY, n, f_out, lddy, b)};
+    const Span out[] = {Span(dZ, n, f_out, lddz, b), Span(dR, n, f_out, lddr, b), Span(dX, n, f_in, lddx, b), Span(dW, f_in, f_out, lddw, b), Span(dbias, 1, f_out, f_out, 4)};
+    bool bad = false;
+    for (int o = 0; o < 5; ++o) {
+        for (int i = 0; i < 6; ++i) {
+            // an element of dZ may take the place of the one of Z or dY that it is made of, one of dR that of dY
+            const bool may = (o == 0 && ((i == 3 && !z.scales) || i == 5)) || (o == 1 && i == 5 && (curved || !products));
+            bad |= out[o].meets(in[i]) && !(may && out[o].is(in[i]));
+        }
+        for (int i = 0; i < o; ++i) bad |= out[o].meets(out[i]);
+    }
+    if (bad) return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
+    if (dbias || dR || dZ) {
+        SlopeArgs a;
+        a.n = n; a.N = f_out; a.Z = z; a.dY = dY; a.lddy = lddy; a.dZ = dZ; a.lddz = lddz; a.also = dR; a.ldalso = lddr; a.rho = rho;
+        a.act = dbias || dZ ? act : GCN_ACT_NONE;
+        GCN_TRY(by_type(type, [&](auto t) {
+            using T = decltype(t);
+            return z.scales ? launch_slope<T, false, true>(a, dbias, s) : launch_slope<T, false, false>(a, dbias, s);
+        }));
+    }
+    BackProducts p;
+    p.n = n; p.f_in = f_in; p.cols = f_out; p.X = x; p.W = W; p.ldw = ldw; p.G = curved ? dZ : dY; p.ldg = curved ? lddz : lddy;
+    p.dX = dX; p.lddx = lddx; p.dW = dW; p.lddw = lddw;
+    return back_products(type, p, s);
+}

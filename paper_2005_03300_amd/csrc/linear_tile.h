@@ -47,6 +47,7 @@ __device__ __forceinline__ float normal_cdf(float z, float& density) {
     density = 0.39894228040143268f * g;
     return z < 0.f ? tail : 1.f - tail;
 }
+inline bool known_act(int act) { return act >= GCN_ACT_NONE && act <= GCN_ACT_SILU; }
 // act and its derivative.  NaN stays NaN.
 template <typename T>
 __device__ __forceinline__ float act_of(float z, int act) {
