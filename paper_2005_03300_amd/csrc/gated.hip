@@ -1,33 +1,6 @@
 // A gated block over the rows of X: Z = X W + 1 bias^T with W of 2 N columns, H = act(Z's first N columns) (Hadamard) the others, and its gradients.
 #include "slope.h"
 
-namespace gcn {
-
-// One result for each thread.
-template <typename T>
-__global__ __launch_bounds__(256) void k_gated(TileArgs a) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, m = t / a.N, n = t % a.N;
-    if (m >= a.M) return;
-    const T* const x = (const T*)a.A + m * a.lda;
-    const T* const w = (const T*)a.B + n;
-    float g = 0.f, u = 0.f;
-    for (int64_t k = 0; k < a.K; ++k) {
-        g = fmaf((float)x[k], (float)w[k * a.ldb], g);
-        u = fmaf((float)x[k], (float)w[k * a.ldb + a.N], u);
-    }
-    if (a.bias) {
-        g += a.bias[n];
-        u += a.bias[a.N + n];
-    }
-    if (a.Z) {
-        ((T*)a.Z)[m * a.ldz + n] = (T)g;
-        ((T*)a.Z)[m * a.ldz + a.N + n] = (T)u;
-    }
-    ((T*)a.Y)[m * a.ldy + n] = (T)(act_of<T>(g, a.act) * u);
-}
-
-}  // namespace gcn
-
 using namespace gcn;
 
 extern "C" int gcn_gated_forward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const void* W, int64_t ldw, const float* bias, int act, void* Z,
@@ -46,11 +19,7 @@ extern "C" int gcn_gated_forward(int64_t n, int32_t f_in, int32_t f_out, int typ
         return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
     TileArgs a;
     a.A = X; a.lda = ldx; a.B = W; a.ldb = ldw; a.M = n; a.N = f_out; a.K = f_in; a.bias = bias; a.act = act; a.Z = Z; a.ldz = ldz; a.Y = H; a.ldy = ldh;
-    return by_type(type, [&](auto t) -> int {
-        hipLaunchKernelGGL(k_gated<decltype(t)>, dim3((unsigned)((n * f_out + 255) / 256)), dim3(256), 0, (hipStream_t)stream, a);
-        GCN_LAUNCH_CHECK();
-        return GCN_OK;
-    });
+    return by_type(type, [&](auto t) { return gated_forward_of<decltype(t)>(a, (hipStream_t)stream); });
 }
 
 extern "C" int gcn_gated_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const void* X, int64_t ldx, const uint16_t* x_scales, int64_t ldxs, const void* W, int64_t ldw,

@@ -22,16 +22,18 @@ constexpr size_t few_lds() { return (size_t)FEW_WAVES * RT * 16 * (16 * C + 4) *
 // a strip can be half of a cache line wide.
 // C is the widest that still leaves a strip for every compute unit: 4096 x 4096 in fp32 with 256 strips of 16 columns 14.5 us, with 128 of 32 18.8.
 // Few strips: the steps are also shared by gridDim.y workgroups, whose partial results k_linear_join adds.
-template <typename T, int C, int RT>
+// GATED: half of a strip's columns are the gate's, the others those of the same 8 C columns of H.
+template <typename T, int C, int RT, bool GATED>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int strips) {
     constexpr int E = Elem<T>::E, STEP = 4 * E, AHEAD = 2, ROW = 16 * C + 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const int per = (strips + 7) / 8, strip = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if (strip >= strips || (int)(blockIdx.x >> 3) >= per) return;
-    const int n0 = strip * 16 * C, n = n0 + r * C;
+    constexpr int WIDE = GATED ? 8 * C : 16 * C;                  // columns of the result
+    const int n0 = strip * WIDE, n = n0 + (GATED ? (r & 7) * C : r * C);
     const int there = a.N - n < 0 ? 0 : (a.N - n > C ? C : a.N - n);
-    const T* const W = (const T*)a.B + n;
+    const T* const W = (const T*)a.B + n + (GATED && r >= 8 ? a.N : 0);
     const T* const X = (const T*)a.A;
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
     v4f acc[RT][C] = {};
@@ -65,7 +67,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int s
     };
     constexpr int ALL = FEW_WAVES * STEP;
     int64_t k = kb + wave * STEP;
-    if (n0 + 16 * C <= a.N)
+    if (n0 + WIDE <= a.N)
         for (; k + (AHEAD - 1) * ALL + STEP <= ke; k += AHEAD * ALL) {
             Step s[AHEAD];
 #pragma unroll
@@ -91,22 +93,29 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int s
         *at = sum;
     }
     __syncthreads();
-    constexpr int PIECES = 16 * C / E;
-    if constexpr (16 * C % E == 0) {
+    constexpr int PIECES = WIDE / E;
+    if constexpr (WIDE % E == 0) {
         for (int i = threadIdx.x; i < RT * 16 * PIECES; i += FEW_WAVES * 64) {
             const int row = i / PIECES, c = i % PIECES * E, count = a.N - n0 - c;
             if (row >= a.M || count <= 0) continue;
-            float d[E];
+            float d[GATED ? 2 : 1][E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) d[e] = ((const float*)lds)[row * ROW + c + e];
-            if (a.part) {
-                float* const p = a.part + ((int64_t)blockIdx.y * a.M + row) * a.N + n0 + c;
+            for (int h = 0; h < (GATED ? 2 : 1); ++h) {
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (e < count) p[e] = d[e];
+                for (int e = 0; e < E; ++e) d[h][e] = ((const float*)lds)[row * ROW + h * WIDE + c + e];
+                if (a.part) {
+                    float* const p = a.part + (((int64_t)blockIdx.y * a.M + row) * (GATED ? 2 : 1) + h) * a.N + n0 + c;
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (e < count) p[e] = d[h][e];
+                }
+            }
+            if (a.part) continue;
+            if constexpr (GATED) {
+                finish_gated<T>(a, row, n0 + c, count, d[0], d[1]);
             } else {
                 float r_[E];
-                finish<T>(a, row, n0 + c, count, d, false, r_);
+                finish<T>(a, row, n0 + c, count, d[0], false, r_);
             }
         }
     }

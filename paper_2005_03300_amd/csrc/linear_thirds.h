@@ -15,9 +15,9 @@ namespace gcn {
 // One operand of a stage: 32 values of k of R rows (of A) or columns (of B), as three planes of bf16.
 //   BY_K   64 bytes per row; its four pieces of 8 k are moved about by bits of the row
 //   BY_MN  one row per k of R elements, whose blocks of 16 are moved about as in Operand
-template <int R, int LIES, int THREADS>
+template <int R, int LIES, int THREADS, int HALF = 0>
 struct Thirds {
-    using Plain = Operand<float, R, LIES, THREADS>;
+    using Plain = Operand<float, R, LIES, THREADS, HALF>;
     static constexpr int PLANE = R * 64, PER = Plain::PER;
     static constexpr int BLOCKS = R / 16 < 8 ? R / 16 : 8;
     __device__ static int twist(int k) { return ((k & 3) | ((k >> 3 & 1) << 2)) & (BLOCKS - 1); }
@@ -68,12 +68,12 @@ struct Thirds {
 // workgroup on the compute unit meanwhile.  Of the compute units' cycles the matrix units are busy in 40 % at 232965 x 602 x 128 (96 products of 16 cycles a stage and wavefront), and
 // vector instructions are issued in 40 %: 22 split four numbers.  (A look at every number for infinities made them as many as the products take: 180 TFLOP/s.)  The second set of
 // results for those that are not finite costs 16 and 18 spilled registers of the 128 x 128 forms whose B lies along n.
-template <int BM, int BN, int WM, int WN, int LA, int LB>
+template <int BM, int BN, int WM, int WN, int LA, int LB, bool GATED>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, BK = 32, E = 4;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     using OpA = Thirds<BM, LA, THREADS>;
-    using OpB = Thirds<BN, LB, THREADS>;
+    using OpB = Thirds<BN, LB, THREADS, GATED ? BN / WN / 2 : 0>;
     using PlainA = typename OpA::Plain;
     using PlainB = typename OpB::Plain;
     constexpr int STAGE = 3 * (OpA::PLANE + OpB::PLANE);
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     int tm, tn;
     tile_place(a, tm, tn);
     const int64_t m0 = (int64_t)tm * BM;
-    const int n0 = tn * BN;
+    const int n0 = tn * (GATED ? BN / 2 : BN);
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
     const float* const A = (const float*)a.A;
     const float* const B = (const float*)a.B;
@@ -181,7 +181,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     }
     constexpr int PHASES = (BM * BN * 4 + STAGE - 1) / STAGE, PART = BM / WM / PHASES * (BN / WN) * 4;
     static_assert(WM * WN * PART <= STAGE && (BM + BN) * 128 <= STAGE, "results and plain stages have room");
-    leave_tile<float, FM, FN, PHASES, LA == BY_MN, LB == BY_MN>(a, acc, stage + wave * PART, m0 + wm, n0 + wn, lane);
+    if constexpr (GATED) leave_gated<float, FM, FN, PHASES, true>(a, acc, stage + wave * PART, m0 + wm, n0 + wn / 2, lane);
+    else leave_tile<float, FM, FN, PHASES, LA == BY_MN, LB == BY_MN>(a, acc, stage + wave * PART, m0 + wm, n0 + wn, lane);
 }
 
 }  // namespace gcn

@@ -4,6 +4,7 @@
 //   forward  X W      A by k, B by n
 //   dX       dZ W^T   A by k, B by k   (the stored W is N x K)
 //   dW       X^T dZ   A by m, B by n   (the stored X is K x M)
+// and the gated block's, whose B has 2 N columns: a tile has as many of the gate's as of the others, and the two results of a place of H with one lane.
 #pragma once
 #include "rows.h"
 
@@ -19,8 +20,8 @@ struct TileArgs {
     int64_t k_share = 0;          // of one split: a multiple of the tile's depth
     int32_t N = 0;
     int32_t tiles_m = 0, tiles_n = 0;
-    float* part = nullptr;        // partial results, one M x N each split; NULL: the epilogue runs here
-    // D' = rho R + act(D + 1 bias^T); the argument of act is Z
+    float* part = nullptr;        // partial results, one M x N (gated: M x 2 N) each split; NULL: the epilogue runs here
+    // D' = rho R + act(D + 1 bias^T); the argument of act is Z.  Gated: D and Z have 2 N columns, D' = act(Z's first N) (Hadamard) the others
     const float* bias = nullptr;
     const void* R = nullptr;
     void* Z = nullptr;
@@ -96,6 +97,36 @@ __device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int 
     store_vec_part((T*)a.Y + m * a.ldy + n, from_floats<T>(d), count);
 }
 
+// What becomes of the gate's results `g` and the others `u` of row m, columns n to n + E - 1 of H.
+template <typename T>
+__device__ __forceinline__ void finish_gated(const TileArgs& a, int64_t m, int n, int count, float (&g)[Elem<T>::E], float (&u)[Elem<T>::E]) {
+    constexpr int E = Elem<T>::E;
+    if (a.bias) {
+        float b[E], c[E];
+        load_floats<E>(a.bias, n, count, 0.f, b);
+        load_floats<E>(a.bias, (int64_t)a.N + n, count, 0.f, c);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            g[e] += b[e];
+            u[e] += c[e];
+        }
+    }
+    if (a.Z) {
+        T* const z = (T*)a.Z + m * a.ldz + n;
+        store_vec_part(z, from_floats<T>(g), count);
+        store_vec_part(z + a.N, from_floats<T>(u), count);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) g[e] = act_of<T>(g[e], a.act) * u[e];
+    if (a.R) {
+        float r[E];
+        to_floats<T>(load_vec_part((const T*)a.R + m * a.ldr + n, count), r);
+#pragma unroll
+        for (int e = 0; e < E; ++e) g[e] = fmaf(a.rho, r[e], g[e]);
+    }
+    store_vec_part((T*)a.Y + m * a.ldy + n, from_floats<T>(g), count);
+}
+
 #if defined(__HIP_DEVICE_COMPILE__)
 #define GCN_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
 #endif
@@ -106,7 +137,8 @@ __device__ __forceinline__ void finish(const TileArgs& a, int64_t m, int n, int 
 //   BY_MN  one row per k of R elements; blocks of 16 elements are moved about within a row by a few bits of k, so that the rows that
 //          a fragment takes together (four, or four of eight) lie in different banks.
 // The place is the same whether pieces come straight from memory or through registers.
-template <typename T, int R, int LIES, int THREADS>
+// HALF > 0 (BY_MN, of a gated block): of each 2 HALF columns of the tile the first HALF are the gate's, the others those of the same places of H, `rows` columns behind.
+template <typename T, int R, int LIES, int THREADS, int HALF = 0>
 struct Operand {
     static constexpr int E = Elem<T>::E, BK = 8 * E, PIECES = R * 8, PER = PIECES / THREADS, ROW = R / E;   // ROW: pieces of a row, BY_MN
     static constexpr int BLOCKS = R / 16 < 8 ? R / 16 : 8;
@@ -114,6 +146,9 @@ struct Operand {
     __device__ static int twist(int k) {                          // which block a row's first lies at
         return (sizeof(T) == 2 ? (k & 3) | ((k >> 3 & 1) << 2) : (k >> 2) & 3) & (BLOCKS - 1);
     }
+    // BY_MN: where a piece of a row begins, from the tile's first column on, and how far behind that the half it belongs to does
+    __device__ static int begins(int piece) { return HALF ? piece * E / (HALF ? 2 * HALF : 1) * HALF + piece * E % (HALF ? HALF : 1) : piece * E; }
+    __device__ static int64_t behind(int piece, int64_t rows) { return HALF && piece * E % (HALF ? 2 * HALF : 1) >= HALF ? rows : 0; }
     // piece `slot` of LDS: its row (of r or k) and which piece of that row in memory
     __device__ static void at(int slot, int& row, int& piece) {
         if (LIES == BY_K) {
@@ -138,9 +173,9 @@ struct Operand {
                 r = r < rows ? r : rows - 1;
                 src = p + r * ld + k0 + piece * E;
             } else {
-                int64_t r = r0 + piece * E;
+                int64_t r = r0 + begins(piece);
                 r = r < rows ? r : rows - E;
-                src = p + (k0 + row) * ld + r;
+                src = p + (k0 + row) * ld + r + behind(piece, rows);
             }
 #if defined(__HIP_DEVICE_COMPILE__)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
@@ -160,7 +195,7 @@ struct Operand {
             int row, piece;
             at(i * THREADS + tid, row, piece);
             if (LIES == BY_K) s.src[i] = p + (r0 + row < rows ? r0 + row : rows - 1) * ld + k0 + piece * E;
-            else s.src[i] = p + (k0 + row) * ld + piece_at(r0 + piece * E, rows);
+            else s.src[i] = p + (k0 + row) * ld + piece_at(r0 + begins(piece), rows) + behind(piece, rows);
         }
         return s;
     }
@@ -200,9 +235,10 @@ struct Operand {
         for (int i = 0; i < PER; ++i) {
             int row, piece;
             at(i * THREADS + tid, row, piece);
-            const int64_t r = r0 + piece * E, k = k0 + row;
-            if (rows >= E) v[i] = k < K ? load_vec(p + k * ld + piece_at(r, rows)) : Vec<T>{};
-            else v[i] = k < K && r == 0 ? load_vec_part(p + k * ld, (int)rows) : Vec<T>{};
+            const int64_t r = r0 + begins(piece), k = k0 + row;
+            const T* const q = p + k * ld + behind(piece, rows);
+            if (rows >= E) v[i] = k < K ? load_vec(q + piece_at(r, rows)) : Vec<T>{};
+            else v[i] = k < K && r == 0 ? load_vec_part(q, (int)rows) : Vec<T>{};
         }
     }
     // Where the piece from r on (a multiple of E) of a dimension that is contiguous in memory is taken from.
@@ -358,6 +394,64 @@ __device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[F
     }
 }
 
+// The same for a gated block: of a wavefront's 16 FN columns the first half are the gate's, the others those of the same 8 FN columns of H from n0 on.
+template <typename T, int FM, int FN, int PHASES, bool CUT_N>
+__device__ __forceinline__ void leave_gated(const TileArgs& a, const v4f (&acc)[FM][FN], char* mine, int64_t m0, int n0, int lane) {
+    constexpr int E = Elem<T>::E, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4, HALF = FN * 8;
+    static_assert(FM % PHASES == 0 && FN % 2 == 0, "whole phases, two halves");
+    constexpr int LANES = HALF / E, STEP = 64 / LANES;            // lanes of a row, rows at a time
+    static_assert(ROWS % STEP == 0, "all lanes have rows");
+    float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N * 2 : nullptr;
+#pragma unroll
+    for (int ph = 0; ph < PHASES; ++ph) {
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int row = i * 16 + (lane & 15);
+                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[ph * FP + i][j];
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const int c = (lane % LANES) * E, n = n0 + c, count = a.N - n;
+        const bool shifted = CUT_N && count < E && a.N >= E;      // as in leave_tile: a piece that the end cut holds the last whole one
+#pragma nounroll
+        for (int row = lane / LANES; row < ROWS; row += STEP) {
+            const int64_t m = m0 + ph * ROWS + row;
+            if (m >= a.M || count <= 0) continue;
+            float d[2][E];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    const v4f x = *reinterpret_cast<const v4f*>(mine + row * (PIECES * 16) + ((((h * HALF + c + e) / 4) ^ (row & (PIECES - 1))) << 4));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) d[h][e + q] = x[q];
+                }
+                if (shifted)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        float x = d[h][e];
+#pragma unroll
+                        for (int o = 1; o < E; ++o) x = e + o < E && E - count == o ? d[h][e + o < E ? e + o : e] : x;
+                        d[h][e] = x;
+                    }
+                if (part) {
+                    float* const p = part + (m * 2 + h) * a.N + n;
+                    if (count >= E)
+#pragma unroll
+                        for (int e = 0; e < E; e += 4) *reinterpret_cast<f4u*>(p + e) = f4u{d[h][e], d[h][e + 1], d[h][e + 2], d[h][e + 3]};
+                    else
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (e < count) p[e] = d[h][e];
+                }
+            }
+            if (!part) finish_gated<T>(a, m, n, count, d[0], d[1]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
 // D = A B for 16-bit elements: BM x BN results of a workgroup of WM x WN wavefronts, 128 bytes of k (64 values) at a time, two such stages in LDS: one is
 // fetched while the other is multiplied.  A wavefront's results are the transpose of what the matrix unit is given (B's columns as its rows), so that a lane
 // holds four neighbouring columns of one row.
@@ -368,13 +462,14 @@ __device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[F
 // the chip otherwise.  128 bytes of k are a cache line of a row, and one barrier for 64 (256 x 256) products of a wavefront.
 // DIRECT: rows of both operands at 16-byte addresses in whole pieces: memory to LDS without registers.  (Through registers the 256 x 256 tile spills 23 of them forward and
 // 60 for dW.)
-template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT>
+template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT, bool GATED>
 __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, E = Elem<T>::E, BK = 8 * E;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
     constexpr int STAGE = (BM + BN) * 128;
+    static_assert(!GATED || LB == BY_MN, "the halves of B lie side by side");
     using OpA = Operand<T, BM, LA, THREADS>;
-    using OpB = Operand<T, BN, LB, THREADS>;
+    using OpB = Operand<T, BN, LB, THREADS, GATED ? BN / WN / 2 : 0>;
     // Two arrays, so that the compiler can tell what is on its way to the one from what is read of the other: it makes a transposing read wait for everything
     // that may be on its way to the same array (16384 x 4096 x 4096 in bf16 with one: 935 TFLOP/s).
     __shared__ __attribute__((aligned(16))) char stage0[STAGE], stage1[STAGE];
@@ -382,7 +477,7 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
     int tm, tn;
     tile_place(a, tm, tn);
     const int64_t m0 = (int64_t)tm * BM;
-    const int n0 = tn * BN;
+    const int n0 = tn * (GATED ? BN / 2 : BN);                    // of the result
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
     const T* const A = (const T*)a.A;
     const T* const B = (const T*)a.B;
@@ -465,45 +560,58 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
     constexpr int HALF = WM * WN / 2;                             // wavefronts that have their part in the first stage
     static_assert(HALF * PART <= STAGE, "results have room");
     __syncthreads();
-    leave_tile<T, FM, FN, PHASES, LA == BY_MN && !DIRECT, LB == BY_MN && !DIRECT>(a, acc, (wave < HALF ? stage0 : stage1) + (wave % HALF) * PART, m0 + wm,
-                                                                                 n0 + wn, lane);
+    char* const mine = (wave < HALF ? stage0 : stage1) + (wave % HALF) * PART;
+    if constexpr (GATED) leave_gated<T, FM, FN, PHASES, !DIRECT>(a, acc, mine, m0 + wm, n0 + wn / 2, lane);
+    else leave_tile<T, FM, FN, PHASES, LA == BY_MN && !DIRECT, LB == BY_MN && !DIRECT>(a, acc, mine, m0 + wm, n0 + wn, lane);
 }
 
 // The partial results of the splits, added in order, and what the layer does with the sum: 16 bytes of it per thread; SHARES threads, a wavefront apart, take a
 // share of the splits each where there are many of them and few results (one thread after 211 of them: 60 us).
-template <typename T, int SHARES>
+template <typename T, int SHARES, bool GATED>
 __global__ __launch_bounds__(64 * (SHARES > 1 ? SHARES : 4)) void k_linear_join(TileArgs a, int splits) {
-    constexpr int E = Elem<T>::E, PER = SHARES > 1 ? 64 : 256;
-    __shared__ float add[SHARES > 1 ? SHARES : 1][SHARES > 1 ? 64 : 1][E + 1];
+    constexpr int E = Elem<T>::E, PER = SHARES > 1 ? 64 : 256, HALVES = GATED ? 2 : 1;
+    __shared__ float add[SHARES > 1 ? SHARES : 1][SHARES > 1 ? 64 : 1][HALVES * E + 1];
     const int64_t per = (a.N + E - 1) / E, t = (int64_t)blockIdx.x * PER + threadIdx.x % PER;
     const int share = threadIdx.x / PER;
     const int64_t m = t / per;
     const int n = (int)(t % per) * E, count = a.N - n;
-    float d[E] = {};
+    float d[HALVES][E] = {};
     if (m < a.M) {
-        const float* const p = a.part + m * a.N + n;
+        const float* const p = a.part + m * HALVES * a.N + n;
 #pragma unroll 4
-        for (int s = share; s < splits; s += SHARES) {
-            float x[E];
-            load_floats<E>(p + (int64_t)s * a.M * a.N, 0, count, 0.f, x);
+        for (int s = share; s < splits; s += SHARES)
 #pragma unroll
-            for (int e = 0; e < E; ++e) d[e] += x[e];
-        }
+            for (int h = 0; h < HALVES; ++h) {
+                float x[E];
+                load_floats<E>(p + (int64_t)s * a.M * HALVES * a.N + (int64_t)h * a.N, 0, count, 0.f, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[h][e] += x[e];
+            }
     }
     if constexpr (SHARES > 1) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) add[share][threadIdx.x % PER][e] = d[e];
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int e = 0; e < E; ++e) add[share][threadIdx.x % PER][h * E + e] = d[h][e];
         __syncthreads();
         if (share) return;
         for (int w = 1; w < SHARES; ++w)
 #pragma unroll
-            for (int e = 0; e < E; ++e) d[e] += add[w][threadIdx.x][e];
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[h][e] += add[w][threadIdx.x][h * E + e];
     }
-    float r[E];
-    if (m < a.M) finish<T>(a, m, n, count, d, false, r);
+    if (m >= a.M) return;
+    if constexpr (GATED) {
+        finish_gated<T>(a, m, n, count, d[0], d[1]);
+    } else {
+        float r[E];
+        finish<T>(a, m, n, count, d[0], false, r);
+    }
 }
 
 template <typename T> int linear_forward_of(const TileArgs& a, hipStream_t s);          // A by k, B by n, with the epilogue
+template <typename T> int gated_forward_of(const TileArgs& a, hipStream_t s);           // the same with 2 N columns of B
 template <typename T> int linear_dx_of(const TileArgs& a, hipStream_t s);               // A by k, B by k
 template <typename T> int linear_dw_of(const TileArgs& a, hipStream_t s);               // A by m, B by n
 
