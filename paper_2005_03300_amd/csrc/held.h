@@ -14,6 +14,15 @@ constexpr float CHECKPOINT_TOP = 127.f, WEIGHT4_TOP = 6.f;
 
 __host__ __device__ constexpr int64_t groups_of(int64_t f, int64_t group) { return (f + group - 1) / group; }
 
+// Weights held in 4 bits, as gcn_linear4_pack lays them out.
+struct Weights4 {
+    const uint32_t* Q = nullptr;
+    const uint16_t* S = nullptr;
+    int64_t ldq = 0, lds = 0;
+    int group = 0;
+    bool gated = false;
+};
+
 // A scale's bits as a number, and 2 of them in a word.
 __device__ __forceinline__ float scale_value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
 

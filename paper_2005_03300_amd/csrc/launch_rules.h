@@ -154,4 +154,26 @@ inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, bool 
     return best;
 }
 
+// In how many shares the sum over k of a product with weights held in 4 bits is cut, for tiles of 128 x 128: the least estimated time, as choose_tiles.  A share is a whole number of blocks of 128
+// values of k.
+inline int splits_of_4(int64_t tiles, int64_t results, int64_t K, bool fp32, int64_t cus) {
+    const int64_t blocks = (K + 127) / 128;
+    const double products = 2.0 * 128 * 128 * 128 / (fp32 ? 1.2e6 : 2.9e6), way = 1.6;         // microseconds of a block: of one tile's products, of its way from memory
+    int best = 1;
+    double least = 1e300;
+    for (int64_t splits = 1; splits <= 512; splits += splits < 4 ? 1 : splits / 2) {
+        const int64_t share = (blocks + splits - 1) / splits;
+        if (splits > 1 && tiles * (splits - 1) > 4 * cus) break;
+        const int64_t each = (tiles * splits + cus - 1) / cus, rounds = (each + 1) / 2, together = each < 2 ? each : 2;
+        double us = rounds * (share * (together * products > way ? together * products : way) + 1.5);
+        if (splits > 1) us += 3.0 + splits * (double)results * 8 / 4.0e6;
+        if (us < least) {
+            least = us;
+            best = (int)splits;
+        }
+        if (share == 1) break;
+    }
+    return best;
+}
+
 }  // namespace gcn

@@ -1,6 +1,5 @@
 // Linear layers and gated blocks whose weights are held in 4 bits: laid out once, and multiplied as they are.
 #include "held.h"
-#include "launch_rules.h"
 #include "linear_tile.h"
 
 namespace gcn {
@@ -22,9 +21,6 @@ __device__ __forceinline__ float weight4_value(uint32_t code) {
     const float v = c < 4 ? 0.5f * c : (c == 7 ? 6.f : (float)c - 2.f);
     return code & 8u ? -v : v;
 }
-
-// What the places are multiplied by in a product, so that the sum over a group, of up to 128 places of up to 6, is no larger than the largest x.
-constexpr float WEIGHT4_DOWN = 1.f / 1024;
 
 // A thread has a group of a column, read twice: the largest first.
 template <typename T>
@@ -63,34 +59,7 @@ __global__ __launch_bounds__(256) void k_linear4_unpack(int32_t K, int64_t cols,
     }
 }
 
-struct Weights4 {
-    const uint32_t* Q = nullptr;
-    const uint16_t* S = nullptr;
-    int64_t ldq = 0, lds = 0;
-    int group = 0;
-    bool gated = false;
-};
-
-// One result for each thread.
-template <typename T>
-__global__ __launch_bounds__(256) void k_linear4(TileArgs a, Weights4 w) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, m = t / a.N, n = t % a.N;
-    if (m >= a.M) return;
-    const T* const x = (const T*)a.A + m * a.lda;
-    auto column = [&](int64_t c) {
-        float sum = 0.f;
-        for (int64_t k0 = 0; k0 < a.K; k0 += w.group) {
-            float part = 0.f;
-            for (int64_t k = k0; k < k0 + w.group && k < a.K; ++k) part = fmaf((float)x[k], WEIGHT4_DOWN * weight4_value(w.Q[k / 8 * w.ldq + c] >> (k % 8 * 4)), part);
-            sum = fmaf(scale_value(w.S[k0 / w.group * w.lds + c]) * part, 1.f / WEIGHT4_DOWN, sum);
-        }
-        return a.bias ? sum + a.bias[c] : sum;
-    };
-    float y = act_of<T>(column(n), a.act);
-    if (w.gated) y *= column(a.N + n);
-    if (a.R) y = fmaf(a.rho, (float)((const T*)a.R)[m * a.ldr + n], y);
-    ((T*)a.Y)[m * a.ldy + n] = (T)y;
-}
+template <typename T> int linear4_of(const TileArgs& a, const Weights4& w, hipStream_t s);
 
 }  // namespace gcn
 
@@ -154,9 +123,5 @@ extern "C" int gcn_linear4_forward(int64_t n, int32_t f_in, int32_t f_out, int t
         return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
     TileArgs a;
     a.A = X; a.lda = ldx; a.M = n; a.N = f_out; a.K = f_in; a.bias = bias; a.act = act; a.R = R; a.ldr = ldr; a.rho = rho; a.Y = Y; a.ldy = ldy;
-    return by_type(type, [&](auto t) -> int {
-        hipLaunchKernelGGL(k_linear4<decltype(t)>, dim3((unsigned)((n * f_out + 255) / 256)), dim3(256), 0, (hipStream_t)stream, a, w);
-        GCN_LAUNCH_CHECK();
-        return GCN_OK;
-    });
+    return by_type(type, [&](auto t) { return linear4_of<decltype(t)>(a, w, (hipStream_t)stream); });
 }

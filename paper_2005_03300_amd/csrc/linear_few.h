@@ -13,6 +13,57 @@ constexpr int FEW_STRIPS = 48;
 template <typename T, int C, int RT>
 constexpr size_t few_lds() { return (size_t)FEW_WAVES * RT * 16 * (16 * C + 4) * 4; }
 
+// The wavefronts' results, of lane (r, quarter) those of row r (of each 16) and columns (4 quarter + e) C + q of the strip from n0 on, added in order in LDS, times `times`, and what the layer does
+// with them.
+template <typename T, int C, int RT, bool GATED>
+__device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT][C], char* lds, int n0, float times = 1.f) {
+    constexpr int E = Elem<T>::E, ROW = 16 * C + 4, WIDE = GATED ? 8 * C : 16 * C;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
+    float* const mine = (float*)lds + wave * (RT * 16 * ROW);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int q = 0; q < C; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine[(t * 16 + r) * ROW + (quarter * 4 + e) * C + q] = acc[t][q][e];
+    __syncthreads();
+    // a thread for each result; the sum takes the place of the first wavefront's, which no other thread reads
+    for (int i = threadIdx.x; i < RT * 16 * 16 * C; i += FEW_WAVES * 64) {
+        float* const at = (float*)lds + i / (16 * C) * ROW + i % (16 * C);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) sum += at[w * RT * 16 * ROW];
+        *at = sum * times;
+    }
+    __syncthreads();
+    constexpr int PIECES = WIDE / E;
+    if constexpr (WIDE % E == 0) {
+        for (int i = threadIdx.x; i < RT * 16 * PIECES; i += FEW_WAVES * 64) {
+            const int row = i / PIECES, c = i % PIECES * E, count = a.N - n0 - c;
+            if (row >= a.M || count <= 0) continue;
+            float d[GATED ? 2 : 1][E];
+#pragma unroll
+            for (int h = 0; h < (GATED ? 2 : 1); ++h) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[h][e] = ((const float*)lds)[row * ROW + h * WIDE + c + e];
+                if (a.part) {
+                    float* const p = a.part + (((int64_t)blockIdx.y * a.M + row) * (GATED ? 2 : 1) + h) * a.N + n0 + c;
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (e < count) p[e] = d[h][e];
+                }
+            }
+            if (a.part) continue;
+            if constexpr (GATED) {
+                finish_gated<T>(a, row, n0 + c, count, d[0], d[1]);
+            } else {
+                float r_[E];
+                finish<T>(a, row, n0 + c, count, d[0], false, r_);
+            }
+        }
+    }
+}
+
 // Y's rows are few, so the product is bound by reading W (and by about 4 us of start and end): 4096 x 4096 in bf16 for 16 rows 13.5 us, in fp32 for one row 14.5 us (4.6
 // TB/s), 4096 x 16384 in bf16 26 to 28 us (4.8 to 5 TB/s).  What is left where strips are narrow: a wavefront waits for its two steps before it multiplies them and sends for the next two
 // after, so at 4096 x 4096 in bf16, two bytes to a load, the weights come at 2.5 TB/s.
@@ -25,7 +76,7 @@ constexpr size_t few_lds() { return (size_t)FEW_WAVES * RT * 16 * (16 * C + 4) *
 // GATED: half of a strip's columns are the gate's, the others those of the same 8 C columns of H.
 template <typename T, int C, int RT, bool GATED>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int strips) {
-    constexpr int E = Elem<T>::E, STEP = 4 * E, AHEAD = 2, ROW = 16 * C + 4;
+    constexpr int E = Elem<T>::E, STEP = 4 * E, AHEAD = 2;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const int per = (strips + 7) / 8, strip = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
@@ -76,49 +127,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int s
             for (int u = 0; u < AHEAD; ++u) products(s[u]);
         }
     for (; k < ke; k += ALL) products(load(k, std::false_type()));
-    float* const mine = (float*)lds + wave * (RT * 16 * ROW);
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int q = 0; q < C; ++q)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mine[(t * 16 + r) * ROW + (quarter * 4 + e) * C + q] = acc[t][q][e];
-    __syncthreads();
-    // a thread for each result; the sum takes the place of the first wavefront's, which no other thread reads
-    for (int i = threadIdx.x; i < RT * 16 * 16 * C; i += FEW_WAVES * 64) {
-        float* const at = (float*)lds + i / (16 * C) * ROW + i % (16 * C);
-        float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) sum += at[w * RT * 16 * ROW];
-        *at = sum;
-    }
-    __syncthreads();
-    constexpr int PIECES = WIDE / E;
-    if constexpr (WIDE % E == 0) {
-        for (int i = threadIdx.x; i < RT * 16 * PIECES; i += FEW_WAVES * 64) {
-            const int row = i / PIECES, c = i % PIECES * E, count = a.N - n0 - c;
-            if (row >= a.M || count <= 0) continue;
-            float d[GATED ? 2 : 1][E];
-#pragma unroll
-            for (int h = 0; h < (GATED ? 2 : 1); ++h) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[h][e] = ((const float*)lds)[row * ROW + h * WIDE + c + e];
-                if (a.part) {
-                    float* const p = a.part + (((int64_t)blockIdx.y * a.M + row) * (GATED ? 2 : 1) + h) * a.N + n0 + c;
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (e < count) p[e] = d[h][e];
-                }
-            }
-            if (a.part) continue;
-            if constexpr (GATED) {
-                finish_gated<T>(a, row, n0 + c, count, d[0], d[1]);
-            } else {
-                float r_[E];
-                finish<T>(a, row, n0 + c, count, d[0], false, r_);
-            }
-        }
-    }
+    leave_few<T, C, RT, GATED>(a, acc, lds, n0);
 }
 
 }  // namespace gcn

@@ -7,21 +7,6 @@
 
 namespace gcn {
 
-template <typename T, int LIES>
-static bool whole_pieces(const void* p, int64_t ld, int64_t along) {
-    constexpr int E = Elem<T>::E;
-    return ((uintptr_t)p & 15) == 0 && ld % E == 0 && (LIES == BY_K || along % E == 0);
-}
-
-template <typename T, bool GATED>
-static int launch_join(const TileArgs& a, int splits, hipStream_t s) {
-    const int64_t threads = a.M * ((a.N + Elem<T>::E - 1) / Elem<T>::E);
-    if (splits > 8) hipLaunchKernelGGL((k_linear_join<T, 16, GATED>), dim3((unsigned)((threads + 63) / 64)), dim3(1024), 0, s, a, splits);
-    else hipLaunchKernelGGL((k_linear_join<T, 1, GATED>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, splits);
-    GCN_LAUNCH_CHECK();
-    return GCN_OK;
-}
-
 template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool GATED>
 static int launch_tile(TileArgs a, int splits, hipStream_t s) {
     constexpr int WIDE = GATED ? BN / 2 : BN;                     // columns of the result that a tile has

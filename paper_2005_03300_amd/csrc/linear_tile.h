@@ -610,6 +610,21 @@ __global__ __launch_bounds__(64 * (SHARES > 1 ? SHARES : 4)) void k_linear_join(
     }
 }
 
+template <typename T, int LIES>
+static bool whole_pieces(const void* p, int64_t ld, int64_t along) {
+    constexpr int E = Elem<T>::E;
+    return ((uintptr_t)p & 15) == 0 && ld % E == 0 && (LIES == BY_K || along % E == 0);
+}
+
+template <typename T, bool GATED>
+static int launch_join(const TileArgs& a, int splits, hipStream_t s) {
+    const int64_t threads = a.M * ((a.N + Elem<T>::E - 1) / Elem<T>::E);
+    if (splits > 8) hipLaunchKernelGGL((k_linear_join<T, 16, GATED>), dim3((unsigned)((threads + 63) / 64)), dim3(1024), 0, s, a, splits);
+    else hipLaunchKernelGGL((k_linear_join<T, 1, GATED>), dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, splits);
+    GCN_LAUNCH_CHECK();
+    return GCN_OK;
+}
+
 template <typename T> int linear_forward_of(const TileArgs& a, hipStream_t s);          // A by k, B by n, with the epilogue
 template <typename T> int gated_forward_of(const TileArgs& a, hipStream_t s);           // the same with 2 N columns of B
 template <typename T> int linear_dx_of(const TileArgs& a, hipStream_t s);               // A by k, B by k
