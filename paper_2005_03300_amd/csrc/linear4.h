@@ -78,26 +78,34 @@ __device__ __forceinline__ void parts_of(const Eight<T>& x, Vec<Unit4<T>> (&p)[P
     }
 }
 
+#if defined(__HIP_DEVICE_COMPILE__)
+#define KEEP_ORDER() __builtin_amdgcn_sched_barrier(0)
+#else
+#define KEEP_ORDER() (void)0
+#endif
+
 constexpr int BLOCK4 = 128;           // values of k that a wavefront takes at a time: a whole number of groups
 
-// Few rows: the strips, wavefronts and their end are those of k_linear_few.  A lane loads C neighbouring words of four rows of words, which are C fragments of four steps of 32 values of k.
-template <typename T, int C, int RT, bool GATED>
-__global__ __launch_bounds__(FEW_WAVES * 64) void k_linear4_few(TileArgs a, Weights4 w, int strips) {
+// Few rows: the strips and their end are those of k_linear_few.  A lane loads C neighbouring words of four rows of words, which are C fragments of four steps of 32 values of k, and has the results of
+// the same columns, so that it needs their scales and no others.  blockIdx.z: which 16 RT rows.
+template <typename T, int C, int RT, int WAVES, bool GATED>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT == 1) ? 4 : 2) void k_linear4_few(TileArgs a, Weights4 w, int strips) {
     using U = Unit4<T>;
     constexpr int PARTS = PARTS4<T>, WIDE = GATED ? 8 * C : 16 * C;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     const int per = (strips + 7) / 8, strip = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if (strip >= strips || (int)(blockIdx.x >> 3) >= per) return;
-    const int n0 = strip * WIDE;
-    // where columns `c` on of the strip's 16 C are, and how many of C or 4 C of them are there
-    auto column = [&](int c) { return GATED ? n0 + (c < 8 * C ? c : c - 8 * C) : n0 + c; };
-    auto behind = [&](int c) { return GATED && c >= 8 * C ? (int64_t)a.N : (int64_t)0; };
-    const int cq = r * C, cs = quarter * 4 * C;
-    const int there_q = a.N - column(cq), there_s = a.N - column(cs);
-    const uint32_t* const Q = w.Q + column(cq) + behind(cq);
-    const uint16_t* const S = w.S + column(cs) + behind(cs);
-    const T* const X = (const T*)a.A;
+    const int n0 = strip * WIDE, n = n0 + (GATED ? (r & 7) * C : r * C);
+    const int there = a.N - n;                                    // of the lane's C columns
+    const int64_t c = n + (GATED && r >= 8 ? (int64_t)a.N : 0);
+    const uint32_t* const Q = w.Q + c;
+    const uint16_t* const S = w.S + c;
+    const int64_t m0 = (int64_t)blockIdx.z * (16 * RT);
+    const T* const X = (const T*)a.A + m0 * a.lda;
+    a.M -= m0;
+    a.Y = (T*)a.Y + m0 * a.ldy;
+    if (a.R) a.R = (const T*)a.R + m0 * a.ldr;
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
     const int steps = w.group / 32;
     v4f acc[RT][C] = {};
@@ -105,19 +113,19 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear4_few(TileArgs a, Weig
     auto block = [&](int64_t k0, auto whole) {
         constexpr bool ALL = decltype(whole)::value;
         Elems<uint32_t, C> word[4];
-        Elems<uint16_t, 4 * C> scale[4];
+        Elems<uint16_t, C> scale[4];
         Eight<T> x[4][RT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t k = k0 + i * 32 + quarter * 8;
-            word[i] = load_elems<C>(Q + k / 8 * w.ldq, ALL ? C : k < ke ? there_q : 0);
+            word[i] = load_elems<C>(Q + k / 8 * w.ldq, ALL ? C : k < ke ? there : 0);
             scale[i] = {};
-            if ((i & (steps - 1)) == 0) scale[i] = load_elems<4 * C>(S + (k0 + i * 32) / w.group * w.lds, ALL ? 4 * C : k0 + i * 32 < ke ? there_s : 0);
+            if ((i & (steps - 1)) == 0) scale[i] = load_elems<C>(S + (k0 + i * 32) / w.group * w.lds, ALL ? C : k0 + i * 32 < ke ? there : 0);
 #pragma unroll
             for (int t = 0; t < RT; ++t) x[i][t] = t * 16 + r < a.M ? load_eight(X + (t * 16 + r) * a.lda + k, ALL ? 8 : ke - k) : Eight<T>{};
         }
         v4f sum[RT][C] = {};
-        Elems<uint16_t, 4 * C> of = {};
+        Elems<uint16_t, C> of = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if ((i & (steps - 1)) == 0) of = scale[i];
@@ -130,7 +138,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear4_few(TileArgs a, Weig
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int p = PARTS - 1; p >= 0; --p) sum[t][q] = mma(f, part[t][p], sum[t][q]);
+                    for (int p = PARTS - 1; p >= 0; --p) sum[t][q] = mma(part[t][p], f, sum[t][q]);
             }
             if (((i + 1) & (steps - 1)) == 0)
 #pragma unroll
@@ -138,173 +146,230 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear4_few(TileArgs a, Weig
 #pragma unroll
                     for (int t = 0; t < RT; ++t) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[t][q][e] = fmaf(scale_value(of[e * C + q]), sum[t][q][e], acc[t][q][e]);
+                        for (int e = 0; e < 4; ++e) acc[t][q][e] = fmaf(scale_value(of[q]), sum[t][q][e], acc[t][q][e]);
                         sum[t][q] = v4f{};
                     }
         }
     };
     int64_t k = kb + wave * BLOCK4;
     if (n0 + WIDE <= a.N)
-        for (; k + BLOCK4 <= ke; k += FEW_WAVES * BLOCK4) block(k, std::true_type());
-    for (; k < ke; k += FEW_WAVES * BLOCK4) block(k, std::false_type());
-    leave_few<T, C, RT, GATED>(a, acc, lds, n0, 1.f / PLACE4<T>);
+        for (; k + BLOCK4 <= ke; k += WAVES * BLOCK4) block(k, std::true_type());
+    for (; k < ke; k += WAVES * BLOCK4) block(k, std::false_type());
+    leave_few<T, C, RT, GATED, WAVES, true>(a, acc, lds, n0, 1.f / PLACE4<T>);
 }
 
-// Many rows: 128 x 128 results of four wavefronts, 64 values of k at a time.  Words become 16-byte pieces of places on their way to LDS, where X and W lie by k alike (see Operand).  The sums over a
-// group are held apart from those over all of them.  fp32 elements: three planes of X, one stage; else two stages, of which one is fetched while the other is multiplied.
-template <typename T, bool DIRECT, bool GATED>
+// Many rows: 128 x 128 results of four wavefronts, 64 values of k at a time, through registers: words become 16-byte pieces of places on their way to LDS, where X and W lie by k alike (see Operand).
+// Two stages, of which one is fetched while the other is multiplied; fp32 elements are three planes of X, and one stage.  A lane has four rows of a column, so that a scale goes with all that it
+// has of a fragment.  STEPS: of 32 values of k in a group.
+template <typename T, bool GATED, int STEPS>
 __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w) {
     using U = Unit4<T>;
-    constexpr int BM = 128, BN = 128, THREADS = 256, PARTS = PARTS4<T>, BK = 64, PLANE = BM * 128, WORDS = BN * 8 / THREADS;
+    constexpr int E = Elem<T>::E, BM = 128, BN = 128, THREADS = 256, PARTS = PARTS4<T>, BK = 64, PLANE = BM * 128, WORDS = BN * 8 / THREADS;
     constexpr int STAGE = PARTS * PLANE + BN * 128, STAGES = PARTS == 1 ? 2 : 1, WIDE = GATED ? BN / 2 : BN;
     using OpX = Operand<U, BM, BY_K, THREADS>;
     using OpW = Operand<U, BN, BY_K, THREADS>;
-    __shared__ __attribute__((aligned(16))) char stage0[STAGE], stage1[STAGES == 2 ? STAGE : 16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, quarter = lane >> 4;
+    __shared__ __attribute__((aligned(16))) char lds[STAGES * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int tm, tn;
     tile_place(a, tm, tn);
     const int64_t m0 = (int64_t)tm * BM;
     const int n0 = tn * WIDE;
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
-    const T* const A = (const T*)a.A;
     const int wm = (wave / 2) * 64, wn = (wave % 2) * 64;
-    const int steps = w.group / 32;
-    // a column of the tile: of each 64 of a gated block's the first 32 are the gate's
-    auto column = [&](int c) -> int64_t {
+    // a column of the tile: of each 64 of a gated block's the first 32 are the gate's; the last one's where there is none
+    auto column = [&](int c) -> uint32_t {
         const int h = GATED ? n0 + c / 64 * 32 + c % 32 : n0 + c;
-        return (h < a.N ? h : a.N - 1) + (GATED && c % 64 >= 32 ? (int64_t)a.N : 0);
+        return (uint32_t)(h < a.N ? h : a.N - 1) + (GATED && c % 64 >= 32 ? (uint32_t)a.N : 0u);
     };
-    const uint32_t* const Q = w.Q + column(tid & (BN - 1));
+    // what a thread takes of a stage: words of one column, and eight elements at one place of XS rows
+    const uint32_t my_column = column(tid & (BN - 1)) * 4;        // bytes, as a scale's place below: 32 bits are enough for rows of up to 2^27
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int my_word = __builtin_amdgcn_readfirstlane(tid / BN);
+#else
+    const int my_word = tid / BN;
+#endif
     const int64_t last_word = (ke - 1) / 8;
+    constexpr int XS = BM * 8 / THREADS, VECS = 8 / E;
+    int my_row, my_piece;
+    OpX::at(tid, my_row, my_piece);                               // (32 rows on: the same piece)
+    const T* rows[XS];
+#pragma unroll
+    for (int i = 0; i < XS; ++i) {
+        const int64_t m = m0 + my_row + i * (THREADS / 8);
+        rows[i] = (const T*)a.A + (m < a.M ? m : a.M - 1) * a.lda;
+    }
     uint32_t word[WORDS];
-    auto send_words = [&](int64_t k) {
+    Words<T, E> x[XS][VECS];
+    auto fetch = [&](int64_t k) {
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) {
-            const int64_t j = k / 8 + (i * THREADS + tid) / BN;
-            word[i] = Q[(j < last_word ? j : last_word) * w.ldq];             // (X is 0 behind the last)
+            const int64_t j = k / 8 + i * (THREADS / BN) + my_word;
+            word[i] = *reinterpret_cast<const uint32_t*>((const char*)(w.Q + (j < last_word ? j : last_word) * w.ldq) + my_column);      // (X is 0 behind the last)
         }
+#pragma unroll
+        for (int v = 0; v < VECS; ++v)
+#pragma unroll
+            for (int i = 0; i < XS; ++i) x[i][v] = load_near<E>(rows[i], k + my_piece * 8 + v * E, a.K);
     };
-    auto put_words = [&](char* to) {
+    auto put = [&](char* to, int64_t k) {
+        if (k + BK > a.K)                                         // the end of the rows: zeros behind it
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            const int c = tid & (BN - 1), piece = (i * THREADS + tid) / BN;
-            *reinterpret_cast<Vec<U>*>(to + c * 128 + ((piece ^ (c & 7)) << 4)) = places_of<U>(word[i], PLACE4<T>);
-        }
-    };
-    constexpr int XS = BM * BK / (8 * THREADS);                               // eight elements of X at a time for each thread
-    Eight<T> x[XS];
-    auto send_rows = [&](int64_t k) {
+            for (int v = 0; v < VECS; ++v) {
+                const int by = settle_by<E>(k + my_piece * 8 + v * E, a.K);
 #pragma unroll
-        for (int i = 0; i < XS; ++i) {
-            int row, piece;
-            OpX::at(i * THREADS + tid, row, piece);
-            const int64_t m = m0 + row < a.M ? m0 + row : a.M - 1, at = k + piece * 8;
-            x[i] = load_eight(A + m * a.lda + at, at + 8 <= ke ? 8 : ke - at);
-        }
-    };
-    auto put_rows = [&](char* to) {
-#pragma unroll
-        for (int i = 0; i < XS; ++i) {
-            Vec<U> p[PARTS];
-            parts_of<T>(x[i], p);
-#pragma unroll
-            for (int k = 0; k < PARTS; ++k) *reinterpret_cast<Vec<U>*>(to + k * PLANE + (i * THREADS + tid) * 16) = p[k];
-        }
-    };
-    v4f acc[4][4] = {}, sum[4][4] = {};
-    auto multiply = [&](const char* stage, int64_t k0) {
-#pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            const int64_t k = k0 + step * 32;
-            Vec<U> p[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[j] = OpW::fragment(stage + PARTS * PLANE, wn + j * 16, step, lane);
-#pragma unroll
-            for (int part = PARTS - 1; part >= 0; --part) {
-                Vec<U> q[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = OpX::fragment(stage + part * PLANE, wm + i * 16, step, lane);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum[i][j] = mma(p[j], q[i], sum[i][j]);
+                for (int i = 0; i < XS; ++i) x[i][v] = __builtin_bit_cast(Words<T, E>, settle<E, T>(x[i][v], by));
             }
-            if (((k / 32 + 1) & (steps - 1)) == 0 || k + 32 >= ke) {           // the end of a group
-                if (k >= ke) continue;
-                const uint16_t* const S = w.S + k / w.group * w.lds;
+#pragma unroll
+        for (int i = 0; i < XS; ++i) {
+            Eight<T> e;
+#pragma unroll
+            for (int v = 0; v < VECS; ++v) e.v[v] = __builtin_bit_cast(Vec<T>, x[i][v]);
+            Vec<U> p[PARTS];
+            parts_of<T>(e, p);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) *reinterpret_cast<Vec<U>*>(to + part * PLANE + (i * THREADS + tid) * 16) = p[part];
+        }
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const int c = tid & (BN - 1), piece = i * (THREADS / BN) + my_word;
+            *reinterpret_cast<Vec<U>*>(to + PARTS * PLANE + c * 128 + ((piece ^ (c & 7)) << 4)) = places_of<U>(word[i], PLACE4<T>);
+        }
+    };
+    // the scales of a lane's column of each fragment
+    uint32_t scale_at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) scale_at[j] = column(wn + j * 16 + (lane & 15)) * 2;
+    constexpr int GROUPS = STEPS == 1 ? 2 : 1;                    // that have their scales in a stage
+    uint16_t scale[GROUPS][4];
+    auto send_scales = [&](int64_t k) {                           // of the groups that begin in the stage
+        if (STEPS == 4 && (k & 64)) return;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            int64_t at = k / (32 * STEPS) + g;
+            at = at < (ke - 1) / (32 * STEPS) ? at : (ke - 1) / (32 * STEPS);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scale[g][j] = *reinterpret_cast<const uint16_t*>((const char*)(w.S + at * w.lds) + scale_at[j]);
+        }
+    };
+    // Groups that end in the stage they begin in need the sums of one column of fragments at a time; of fp32 elements, whose sums are three products each, every 32 values of k are a group.
+    constexpr int TOGETHER = PARTS == 3 ? 1 : STEPS;
+    constexpr bool LONG = TOGETHER == 4;
+    v4f acc[4][4] = {}, sum[4][LONG ? 4 : 1] = {};
+    auto add = [&](int j, const v4f (&of)[4], uint16_t bits) {
+        const float s = scale_value(bits);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s, of[i][e], acc[i][j][e]);
+#if defined(__HIP_DEVICE_COMPILE__)
+        // here and not behind the branch that follows the stage, where the compiler would put all of it at once, and the matrix units wait
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[i][j]));
+#endif
+    };
+    auto multiply = [&](const char* stage, int64_t k0) {
+        uint16_t of[GROUPS][4];
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) of[g][j] = scale[g][j];
+        if (k0 + BK < ke) send_scales(k0 + BK);
+        auto row_fragments = [&](int part, int step, Vec<U> (&q)[4]) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = OpX::fragment(stage + part * PLANE, wm + i * 16, step, lane);
+        };
+        auto columns = [&](int j, int step) { return OpW::fragment(stage + PARTS * PLANE, wn + j * 16, step, lane); };
+        if constexpr (LONG) {
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                Vec<U> q[4];
+                row_fragments(0, step, q);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float s[4];
+                    const Vec<U> p = columns(j, step);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[e] = scale_value(S[column(wn + j * 16 + quarter * 4 + e)]);
+                    for (int i = 0; i < 4; ++i) sum[i][j] = mma(q[i], p, sum[i][j]);
+                }
+            }
+            if ((k0 & 64) || k0 + BK >= ke)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v4f one[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[e], sum[i][j][e], acc[i][j][e]);
+                        one[i] = sum[i][j];
                         sum[i][j] = v4f{};
                     }
+                    add(j, one, of[0][j]);
+                }
+        } else {
+            constexpr int AT_ONCE = TOGETHER;                     // steps
+#pragma unroll
+            for (int step = 0; step < 2; step += AT_ONCE) {
+                Vec<U> q[AT_ONCE][PARTS][4], p[AT_ONCE][4];
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) p[u][j] = columns(j, step + u);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) row_fragments(part, step + u, q[u][part]);
+                }
+                v4f one[2][4];
+#pragma unroll
+                for (int j = 0; j < 5; ++j) {                     // a column's sums leave while the next one's products are made
+                    if (j < 4) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) one[j & 1][i] = v4f{};
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+                            for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) one[j & 1][i] = mma(q[u][part][i], p[u][j], one[j & 1][i]);
+                    }
+                    if (j > 0) add(j - 1, one[(j - 1) & 1], of[STEPS == 1 ? step : 0][j - 1]);
+                    KEEP_ORDER();
                 }
             }
         }
     };
-    auto fetch = [&](char* stage, int64_t k) {
-        send_words(k);
-        if (DIRECT && k + BK <= ke) OpX::direct((const U*)A, a.lda, m0, a.M, k, stage, tid);
-        else send_rows(k);
-    };
-    auto put = [&](char* stage, int64_t k) {
-        if (!(DIRECT && k + BK <= ke)) put_rows(stage);
-        put_words(stage + PARTS * PLANE);
-        if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    fetch(stage0, kb);
-    put(stage0, kb);
+    char* stage = lds;
     int64_t k = kb;
-    if constexpr (STAGES == 2) {
-        while (true) {
-            const bool more = k + BK < ke;
-            if (more) fetch(stage1, k + BK);
-            multiply(stage0, k);
-            if (!more) break;
-            k += BK;
-            put(stage1, k);
-            const bool again = k + BK < ke;
-            if (again) fetch(stage0, k + BK);
-            multiply(stage1, k);
-            if (!again) break;
-            k += BK;
-            put(stage0, k);
-        }
-    } else {
-        while (true) {
-            const bool more = k + BK < ke;
-            if (more) fetch(stage0, k + BK);
-            multiply(stage0, k);
-            if (!more) break;
-            k += BK;
-            __syncthreads();
-            put(stage0, k);
-        }
+    send_scales(k);
+    fetch(k);
+    put(stage, k);
+    __syncthreads();
+    while (true) {
+        const bool more = k + BK < ke;
+        if (more) fetch(k + BK);
+        multiply(stage, k);
+        if (!more) break;
+        k += BK;
+        if (STAGES == 1) __syncthreads();
+        else stage = stage == lds ? lds + STAGE : lds;
+        put(stage, k);
+        __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] *= 1.f / PLACE4<T>;
     constexpr int PART = 64 * 64 * 4;
-    static_assert(STAGES == 2 ? 2 * PART <= STAGE : 4 * PART <= STAGE, "results have room");
+    static_assert(4 * PART <= STAGES * STAGE, "results have room");
     __syncthreads();
-    char* const mine = STAGES == 2 ? (wave < 2 ? stage0 : stage1) + (wave & 1) * PART : stage0 + wave * PART;
-    if constexpr (GATED) leave_gated<T, 4, 4, 1, false>(a, acc, mine, m0 + wm, n0 + wn / 2, lane);
-    else leave_tile<T, 4, 4, 1, false, false>(a, acc, mine, m0 + wm, n0 + wn, lane);
+    char* const mine = lds + wave * PART;
+    if constexpr (GATED) leave_gated<T, 4, 4, 1, false, true>(a, acc, mine, m0 + wm, n0 + wn / 2, lane);
+    else leave_tile<T, 4, 4, 1, false, false, true>(a, acc, mine, m0 + wm, n0 + wn, lane);
 }
 
 template <typename T, int C, int RT, bool GATED>
 static int launch_few4(TileArgs a, const Weights4& w, hipStream_t s) {
-    constexpr int WIDE = GATED ? 8 * C : 16 * C, ALL = BLOCK4 * FEW_WAVES;
+    constexpr int WAVES = C == 1 && RT == 1 ? 16 : 8;
+    constexpr int WIDE = GATED ? 8 * C : 16 * C, ALL = BLOCK4 * WAVES;
     const int strips = (a.N + WIDE - 1) / WIDE;
+    constexpr int ROWS = 16 * RT;
     int64_t splits = 1;
-    if (strips < FEW_STRIPS) {
+    if (strips < FEW_STRIPS && a.M <= ROWS) {
         splits = 128 / strips;
         const int64_t most = (a.K + ALL - 1) / ALL;
         if (splits > most) splits = most;
@@ -318,8 +383,17 @@ static int launch_few4(TileArgs a, const Weights4& w, hipStream_t s) {
         GCN_TRY(lease.get(&p, (size_t)splits * a.M * a.N * (GATED ? 8 : 4), s));
         a.part = (float*)p;
     }
-    launch_lds<k_linear4_few<T, C, RT, GATED>>(dim3((unsigned)((strips + 7) / 8 * 8), (unsigned)splits), FEW_WAVES * 64, few_lds<T, C, RT>(), s, a, w, strips);
-    GCN_LAUNCH_CHECK();
+    for (int64_t m = 0; m < a.M; m += 65535 * ROWS) {             // (a launch has so many workgroups along a dimension; more than one take whole sums)
+        TileArgs b = a;
+        b.A = (const T*)a.A + m * a.lda;
+        b.Y = (T*)a.Y + m * a.ldy;
+        if (a.R) b.R = (const T*)a.R + m * a.ldr;
+        b.M = a.M - m;
+        const int64_t blocks_m = (b.M + ROWS - 1) / ROWS;
+        launch_lds<k_linear4_few<T, C, RT, WAVES, GATED>>(dim3((unsigned)((strips + 7) / 8 * 8), (unsigned)splits, (unsigned)(blocks_m < 65535 ? blocks_m : 65535)), WAVES * 64,
+                                                          few_lds<C, RT, WAVES>(), s, b, w, strips);
+        GCN_LAUNCH_CHECK();
+    }
     return splits > 1 ? launch_join<T, GATED>(a, (int)splits, s) : GCN_OK;
 }
 
@@ -341,15 +415,17 @@ static int launch_tile4(TileArgs a, const Weights4& w, hipStream_t s) {
         a.part = (float*)p;
     }
     const dim3 grid((unsigned)(tm * tn), (unsigned)splits);
-    if (sizeof(T) == 2 && whole_pieces<T, BY_K>(a.A, a.lda, a.K)) hipLaunchKernelGGL((k_linear4_tile<T, sizeof(T) == 2, GATED>), grid, dim3(256), 0, s, a, w);
-    else hipLaunchKernelGGL((k_linear4_tile<T, false, GATED>), grid, dim3(256), 0, s, a, w);
+    auto launch = [&](auto steps) { hipLaunchKernelGGL((k_linear4_tile<T, GATED, decltype(steps)::value>), grid, dim3(256), 0, s, a, w); };
+    if (w.group == 32) launch(std::integral_constant<int, 1>());
+    else if (w.group == 64) launch(std::integral_constant<int, 2>());
+    else launch(std::integral_constant<int, 4>());
     GCN_LAUNCH_CHECK();
     return splits > 1 ? launch_join<T, GATED>(a, splits, s) : GCN_OK;
 }
 
 template <typename T, bool GATED>
 static int linear4_impl(const TileArgs& a, const Weights4& w, hipStream_t s) {
-    if (a.M > 32) return launch_tile4<T, GATED>(a, w, s);
+    if (a.M > 32 && a.K >= Elem<T>::E) return launch_tile4<T, GATED>(a, w, s);
     const int64_t cus = device_info().cus, cols = GATED ? 2 * (int64_t)a.N : a.N;
     const int c = cols >= 64 * cus ? 4 : cols >= 32 * cus ? 2 : 1;            // as k_linear_few: the widest strips that are one for every compute unit
     if (a.M <= 16) return c == 4 ? launch_few4<T, 4, 1, GATED>(a, w, s) : c == 2 ? launch_few4<T, 2, 1, GATED>(a, w, s) : launch_few4<T, 1, 1, GATED>(a, w, s);

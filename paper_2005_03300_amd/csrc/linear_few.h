@@ -10,12 +10,12 @@ constexpr int FEW_WAVES = 16;
 // 5.0: the second launch costs more than it saves); 752 columns, 47 strips, k of 4096 9.5 and 10.0 (11.6, 13.7).  With 64 strips the other way round from k of about 8192 on:
 // 1024 columns, k of 16384 23.8 with a split, 37.4 without (30.4, 49.9), of 4096 8.3 and 8.0 (12.1, 14.8), of 1024 4.1 and 4.1 (6.5, 5.0).
 constexpr int FEW_STRIPS = 48;
-template <typename T, int C, int RT>
-constexpr size_t few_lds() { return (size_t)FEW_WAVES * RT * 16 * (16 * C + 4) * 4; }
+template <int C, int RT, int WAVES = FEW_WAVES>
+constexpr size_t few_lds() { return (size_t)WAVES * RT * 16 * (16 * C + 4) * 4; }
 
-// The wavefronts' results, of lane (r, quarter) those of row r (of each 16) and columns (4 quarter + e) C + q of the strip from n0 on, added in order in LDS, times `times`, and what the layer does
-// with them.
-template <typename T, int C, int RT, bool GATED>
+// The wavefronts' results, of lane (r, quarter) those of row r (of each 16) and columns (4 quarter + e) C + q of the strip from n0 on (TURNED: of rows 4 quarter + e and columns r C + q), added in
+// order in LDS, times `times`, and what the layer does with them.
+template <typename T, int C, int RT, bool GATED, int WAVES = FEW_WAVES, bool TURNED = false>
 __device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT][C], char* lds, int n0, float times = 1.f) {
     constexpr int E = Elem<T>::E, ROW = 16 * C + 4, WIDE = GATED ? 8 * C : 16 * C;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
@@ -25,20 +25,20 @@ __device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT
 #pragma unroll
         for (int q = 0; q < C; ++q)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mine[(t * 16 + r) * ROW + (quarter * 4 + e) * C + q] = acc[t][q][e];
+            for (int e = 0; e < 4; ++e) mine[TURNED ? (t * 16 + quarter * 4 + e) * ROW + r * C + q : (t * 16 + r) * ROW + (quarter * 4 + e) * C + q] = acc[t][q][e];
     __syncthreads();
     // a thread for each result; the sum takes the place of the first wavefront's, which no other thread reads
-    for (int i = threadIdx.x; i < RT * 16 * 16 * C; i += FEW_WAVES * 64) {
+    for (int i = threadIdx.x; i < RT * 16 * 16 * C; i += WAVES * 64) {
         float* const at = (float*)lds + i / (16 * C) * ROW + i % (16 * C);
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) sum += at[w * RT * 16 * ROW];
+        for (int w = 0; w < WAVES; ++w) sum += at[w * RT * 16 * ROW];
         *at = sum * times;
     }
     __syncthreads();
     constexpr int PIECES = WIDE / E;
     if constexpr (WIDE % E == 0) {
-        for (int i = threadIdx.x; i < RT * 16 * PIECES; i += FEW_WAVES * 64) {
+        for (int i = threadIdx.x; i < RT * 16 * PIECES; i += WAVES * 64) {
             const int row = i / PIECES, c = i % PIECES * E, count = a.N - n0 - c;
             if (row >= a.M || count <= 0) continue;
             float d[GATED ? 2 : 1][E];

@@ -70,7 +70,7 @@ static int launch_few(TileArgs a, hipStream_t s) {
         GCN_TRY(lease.get(&p, (size_t)splits * a.M * a.N * (GATED ? 8 : 4), s));
         a.part = (float*)p;
     }
-    launch_lds<k_linear_few<T, C, RT, GATED>>(dim3((unsigned)((strips + 7) / 8 * 8), (unsigned)splits), FEW_WAVES * 64, few_lds<T, C, RT>(), s, a, strips);
+    launch_lds<k_linear_few<T, C, RT, GATED>>(dim3((unsigned)((strips + 7) / 8 * 8), (unsigned)splits), FEW_WAVES * 64, few_lds<C, RT>(), s, a, strips);
     GCN_LAUNCH_CHECK();
     return splits > 1 ? launch_join<T, GATED>(a, (int)splits, s) : GCN_OK;
 }

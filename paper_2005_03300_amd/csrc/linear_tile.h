@@ -313,21 +313,34 @@ __device__ __forceinline__ void tile_place(const TileArgs& a, int& tm, int& tn) 
 
 // A wavefront's results, 16 FM rows from m0 and 16 FN columns from n0 on, leave through LDS, its own part `mine` of it, in PHASES: what the matrix unit leaves with a
 // lane are four columns of a row, and whole rows of the wavefront's tile go out together, 16 bytes per lane.  The pieces of a row are moved about by the row, so that
-// the lanes' writes meet all banks.  CUT_M, CUT_N: pieces that the end of a dimension cuts were taken from its last whole one.
-template <typename T, int FM, int FN, int PHASES, bool CUT_M, bool CUT_N>
+// the lanes' writes meet all banks.  CUT_M, CUT_N: pieces that the end of a dimension cuts were taken from its last whole one.  TURNED: a lane has four rows of a column instead.
+template <int FM, int FN, int FP, bool TURNED>
+__device__ __forceinline__ void results_to_lds(const v4f (&acc)[FM][FN], int first, char* mine, int lane) {
+    constexpr int PIECES = FN * 4;
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+            if constexpr (TURNED) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int row = i * 16 + (lane >> 4) * 4 + e, c = j * 16 + (lane & 15);
+                    *reinterpret_cast<float*>(mine + row * (PIECES * 16) + (((c >> 2) ^ (row & (PIECES - 1))) << 4) + (c & 3) * 4) = acc[first + i][j][e];
+                }
+            } else {
+                const int row = i * 16 + (lane & 15);
+                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[first + i][j];
+            }
+        }
+}
+template <typename T, int FM, int FN, int PHASES, bool CUT_M, bool CUT_N, bool TURNED = false>
 __device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[FM][FN], char* mine, int64_t m0, int n0, int lane) {
     constexpr int E = Elem<T>::E, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4;
     static_assert(FM % PHASES == 0, "whole phases");
     float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N : nullptr;
 #pragma unroll
     for (int ph = 0; ph < PHASES; ++ph) {
-#pragma unroll
-        for (int i = 0; i < FP; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int row = i * 16 + (lane & 15);
-                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[ph * FP + i][j];
-            }
+        results_to_lds<FM, FN, FP, TURNED>(acc, ph * FP, mine, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         constexpr int LANES = FN * 16 / E, STEP = 64 / LANES;     // lanes of a row, rows at a time
         const int c = (lane % LANES) * E, n = n0 + c, count = a.N - n;
@@ -395,7 +408,7 @@ __device__ __forceinline__ void leave_tile(const TileArgs& a, const v4f (&acc)[F
 }
 
 // The same for a gated block: of a wavefront's 16 FN columns the first half are the gate's, the others those of the same 8 FN columns of H from n0 on.
-template <typename T, int FM, int FN, int PHASES, bool CUT_N>
+template <typename T, int FM, int FN, int PHASES, bool CUT_N, bool TURNED = false>
 __device__ __forceinline__ void leave_gated(const TileArgs& a, const v4f (&acc)[FM][FN], char* mine, int64_t m0, int n0, int lane) {
     constexpr int E = Elem<T>::E, FP = FM / PHASES, ROWS = FP * 16, PIECES = FN * 4, HALF = FN * 8;
     static_assert(FM % PHASES == 0 && FN % 2 == 0, "whole phases, two halves");
@@ -404,13 +417,7 @@ __device__ __forceinline__ void leave_gated(const TileArgs& a, const v4f (&acc)[
     float* const part = a.part ? a.part + (int64_t)blockIdx.y * a.M * a.N * 2 : nullptr;
 #pragma unroll
     for (int ph = 0; ph < PHASES; ++ph) {
-#pragma unroll
-        for (int i = 0; i < FP; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int row = i * 16 + (lane & 15);
-                *reinterpret_cast<v4f*>(mine + row * (PIECES * 16) + (((j * 4 + (lane >> 4)) ^ (row & (PIECES - 1))) << 4)) = acc[ph * FP + i][j];
-            }
+        results_to_lds<FM, FN, FP, TURNED>(acc, ph * FP, mine, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const int c = (lane % LANES) * E, n = n0 + c, count = a.N - n;
         const bool shifted = CUT_N && count < E && a.N >= E;      // as in leave_tile: a piece that the end cut holds the last whole one
