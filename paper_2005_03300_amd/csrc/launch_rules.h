@@ -176,4 +176,32 @@ inline int splits_of_4(int64_t tiles, int64_t results, int64_t K, bool fp32, int
     return best;
 }
 
+// A product of few rows with weights held in 4 bits: rows in 16s that a wavefront takes at a time (0: too many, tiles), columns of a lane, shares of the sum over k.  A workgroup has a strip of 16
+// columns for each column of a lane, all of k or a share of it.
+//  - Strips as narrow as still give no compute unit a second one, up to 8 columns a lane: a second round costs as much as the first.  Microseconds of bf16 with 1, 2, 4 and 8 columns a lane, k of 8192,
+//    1 row and 16: 8192 columns 12.5 11.2 12.5 15.8 and 22.9 13.4 15.5 20.8, 14336 columns 22.0 17.8 13.3 23.6 and 39.7 26.4 17.2 26.1, 28672 columns 36.2 30.6 24.4 23.2 and 70.5 48.7 34.1 26.6.
+//  - The rows of X are read again for every strip, 128 bytes of 64 rows for each 32 of codes that a strip of 64 columns has.  So from 17 rows on, and from 9 on where strips would be 16 columns wide and
+//    k is long, strips are 64 wide and the sum is shared instead, 64 rows and 4096 columns, k of 4096 and 14336, 20 and 59 -> 18 and 31, 16 rows and k of 14336 19 -> 15; with fewer rows the second
+//    launch costs more (1 row 11.6 -> 13.5).
+//  - 64 rows as tiles took 25 and 39 there, 57 with 14336 columns and k of 8192 (so 42).
+struct Few4 {
+    int rows, columns;
+    int64_t splits;
+};
+constexpr int few4_waves(int columns, int rows) { return columns == 1 && rows == 1 ? 16 : 8; }
+inline Few4 few4_choice(int64_t M, int64_t cols, int64_t K, bool fp32, int64_t cus) {
+    Few4 f{M <= 16 ? 1 : M <= 32 ? 2 : 4, 1, 1};
+    if (M > 64 || (fp32 && M > 32)) f.rows = 0;
+    const int widest = f.rows == 1 || (f.rows == 2 && !fp32) ? 8 : 4;
+    const bool shared = ((f.rows != 1 && K >= 4096) || (M > 8 && K >= 8192 && cols <= 16 * cus)) && cols <= 64 * cus;
+    if (shared) f.columns = 4;
+    else
+        while (f.columns < widest && cols > 16 * f.columns * cus) f.columns *= 2;
+    const int64_t strips = (cols + 16 * f.columns - 1) / (16 * f.columns), all = 128 * few4_waves(f.columns, f.rows), most = (K + all - 1) / all;
+    if (shared) f.splits = cus / strips;
+    else if (strips < 48) f.splits = 128 / strips;                // as k_linear_few
+    f.splits = f.splits < 1 ? 1 : f.splits > most ? most : f.splits;
+    return f;
+}
+
 }  // namespace gcn

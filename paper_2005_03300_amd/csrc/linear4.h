@@ -84,22 +84,31 @@ __device__ __forceinline__ void parts_of(const Eight<T>& x, Vec<Unit4<T>> (&p)[P
 #define KEEP_ORDER() (void)0
 #endif
 
+// The number of the wavefront in its workgroup, as the scalar that it is.
+__device__ __forceinline__ int wave_number() {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+#else
+    return 0;
+#endif
+}
+
 constexpr int BLOCK4 = 128;           // values of k that a wavefront takes at a time: a whole number of groups
 
 // Few rows: the strips and their end are those of k_linear_few.  A lane loads C neighbouring words of four rows of words, which are C fragments of four steps of 32 values of k, and has the results of
 // the same columns, so that it needs their scales and no others.  blockIdx.z: which 16 RT rows.
 template <typename T, int C, int RT, int WAVES, bool GATED>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT == 1) ? 4 : 2) void k_linear4_few(TileArgs a, Weights4 w, int strips) {
+__global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT == 1 && C <= 4) ? 4 : 2) void k_linear4_few(TileArgs a, Weights4 w, int strips) {
     using U = Unit4<T>;
     constexpr int PARTS = PARTS4<T>, WIDE = GATED ? 8 * C : 16 * C;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = wave_number(), r = lane & 15, quarter = lane >> 4;
     const int per = (strips + 7) / 8, strip = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if (strip >= strips || (int)(blockIdx.x >> 3) >= per) return;
     const int n0 = strip * WIDE, n = n0 + (GATED ? (r & 7) * C : r * C);
     const int there = a.N - n;                                    // of the lane's C columns
     const int64_t c = n + (GATED && r >= 8 ? (int64_t)a.N : 0);
-    const uint32_t* const Q = w.Q + c;
+    const uint32_t* const Q = w.Q + quarter * w.ldq + c;          // of the first step's word
     const uint16_t* const S = w.S + c;
     const int64_t m0 = (int64_t)blockIdx.z * (16 * RT);
     const T* const X = (const T*)a.A + m0 * a.lda;
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT ==
     a.Y = (T*)a.Y + m0 * a.ldy;
     if (a.R) a.R = (const T*)a.R + m0 * a.ldr;
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
-    const int steps = w.group / 32;
+    const int shift = w.group == 32 ? 5 : w.group == 64 ? 6 : 7, steps = 1 << (shift - 5);
     v4f acc[RT][C] = {};
     // `whole`: all of the block's k and all of the strip's columns are there
     auto block = [&](int64_t k0, auto whole) {
@@ -118,9 +127,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT ==
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t k = k0 + i * 32 + quarter * 8;
-            word[i] = load_elems<C>(Q + k / 8 * w.ldq, ALL ? C : k < ke ? there : 0);
+            word[i] = load_elems<C>(Q + (k0 / 8 + i * 4) * w.ldq, ALL ? C : k < ke ? there : 0);
             scale[i] = {};
-            if ((i & (steps - 1)) == 0) scale[i] = load_elems<C>(S + (k0 + i * 32) / w.group * w.lds, ALL ? C : k0 + i * 32 < ke ? there : 0);
+            if ((i & (steps - 1)) == 0) scale[i] = load_elems<C>(S + ((k0 + i * 32) >> shift) * w.lds, ALL ? C : k0 + i * 32 < ke ? there : 0);
 #pragma unroll
             for (int t = 0; t < RT; ++t) x[i][t] = t * 16 + r < a.M ? load_eight(X + (t * 16 + r) * a.lda + k, ALL ? 8 : ke - k) : Eight<T>{};
         }
@@ -183,11 +192,7 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
     };
     // what a thread takes of a stage: words of one column, and eight elements at one place of XS rows
     const uint32_t my_column = column(tid & (BN - 1)) * 4;        // bytes, as a scale's place below: 32 bits are enough for rows of up to 2^27
-#if defined(__HIP_DEVICE_COMPILE__)
-    const int my_word = __builtin_amdgcn_readfirstlane(tid / BN);
-#else
-    const int my_word = tid / BN;
-#endif
+    const int my_word = wave_number() / (BN / 64);
     const int64_t last_word = (ke - 1) / 8;
     constexpr int XS = BM * 8 / THREADS, VECS = 8 / E;
     int my_row, my_piece;
@@ -363,17 +368,10 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
 }
 
 template <typename T, int C, int RT, bool GATED>
-static int launch_few4(TileArgs a, const Weights4& w, hipStream_t s) {
-    constexpr int WAVES = C == 1 && RT == 1 ? 16 : 8;
-    constexpr int WIDE = GATED ? 8 * C : 16 * C, ALL = BLOCK4 * WAVES;
+static int launch_few4(TileArgs a, const Weights4& w, int64_t splits, hipStream_t s) {
+    constexpr int WAVES = few4_waves(C, RT), WIDE = GATED ? 8 * C : 16 * C, ALL = BLOCK4 * WAVES, ROWS = 16 * RT;
     const int strips = (a.N + WIDE - 1) / WIDE;
-    constexpr int ROWS = 16 * RT;
-    int64_t splits = 1;
-    if (strips < FEW_STRIPS && a.M <= ROWS) {
-        splits = 128 / strips;
-        const int64_t most = (a.K + ALL - 1) / ALL;
-        if (splits > most) splits = most;
-    }
+    if (a.M > ROWS) splits = 1;
     const int64_t blocks = (a.K + ALL - 1) / ALL;
     a.k_share = (blocks + splits - 1) / splits * ALL;
     splits = (a.K + a.k_share - 1) / a.k_share;
@@ -425,11 +423,21 @@ static int launch_tile4(TileArgs a, const Weights4& w, hipStream_t s) {
 
 template <typename T, bool GATED>
 static int linear4_impl(const TileArgs& a, const Weights4& w, hipStream_t s) {
-    if (a.M > 32 && a.K >= Elem<T>::E) return launch_tile4<T, GATED>(a, w, s);
-    const int64_t cus = device_info().cus, cols = GATED ? 2 * (int64_t)a.N : a.N;
-    const int c = cols >= 64 * cus ? 4 : cols >= 32 * cus ? 2 : 1;            // as k_linear_few: the widest strips that are one for every compute unit
-    if (a.M <= 16) return c == 4 ? launch_few4<T, 4, 1, GATED>(a, w, s) : c == 2 ? launch_few4<T, 2, 1, GATED>(a, w, s) : launch_few4<T, 1, 1, GATED>(a, w, s);
-    return c == 4 ? launch_few4<T, 4, 2, GATED>(a, w, s) : c == 2 ? launch_few4<T, 2, 2, GATED>(a, w, s) : launch_few4<T, 1, 2, GATED>(a, w, s);
+    constexpr bool FP32 = sizeof(T) == 4;
+    const Few4 f = few4_choice(a.M, GATED ? 2 * (int64_t)a.N : a.N, a.K, FP32, device_info().cus);
+    if (f.rows == 0 && a.K >= Elem<T>::E) return launch_tile4<T, GATED>(a, w, s);
+    auto by_columns = [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        if constexpr (RT == 1 || (RT == 2 && !FP32))
+            if (f.columns == 8) return launch_few4<T, 8, RT, GATED>(a, w, f.splits, s);
+        if (f.columns >= 4) return launch_few4<T, 4, RT, GATED>(a, w, f.splits, s);
+        if (f.columns == 2) return launch_few4<T, 2, RT, GATED>(a, w, f.splits, s);
+        return launch_few4<T, 1, RT, GATED>(a, w, f.splits, s);
+    };
+    if (f.rows == 1) return by_columns(std::integral_constant<int, 1>());
+    if constexpr (!FP32)
+        if (f.rows == 4) return by_columns(std::integral_constant<int, 4>());
+    return by_columns(std::integral_constant<int, 2>());
 }
 
 }  // namespace gcn
