@@ -183,7 +183,8 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
     tile_place(a, tm, tn);
     const int64_t m0 = (int64_t)tm * BM;
     const int n0 = tn * WIDE;
-    const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
+    // (k is 2^27 at most)
+    const int K = (int)a.K, kb = (int)(blockIdx.y * a.k_share), ke = kb + a.k_share < a.K ? (int)(kb + a.k_share) : K;
     const int wm = (wave / 2) * 64, wn = (wave % 2) * 64;
     // a column of the tile: of each 64 of a gated block's the first 32 are the gate's; the last one's where there is none
     auto column = [&](int c) -> uint32_t {
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
     // what a thread takes of a stage: words of one column, and eight elements at one place of XS rows
     const uint32_t my_column = column(tid & (BN - 1)) * 4;        // bytes, as a scale's place below: 32 bits are enough for rows of up to 2^27
     const int my_word = wave_number() / (BN / 64);
-    const int64_t last_word = (ke - 1) / 8;
+    const int last_word = (ke - 1) >> 3, last_group = (ke - 1) / (32 * STEPS);
     constexpr int XS = BM * 8 / THREADS, VECS = 8 / E;
     int my_row, my_piece;
     OpX::at(tid, my_row, my_piece);                               // (32 rows on: the same piece)
@@ -203,32 +204,54 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
         const int64_t m = m0 + my_row + i * (THREADS / 8);
         rows[i] = (const T*)a.A + (m < a.M ? m : a.M - 1) * a.lda;
     }
-    uint32_t word[WORDS];
-    Words<T, E> x[XS][VECS];
-    auto fetch = [&](int64_t k) {
+    // the scales of a lane's column of each fragment
+    uint32_t scale_at[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) scale_at[j] = column(wn + j * 16 + (lane & 15)) * 2;
+    constexpr int GROUPS = STEPS == 1 ? 2 : 1;                    // that a stage has scales of
+    // What is on its way: of two stages, with fp32 elements, which have the registers of one only, of one
+    constexpr int SETS = PARTS == 1 ? 2 : 1;
+    uint32_t word[SETS][WORDS];
+    Words<T, E> x[SETS][XS][VECS];
+    uint16_t scale[SETS][GROUPS][4];
+    auto fetch = [&](auto of_set, int k) {
+        constexpr int s = decltype(of_set)::value;
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) {
-            const int64_t j = k / 8 + i * (THREADS / BN) + my_word;
-            word[i] = *reinterpret_cast<const uint32_t*>((const char*)(w.Q + (j < last_word ? j : last_word) * w.ldq) + my_column);      // (X is 0 behind the last)
+            int j = (k >> 3) + i * (THREADS / BN) + my_word;
+            j = j < last_word ? j : last_word;                    // (X is 0 behind it)
+            word[s][i] = *reinterpret_cast<const uint32_t*>((const char*)(w.Q + j * w.ldq) + my_column);
         }
 #pragma unroll
-        for (int v = 0; v < VECS; ++v)
+        for (int v = 0; v < VECS; ++v) {
+            int at = k + my_piece * 8 + v * E;
+            at = at < K - E ? at : K - E;                         // as load_near
 #pragma unroll
-            for (int i = 0; i < XS; ++i) x[i][v] = load_near<E>(rows[i], k + my_piece * 8 + v * E, a.K);
+            for (int i = 0; i < XS; ++i) x[s][i][v] = load_near<E>(rows[i] + at, 0, E);
+        }
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            int at = k / (32 * STEPS) + g;
+            at = at < last_group ? at : last_group;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) scale[s][g][j] = *reinterpret_cast<const uint16_t*>((const char*)(w.S + at * w.lds) + scale_at[j]);
+        }
     };
-    auto put = [&](char* to, int64_t k) {
-        if (k + BK > a.K)                                         // the end of the rows: zeros behind it
+    float of[GROUPS][4];                                          // the scales of the stage in LDS
+    auto put = [&](auto of_set, char* to, int k) {
+        constexpr int s = decltype(of_set)::value;
+        if (k + BK > K)                                           // the end of the rows: zeros behind it
 #pragma unroll
             for (int v = 0; v < VECS; ++v) {
-                const int by = settle_by<E>(k + my_piece * 8 + v * E, a.K);
+                const int by = settle_by<E>(k + my_piece * 8 + v * E, K);
 #pragma unroll
-                for (int i = 0; i < XS; ++i) x[i][v] = __builtin_bit_cast(Words<T, E>, settle<E, T>(x[i][v], by));
+                for (int i = 0; i < XS; ++i) x[s][i][v] = __builtin_bit_cast(Words<T, E>, settle<E, T>(x[s][i][v], by));
             }
 #pragma unroll
         for (int i = 0; i < XS; ++i) {
             Eight<T> e;
 #pragma unroll
-            for (int v = 0; v < VECS; ++v) e.v[v] = __builtin_bit_cast(Vec<T>, x[i][v]);
+            for (int v = 0; v < VECS; ++v) e.v[v] = __builtin_bit_cast(Vec<T>, x[s][i][v]);
             Vec<U> p[PARTS];
             parts_of<T>(e, p);
 #pragma unroll
@@ -237,31 +260,23 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) {
             const int c = tid & (BN - 1), piece = i * (THREADS / BN) + my_word;
-            *reinterpret_cast<Vec<U>*>(to + PARTS * PLANE + c * 128 + ((piece ^ (c & 7)) << 4)) = places_of<U>(word[i], PLACE4<T>);
+            *reinterpret_cast<Vec<U>*>(to + PARTS * PLANE + c * 128 + ((piece ^ (c & 7)) << 4)) = places_of<U>(word[s][i], PLACE4<T>);
         }
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                of[g][j] = scale_value(scale[s][g][j]);
+#if defined(__HIP_DEVICE_COMPILE__)
+                asm volatile("" : "+v"(of[g][j]));                // now, or the next ones would have to be copied before they arrive
+#endif
+            }
     };
-    // the scales of a lane's column of each fragment
-    uint32_t scale_at[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) scale_at[j] = column(wn + j * 16 + (lane & 15)) * 2;
-    constexpr int GROUPS = STEPS == 1 ? 2 : 1;                    // that have their scales in a stage
-    uint16_t scale[GROUPS][4];
-    auto send_scales = [&](int64_t k) {                           // of the groups that begin in the stage
-        if (STEPS == 4 && (k & 64)) return;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            int64_t at = k / (32 * STEPS) + g;
-            at = at < (ke - 1) / (32 * STEPS) ? at : (ke - 1) / (32 * STEPS);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) scale[g][j] = *reinterpret_cast<const uint16_t*>((const char*)(w.S + at * w.lds) + scale_at[j]);
-        }
-    };
-    // Groups that end in the stage they begin in need the sums of one column of fragments at a time; of fp32 elements, whose sums are three products each, every 32 values of k are a group.
-    constexpr int TOGETHER = PARTS == 3 ? 1 : STEPS;
-    constexpr bool LONG = TOGETHER == 4;
-    v4f acc[4][4] = {}, sum[4][LONG ? 4 : 1] = {};
-    auto add = [&](int j, const v4f (&of)[4], uint16_t bits) {
-        const float s = scale_value(bits);
+    // The sums of a group leave with its stage, or with its 32 values of k: longer groups would need a second set of all sums (128 values of k at a time: 93 us at 2048 x 4096 x 4096, 64 at a
+    // time 86).  Those of fp32 elements, three products each, every 32.
+    constexpr int AT_ONCE = PARTS == 3 || STEPS == 1 ? 1 : 2;     // steps
+    v4f acc[4][4] = {};
+    auto add = [&](int j, const v4f (&of)[4], float s) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -272,89 +287,60 @@ __global__ __launch_bounds__(256, 2) void k_linear4_tile(TileArgs a, Weights4 w)
         for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(acc[i][j]));
 #endif
     };
-    auto multiply = [&](const char* stage, int64_t k0) {
-        uint16_t of[GROUPS][4];
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) of[g][j] = scale[g][j];
-        if (k0 + BK < ke) send_scales(k0 + BK);
+    auto multiply = [&](const char* stage, int k0) {
         auto row_fragments = [&](int part, int step, Vec<U> (&q)[4]) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) q[i] = OpX::fragment(stage + part * PLANE, wm + i * 16, step, lane);
         };
         auto columns = [&](int j, int step) { return OpW::fragment(stage + PARTS * PLANE, wn + j * 16, step, lane); };
-        if constexpr (LONG) {
 #pragma unroll
-            for (int step = 0; step < 2; ++step) {
-                Vec<U> q[4];
-                row_fragments(0, step, q);
+        for (int step = 0; step < 2; step += AT_ONCE) {
+            Vec<U> q[AT_ONCE][PARTS][4], p[AT_ONCE][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const Vec<U> p = columns(j, step);
+            for (int u = 0; u < AT_ONCE; ++u) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[i][j] = mma(q[i], p, sum[i][j]);
-                }
+                for (int j = 0; j < 4; ++j) p[u][j] = columns(j, step + u);
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) row_fragments(part, step + u, q[u][part]);
             }
-            if ((k0 & 64) || k0 + BK >= ke)
+            v4f one[2][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v4f one[4];
+            for (int j = 0; j < 5; ++j) {                     // a column's sums leave while the next one's products are made
+                if (j < 4) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        one[i] = sum[i][j];
-                        sum[i][j] = v4f{};
-                    }
-                    add(j, one, of[0][j]);
+                    for (int i = 0; i < 4; ++i) one[j & 1][i] = v4f{};
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+                        for (int part = PARTS - 1; part >= 0; --part)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) one[j & 1][i] = mma(q[u][part][i], p[u][j], one[j & 1][i]);
                 }
-        } else {
-            constexpr int AT_ONCE = TOGETHER;                     // steps
-#pragma unroll
-            for (int step = 0; step < 2; step += AT_ONCE) {
-                Vec<U> q[AT_ONCE][PARTS][4], p[AT_ONCE][4];
-#pragma unroll
-                for (int u = 0; u < AT_ONCE; ++u) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) p[u][j] = columns(j, step + u);
-#pragma unroll
-                    for (int part = 0; part < PARTS; ++part) row_fragments(part, step + u, q[u][part]);
-                }
-                v4f one[2][4];
-#pragma unroll
-                for (int j = 0; j < 5; ++j) {                     // a column's sums leave while the next one's products are made
-                    if (j < 4) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) one[j & 1][i] = v4f{};
-#pragma unroll
-                        for (int u = 0; u < AT_ONCE; ++u)
-#pragma unroll
-                            for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) one[j & 1][i] = mma(q[u][part][i], p[u][j], one[j & 1][i]);
-                    }
-                    if (j > 0) add(j - 1, one[(j - 1) & 1], of[STEPS == 1 ? step : 0][j - 1]);
-                    KEEP_ORDER();
-                }
+                if (j > 0) add(j - 1, one[(j - 1) & 1], of[STEPS == 1 ? step : 0][j - 1]);
+                KEEP_ORDER();
             }
         }
     };
-    char* stage = lds;
-    int64_t k = kb;
-    send_scales(k);
-    fetch(k);
-    put(stage, k);
-    __syncthreads();
-    while (true) {
-        const bool more = k + BK < ke;
-        if (more) fetch(k + BK);
+    // The stage at k is in LDS, the next one in the other set or, with one set, not on its way yet.
+    int k = kb;
+    auto turn = [&](auto mine, auto next, char* stage, char* other) {
+        if (k + SETS * BK < ke) fetch(mine, k + SETS * BK);
         multiply(stage, k);
-        if (!more) break;
         k += BK;
+        if (k >= ke) return false;
         if (STAGES == 1) __syncthreads();
-        else stage = stage == lds ? lds + STAGE : lds;
-        put(stage, k);
+        put(next, other, k);
         __syncthreads();
-    }
+        return true;
+    };
+    constexpr std::integral_constant<int, 0> zero{};
+    constexpr std::integral_constant<int, SETS - 1> last{};
+    fetch(zero, k);
+    if (SETS == 2 && k + BK < ke) fetch(last, k + BK);
+    put(zero, lds, k);
+    __syncthreads();
+    char* const other = lds + (STAGES - 1) * STAGE;
+    while (turn(zero, last, lds, other) && turn(last, zero, other, lds)) {}
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
