@@ -16,46 +16,108 @@ __device__ __forceinline__ uint32_t weight4_code(float w, float s) {
     c += a > 5.f * s;
     return c ? c | (w < 0.f ? 8u : 0u) : 0u;
 }
+// A place as a number: from 2 on bits 1 and 2 are its exponent and bit 0 is its mantissa; below it is half of itself.
 __device__ __forceinline__ float weight4_value(uint32_t code) {
     const uint32_t c = code & 7u;
-    const float v = c < 4 ? 0.5f * c : (c == 7 ? 6.f : (float)c - 2.f);
-    return code & 8u ? -v : v;
+    const float v = c < 2 ? 0.5f * (float)c : __builtin_bit_cast(float, (c << 22) + (126u << 23));
+    return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) | (code & 8u) << 28);
+}
+template <int E>
+__device__ __forceinline__ void store_words(uint32_t* p, Elems<uint32_t, E> x, int there) {
+    if (there >= E) {
+        *reinterpret_cast<LooseElems<uint32_t, E>*>(p) = __builtin_bit_cast(LooseElems<uint32_t, E>, x);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (e < there) p[e] = x[e];
 }
 
-// A thread has a group of a column, read twice: the largest first.
+// A lane has four columns, a wavefront eight rows of them, which are a word each (of groups of 128 two times eight): read once, and held until the workgroup's wavefronts have found the largest
+// numbers of the groups in LDS.  Bound by memory: 4099 x 4096 in fp32 PACK_US.
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear4_pack(int32_t K, int64_t cols, const T* W, int64_t ldw, int group, uint32_t* Q, int64_t ldq, uint16_t* S, int64_t lds) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
-    const int64_t groups = groups_of(K, group);
-    for (int64_t g = blockIdx.y; g < groups; g += gridDim.y) {
-        const int64_t k0 = g * group, k1 = k0 + group < K ? k0 + group : K;
-        uint32_t most = 0;
-        for (int64_t k = k0; k < k1; ++k) {
-            const uint32_t b = __builtin_bit_cast(uint32_t, (float)W[k * ldw + c]) & 0x7fffffffu;
-            most = most > b ? most : b;
+__global__ __launch_bounds__(512) void k_linear4_pack(int32_t K, int64_t cols, const T* W, int64_t ldw, int group, uint32_t* Q, int64_t ldq, uint16_t* S, int64_t lds) {
+    constexpr int E = 4, WAVES = 8;
+    __shared__ uint32_t found[WAVES][64][E];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E;
+    const int count = cols - c < 0 ? 0 : cols - c < E ? (int)(cols - c) : E;
+    auto unit = [&](int64_t k0, auto words_of_wave) {
+        constexpr int WORDS = decltype(words_of_wave)::value;
+        Elems<T, E> v[WORDS][8];
+        uint32_t most[E] = {};
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int64_t k = k0 + (w * WAVES + wave) * 8 + r;
+                v[w][r] = load_elems<E>(W + k * ldw + c, k < K ? count : 0);
+            }
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w)
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const uint32_t b = __builtin_bit_cast(uint32_t, (float)v[w][r][e]) & 0x7fffffffu;
+                    most[e] = most[e] > b ? most[e] : b;
+                }
+#pragma unroll
+        for (int e = 0; e < E; ++e) found[wave][lane][e] = most[e];
+        __syncthreads();
+        const int slices = group == 32 ? 4 : WAVES, first = wave & ~(slices - 1);
+        for (int w = 0; w < slices; ++w)
+#pragma unroll
+            for (int e = 0; e < E; ++e) most[e] = most[e] > found[first + w][lane][e] ? most[e] : found[first + w][lane][e];
+        __syncthreads();
+        uint32_t bits[E];
+        float s[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            bits[e] = scale_of<T>(most[e], WEIGHT4_TOP);
+            s[e] = scale_value(bits[e]);
         }
-        const uint32_t bits = scale_of<T>(most, WEIGHT4_TOP);
-        const float s = scale_value(bits);
-        for (int64_t k = k0; k < k1; k += 8) {
-            uint32_t word = 0;
-            for (int e = 0; e < 8; ++e)
-                if (k + e < k1) word |= weight4_code((float)W[(k + e) * ldw + c], s) << (4 * e);
-            Q[k / 8 * ldq + c] = word;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) {
+            const int64_t k = k0 + (w * WAVES + wave) * 8;
+            if (k >= K) continue;
+            Elems<uint32_t, E> word = {};
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int r = 0; r < 8; ++r) word[e] |= weight4_code((float)v[w][r][e], s[e]) << (4 * r);     // (rows behind the last are zeros, of code 0)
+            store_words(Q + k / 8 * ldq + c, word, count);
+            if (k % group == 0)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e < count) S[k / group * lds + c + e] = (uint16_t)bits[e];
         }
-        S[g * lds + c] = (uint16_t)bits;
+    };
+    const int64_t rows = group == 128 ? 128 : 64;
+    for (int64_t k0 = (int64_t)blockIdx.y * rows; k0 < K; k0 += gridDim.y * rows) {
+        if (group == 128) unit(k0, std::integral_constant<int, 2>());
+        else unit(k0, std::integral_constant<int, 1>());
     }
 }
 
+// A lane has the words of 16 bytes of columns.
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear4_unpack(int32_t K, int64_t cols, const uint32_t* Q, int64_t ldq, const uint16_t* S, int64_t lds, int group, T* W, int64_t ldw) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, words = groups_of(K, 8);
-    if (c >= cols) return;
-    for (int64_t j = blockIdx.y; j < words; j += gridDim.y) {
-        const uint32_t q = Q[j * ldq + c];
-        const float s = scale_value(S[j * 8 / group * lds + c]);
-        for (int e = 0; e < 8; ++e)
-            if (j * 8 + e < K) W[(j * 8 + e) * ldw + c] = (T)(s * weight4_value(q >> (4 * e)));
+    constexpr int E = Elem<T>::E;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + (threadIdx.x & 63)) * E, words = groups_of(K, 8);
+    const int count = cols - c < 0 ? 0 : cols - c < E ? (int)(cols - c) : E, shift = group == 32 ? 2 : group == 64 ? 3 : 4;
+    if (count == 0) return;
+    for (int64_t j = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); j < words; j += (int64_t)gridDim.y * 4) {
+        const Elems<uint32_t, E> word = load_elems<E>(Q + j * ldq + c, count);
+        const Elems<uint16_t, E> bits = load_elems<E>(S + (j >> shift) * lds + c, count);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            if (j * 8 + r >= K) break;
+            float v[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = scale_value(bits[e]) * weight4_value(word[e] >> (4 * r));
+            store_vec_part(W + (j * 8 + r) * ldw + c, from_floats<T>(v), count);
+        }
     }
 }
 
@@ -84,13 +146,17 @@ static int check_layout(const char* who, int32_t f_in, int32_t cols, int type, c
     if (m.meets(q) || m.meets(s) || q.meets(s)) return fail(GCN_ERR_BADARG, "%s: an output overlaps an input or another output", who);
     return GCN_OK;
 }
-static dim3 columns_and_steps(int64_t cols, int64_t steps) { return dim3((unsigned)((cols + 255) / 256), (unsigned)(steps < 65535 ? steps : 65535)); }
+// Workgroups of 64 lanes of so many columns, and enough along k
+static dim3 across_and_down(int64_t cols, int64_t each, int64_t down) {
+    const int64_t wide = 64 * each;
+    return dim3((unsigned)((cols + wide - 1) / wide), (unsigned)(down < 65535 ? down : 65535));
+}
 
 extern "C" int gcn_linear4_pack(int32_t f_in, int32_t cols, int type, const void* W, int64_t ldw, int group, uint32_t* Q, int64_t ldq, uint16_t* S, int64_t lds, void* stream) {
     GCN_TRY(check_layout("gcn_linear4_pack", f_in, cols, type, W, ldw, {Q, S, ldq, lds, group}));
     return by_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_linear4_pack<T>, columns_and_steps(cols, groups_of(f_in, group)), dim3(256), 0, (hipStream_t)stream, f_in, cols, (const T*)W, ldw, group, Q, ldq, S, lds);
+        hipLaunchKernelGGL(k_linear4_pack<T>, across_and_down(cols, 4, groups_of(f_in, group == 128 ? 128 : 64)), dim3(512), 0, (hipStream_t)stream, f_in, cols, (const T*)W, ldw, group, Q, ldq, S, lds);
         GCN_LAUNCH_CHECK();
         return GCN_OK;
     });
@@ -100,7 +166,7 @@ extern "C" int gcn_linear4_unpack(int32_t f_in, int32_t cols, int type, const ui
     GCN_TRY(check_layout("gcn_linear4_unpack", f_in, cols, type, W, ldw, {Q, S, ldq, lds, group}));
     return by_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_linear4_unpack<T>, columns_and_steps(cols, groups_of(f_in, 8)), dim3(256), 0, (hipStream_t)stream, f_in, cols, Q, ldq, S, lds, group, (T*)W, ldw);
+        hipLaunchKernelGGL(k_linear4_unpack<T>, across_and_down(cols, Elem<T>::E, groups_of(f_in, 32)), dim3(256), 0, (hipStream_t)stream, f_in, cols, Q, ldq, S, lds, group, (T*)W, ldw);
         GCN_LAUNCH_CHECK();
         return GCN_OK;
     });
