@@ -17,65 +17,114 @@ __device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {
     return v;
 }
 
-// 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.
+// The pieces of a matrix, `per` of each row, that a lane comes to: from number t on every `step`th.
+struct Walk {
+    int64_t row;
+    int32_t piece, per, step_pieces;
+    int64_t step_rows;
+    __device__ Walk(int64_t t, int32_t per, int64_t step) : row(t / per), piece((int32_t)(t % per)), per(per), step_pieces((int32_t)(step % per)), step_rows(step / per) {}
+    __device__ void next() {
+        row += step_rows;
+        piece += step_pieces;
+        if (piece >= per) {
+            piece -= per;
+            ++row;
+        }
+    }
+};
+constexpr int PASS_AHEAD = 2;                                     // pieces of a lane that are on their way together
+
+// 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.  Bound by memory: 232965 x 602 in bf16 PACK_US.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* C, int64_t ldc, uint16_t* S, int64_t lds) {
-    constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E;
-    const int64_t groups = groups_of(f, CHECKPOINT_GROUP), all = n * groups;
-    for (int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L; t < all; t += (int64_t)gridDim.x * (256 / L)) {
-        const int64_t i = t / groups, g = t % groups, c = g * CHECKPOINT_GROUP + (int)(threadIdx.x % L) * E;
-        const int count = f - c < 0 ? 0 : f - c < E ? (int)(f - c) : E;
-        float v[E];
-        to_floats<T>(count > 0 ? load_vec_part(X + i * ldx + c, count) : Vec<T>{}, v);
-        uint32_t most = 0;
+    constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E, A = PASS_AHEAD;
+    const int32_t per = (int32_t)groups_of(f, CHECKPOINT_GROUP) * L;          // lanes of a row
+    Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, per, (int64_t)gridDim.x * 256);
+    while (at.row < n) {                                          // (a group's lanes go together)
+        Words<T, E> x[A];
+        int64_t row[A];
+        int32_t piece[A];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
-            most = most > b ? most : b;
+        for (int u = 0; u < A; ++u) {
+            row[u] = at.row;
+            piece[u] = at.piece;
+            at.next();
+            const int64_t i = row[u] < n ? row[u] : n - 1;
+            if (f >= E) x[u] = load_near<E>(X + i * ldx, (int64_t)piece[u] * E, f);
+            else x[u] = __builtin_bit_cast(Words<T, E>, load_vec_part(X + i * ldx, piece[u] == 0 ? f : 0));
         }
-        const uint32_t bits = scale_of<T>(most_of_lanes<L>(most), CHECKPOINT_TOP);
-        const float s = scale_value(bits), inv = inverse(s);
-        uint32_t code[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) code[e] = checkpoint_code<T>(v[e], s, inv) & 255u;
-        int8_t* const to = C + i * ldc + c;
-        if (count == E) {
-            LooseCodes<E> x;
+        for (int u = 0; u < A; ++u) {
+            const int64_t i = row[u], c = (int64_t)piece[u] * E;
+            const int count = f - c < 0 ? 0 : f - c < E ? (int)(f - c) : E;
+            float v[E];
+            to_floats<T>(f >= E && count < E ? __builtin_bit_cast(Vec<T>, settle<E, T>(x[u], settle_by<E>(c, f))) : __builtin_bit_cast(Vec<T>, x[u]), v);
+            uint32_t most = 0;
 #pragma unroll
-            for (int w = 0; w < E / 4; ++w) x.w[w] = code[4 * w] | code[4 * w + 1] << 8 | code[4 * w + 2] << 16 | code[4 * w + 3] << 24;
-            *reinterpret_cast<LooseCodes<E>*>(to) = x;
-        } else {
+            for (int e = 0; e < E; ++e) {
+                const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
+                most = most > b ? most : b;
+            }
+            const uint32_t bits = scale_of<T>(most_of_lanes<L>(most), CHECKPOINT_TOP);
+            if (i >= n) continue;
+            const float s = scale_value(bits), inv = inverse(s);
+            uint32_t code[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (e < count) to[e] = (int8_t)code[e];
+            for (int e = 0; e < E; ++e) code[e] = checkpoint_code<T>(v[e], s, inv) & 255u;
+            int8_t* const to = C + i * ldc + c;
+            if (count == E) {
+                LooseCodes<E> q;
+#pragma unroll
+                for (int w = 0; w < E / 4; ++w) q.w[w] = code[4 * w] | code[4 * w + 1] << 8 | code[4 * w + 2] << 16 | code[4 * w + 3] << 24;
+                *reinterpret_cast<LooseCodes<E>*>(to) = q;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e < count) to[e] = (int8_t)code[e];
+            }
+            if (piece[u] % L == 0) S[i * lds + piece[u] / L] = (uint16_t)bits;
         }
-        if (threadIdx.x % L == 0) S[i * lds + g] = (uint16_t)bits;
     }
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f, const int8_t* C, int64_t ldc, const uint16_t* S, int64_t lds, T* X, int64_t ldx) {
-    constexpr int E = Elem<T>::E;
-    const int64_t pieces = groups_of(f, E), all = n * pieces;
-    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all; t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / pieces, c = t % pieces * E;
-        const Codes<E> q = load_codes<E>(C + i * ldc, c, f);
-        const float s = scale_value(S[i * lds + c / CHECKPOINT_GROUP]);
-        float v[E];
+    constexpr int E = Elem<T>::E, A = PASS_AHEAD;
+    Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, (int32_t)groups_of(f, E), (int64_t)gridDim.x * 256);
+    while (at.row < n) {
+        Codes<E> q[A];
+        uint16_t s[A];
+        int64_t row[A];
+        int32_t piece[A];
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = s * code_value<E>(q, e);
-        store_vec_part(X + i * ldx + c, from_floats<T>(v), f - c < E ? (int)(f - c) : E);
+        for (int u = 0; u < A; ++u) {
+            row[u] = at.row;
+            piece[u] = at.piece;
+            at.next();
+            const int64_t i = row[u] < n ? row[u] : n - 1;
+            q[u] = load_codes<E>(C + i * ldc, (int64_t)piece[u] * E, f);
+            s[u] = S[i * lds + piece[u] / (CHECKPOINT_GROUP / E)];
+        }
+#pragma unroll
+        for (int u = 0; u < A; ++u) {
+            if (row[u] >= n) break;
+            const int64_t c = (int64_t)piece[u] * E;
+            float v[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = scale_value(s[u]) * code_value<E>(q[u], e);
+            store_vec_part(X + row[u] * ldx + c, from_floats<T>(v), f - c < E ? (int)(f - c) : E);
+        }
     }
 }
 
-static unsigned passes(int64_t items, int64_t each) {             // workgroups of a pass over `items`, `each` at a time for one
-    const int64_t blocks = (items + each - 1) / each, most = 32 * (int64_t)device_info().cus;
+static unsigned passes(int64_t lanes) {                           // workgroups of a pass over matrices
+    const int64_t blocks = (lanes + 255) / 256, most = 16 * (int64_t)device_info().cus;
     return (unsigned)(blocks < most ? blocks : most);
 }
 
 template <typename T>
 static int unpack_launch(int64_t n, int32_t f, const Kept& k, void* X, int64_t ldx, hipStream_t s) {
-    hipLaunchKernelGGL(k_checkpoint_unpack<T>, dim3(passes(n * groups_of(f, Elem<T>::E), 256)), dim3(256), 0, s, n, f, (const int8_t*)k.p, k.ld, k.scales, k.lds, (T*)X, ldx);
+    hipLaunchKernelGGL(k_checkpoint_unpack<T>, dim3(passes(n * groups_of(f, Elem<T>::E))), dim3(256), 0, s, n, f, (const int8_t*)k.p, k.ld, k.scales, k.lds, (T*)X, ldx);
     GCN_LAUNCH_CHECK();
     return GCN_OK;
 }
@@ -125,7 +174,7 @@ extern "C" int gcn_checkpoint_pack(int64_t n, int32_t f, int type, const void* X
     GCN_TRY(check_pack("gcn_checkpoint_pack", n, f, type, X, ldx, {codes, ldc, scales, lds}));
     return by_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        hipLaunchKernelGGL(k_checkpoint_pack<T>, dim3(passes(n * groups_of(f, CHECKPOINT_GROUP), 256 / (CHECKPOINT_GROUP / Elem<T>::E))), dim3(256), 0, (hipStream_t)stream, n, f,
+        hipLaunchKernelGGL(k_checkpoint_pack<T>, dim3(passes(n * groups_of(f, CHECKPOINT_GROUP) * (CHECKPOINT_GROUP / Elem<T>::E))), dim3(256), 0, (hipStream_t)stream, n, f,
                            (const T*)X, ldx, codes, ldc, scales, lds);
         GCN_LAUNCH_CHECK();
         return GCN_OK;

@@ -37,13 +37,14 @@ struct SlopeArgs {
 // (2.9e-4 of their norm in fp16 where the sum of an unrounded dZ has 2.1e-4, 2.3e-3 and 1.7e-3 in bf16); the bias's gradient is the sum of what was not rounded.
 template <typename T, bool GATED, bool HELD>
 __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
-    constexpr int E = Elem<T>::E, SETS = 4, AHEAD = 2, HALVES = GATED ? 2 : 1;
+    constexpr int E = Elem<T>::E, SETS = 4, AHEAD = GATED ? 2 : 4, HALVES = GATED ? 2 : 1;
     __shared__ float sums[SETS][64][HALVES * E + 1];
     const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
     const int32_t N = a.N;
     const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E, width = (int64_t)HALVES * N;
     const int64_t rb = (int64_t)blockIdx.y * a.rows_per_block, re = rb + a.rows_per_block < a.n ? rb + a.rows_per_block : a.n;
     const int count = c >= N ? 0 : N - c < E ? (int)(N - c) : E;
+    const bool apart = GATED && N % E != 0;                       // a piece of the second half can lie in two groups
     float sum[HALVES][E] = {};
     struct Piece {                                                // of a row: dY's elements, and Z's or their codes
         Vec<T> y, z[HALVES];
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
                 p.q[h] = load_codes<E>((const int8_t*)a.Z.p + i * a.Z.ld, at, width);
                 const int64_t g = at / CHECKPOINT_GROUP, last = (at + count - 1) / CHECKPOINT_GROUP;
                 p.s[h][0] = a.Z.scales[i * a.Z.lds + g];
-                p.s[h][1] = a.Z.scales[i * a.Z.lds + last];
+                if (apart) p.s[h][1] = a.Z.scales[i * a.Z.lds + last];
             } else {
                 p.z[h] = part((const T*)a.Z.p + i * a.Z.ld, at, width);
             }
@@ -80,10 +81,16 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
 #pragma unroll
         for (int h = 0; h < HALVES; ++h)
             if constexpr (HELD) {
-                const int here = CHECKPOINT_GROUP - (int)(((int64_t)h * N + c) % CHECKPOINT_GROUP);
-                const float s0 = scale_value(p.s[h][0]), s1 = scale_value(p.s[h][1]);
+                const float s0 = scale_value(p.s[h][0]);
+                if (h == 1 && apart) {
+                    const int here = CHECKPOINT_GROUP - (int)(((int64_t)h * N + c) % CHECKPOINT_GROUP);
+                    const float s1 = scale_value(p.s[h][1]);
 #pragma unroll
-                for (int e = 0; e < E; ++e) z[h][e] = (float)(T)((e < here ? s0 : s1) * code_value<E>(p.q[h], e));
+                    for (int e = 0; e < E; ++e) z[h][e] = (float)(T)((e < here ? s0 : s1) * code_value<E>(p.q[h], e));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) z[h][e] = (float)(T)(s0 * code_value<E>(p.q[h], e));
+                }
             } else {
                 to_floats<T>(p.z[h], z[h]);
             }
@@ -117,7 +124,8 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
                 if (i + u * SETS < re) row(i + u * SETS, p[u]);
         }
     };
-    if (count == E) rows(std::true_type());
+    // a workgroup whose columns are not all whole pieces goes the other way with all of them: two ways one after the other took twice as long (4099 x 1001 WAYS_US)
+    if (((int64_t)blockIdx.x + 1) * 64 * E <= N) rows(std::true_type());
     else if (count > 0) rows(std::false_type());
     if (!a.part) return;
 #pragma unroll
