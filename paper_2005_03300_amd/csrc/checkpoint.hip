@@ -17,6 +17,38 @@ __device__ __forceinline__ uint32_t most_of_lanes(uint32_t v) {
     return v;
 }
 
+// The largest of the bits of 16 bytes of elements without their signs, as those of an fp32 number; of 16-bit ones two at a time.
+template <typename T>
+__device__ __forceinline__ uint32_t most_of(Vec<T> x) {
+    if constexpr (sizeof(T) == 4) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float v = x[e];                                 // (the bits of a vector's element taken in place are those of its first)
+            const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
+            most = most > b ? most : b;
+        }
+        return most;
+    } else {
+        typedef unsigned short u2 __attribute__((ext_vector_type(2)));
+        const Words<T, 8> w = __builtin_bit_cast(Words<T, 8>, x);
+        u2 most = __builtin_bit_cast(u2, w[0] & 0x7fff7fffu);
+#pragma unroll
+        for (int e = 1; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u2, w[e] & 0x7fff7fffu));
+        const uint16_t m = most[0] > most[1] ? most[0] : most[1];
+        return __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(T, m));
+    }
+}
+// The lowest bytes of four words.
+__device__ __forceinline__ uint32_t lowest_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), cd = __builtin_amdgcn_perm(d, c, 0x0c0c0400u);
+    return __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+#else
+    return (a & 255u) | (b & 255u) << 8 | (c & 255u) << 16 | d << 24;
+#endif
+}
+
 // The pieces of a matrix, `per` of each row, that a lane comes to: from number t on every `step`th.
 struct Walk {
     int64_t row;
@@ -34,85 +66,91 @@ struct Walk {
 };
 constexpr int PASS_AHEAD = 2;                                     // pieces of a lane that are on their way together
 
-// 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.  Bound by memory: 232965 x 602 in bf16 PACK_US.
+// 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.  A piece that a row's end cuts is the row's last whole one instead, where that lies in the
+// same group: its codes are written twice, the same.  Bound by memory and, with 12 vector instructions an element, nearly as much by these: 232965 x 602 in bf16 PACK_US.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* C, int64_t ldc, uint16_t* S, int64_t lds) {
     constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E, A = PASS_AHEAD;
     const int32_t per = (int32_t)groups_of(f, CHECKPOINT_GROUP) * L;          // lanes of a row
+    const int32_t end = f % CHECKPOINT_GROUP, last = end == 0 || end >= E ? f - E : f;         // where the last whole piece of the last group begins
     Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, per, (int64_t)gridDim.x * 256);
     while (at.row < n) {                                          // (a group's lanes go together)
-        Words<T, E> x[A];
+        Vec<T> x[A];
         int64_t row[A];
-        int32_t piece[A];
+        int32_t col[A];
 #pragma unroll
         for (int u = 0; u < A; ++u) {
             row[u] = at.row;
-            piece[u] = at.piece;
+            col[u] = at.piece * E;
             at.next();
-            const int64_t i = row[u] < n ? row[u] : n - 1;
-            if (f >= E) x[u] = load_near<E>(X + i * ldx, (int64_t)piece[u] * E, f);
-            else x[u] = __builtin_bit_cast(Words<T, E>, load_vec_part(X + i * ldx, piece[u] == 0 ? f : 0));
+            const T* const from = X + (row[u] < n ? row[u] : n - 1) * ldx;
+            if (last < f) x[u] = load_vec(from + (col[u] < last ? col[u] : last));
+            else x[u] = load_vec_part(from + col[u], f - col[u] < 0 ? 0 : f - col[u]);
         }
 #pragma unroll
         for (int u = 0; u < A; ++u) {
-            const int64_t i = row[u], c = (int64_t)piece[u] * E;
-            const int count = f - c < 0 ? 0 : f - c < E ? (int)(f - c) : E;
-            float v[E];
-            to_floats<T>(f >= E && count < E ? __builtin_bit_cast(Vec<T>, settle<E, T>(x[u], settle_by<E>(c, f))) : __builtin_bit_cast(Vec<T>, x[u]), v);
-            uint32_t most = 0;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
-                most = most > b ? most : b;
-            }
-            const uint32_t bits = scale_of<T>(most_of_lanes<L>(most), CHECKPOINT_TOP);
-            if (i >= n) continue;
+            const uint32_t bits = scale_of<T>(most_of_lanes<L>(most_of<T>(x[u])), CHECKPOINT_TOP);
+            const int64_t i = row[u];
+            if (i >= n || col[u] >= f) continue;
             const float s = scale_value(bits), inv = inverse(s);
+            float v[E];
+            to_floats<T>(x[u], v);
+            if (bits == largest_scale<T>(CHECKPOINT_TOP)) {       // numbers beyond what that reaches
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = fminf(fmaxf(v[e], -CHECKPOINT_TOP * s), CHECKPOINT_TOP * s);
+            }
             uint32_t code[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) code[e] = checkpoint_code<T>(v[e], s, inv) & 255u;
-            int8_t* const to = C + i * ldc + c;
-            if (count == E) {
+            for (int e = 0; e < E; ++e) code[e] = checkpoint_code<T>(v[e], s, inv);
+            int8_t* const to = C + i * ldc;
+            if (last < f) {
                 LooseCodes<E> q;
 #pragma unroll
-                for (int w = 0; w < E / 4; ++w) q.w[w] = code[4 * w] | code[4 * w + 1] << 8 | code[4 * w + 2] << 16 | code[4 * w + 3] << 24;
-                *reinterpret_cast<LooseCodes<E>*>(to) = q;
+                for (int w = 0; w < E / 4; ++w) q.w[w] = lowest_bytes(code[4 * w], code[4 * w + 1], code[4 * w + 2], code[4 * w + 3]);
+                *reinterpret_cast<LooseCodes<E>*>(to + (col[u] < last ? col[u] : last)) = q;
             } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (e < count) to[e] = (int8_t)code[e];
+                    if (col[u] + e < f) to[col[u] + e] = (int8_t)code[e];
             }
-            if (piece[u] % L == 0) S[i * lds + piece[u] / L] = (uint16_t)bits;
+            if (col[u] % CHECKPOINT_GROUP == 0) S[i * lds + col[u] / CHECKPOINT_GROUP] = (uint16_t)bits;
         }
     }
 }
 
+// A lane has 16 bytes of a row; those that its end cuts are the row's last whole ones, of which some lie in the group before.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f, const int8_t* C, int64_t ldc, const uint16_t* S, int64_t lds, T* X, int64_t ldx) {
     constexpr int E = Elem<T>::E, A = PASS_AHEAD;
+    const int32_t last = f - E;
     Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, (int32_t)groups_of(f, E), (int64_t)gridDim.x * 256);
     while (at.row < n) {
         Codes<E> q[A];
-        uint16_t s[A];
+        uint16_t s[A][2];
         int64_t row[A];
-        int32_t piece[A];
+        int32_t col[A];
 #pragma unroll
         for (int u = 0; u < A; ++u) {
             row[u] = at.row;
-            piece[u] = at.piece;
+            col[u] = at.piece * E;
+            if (last >= 0 && col[u] > last) col[u] = last;
             at.next();
             const int64_t i = row[u] < n ? row[u] : n - 1;
-            q[u] = load_codes<E>(C + i * ldc, (int64_t)piece[u] * E, f);
-            s[u] = S[i * lds + piece[u] / (CHECKPOINT_GROUP / E)];
+            q[u] = load_codes<E>(C + i * ldc, col[u], f);
+            s[u][0] = S[i * lds + col[u] / CHECKPOINT_GROUP];
+            s[u][1] = S[i * lds + (last >= 0 ? col[u] + E - 1 : f - 1) / CHECKPOINT_GROUP];
         }
 #pragma unroll
         for (int u = 0; u < A; ++u) {
             if (row[u] >= n) break;
-            const int64_t c = (int64_t)piece[u] * E;
+            const int here = CHECKPOINT_GROUP - col[u] % CHECKPOINT_GROUP;
+            const float s0 = scale_value(s[u][0]), s1 = scale_value(s[u][1]);
             float v[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = scale_value(s[u]) * code_value<E>(q[u], e);
-            store_vec_part(X + row[u] * ldx + c, from_floats<T>(v), f - c < E ? (int)(f - c) : E);
+            for (int e = 0; e < E; ++e) v[e] = (e < here ? s0 : s1) * code_value<E>(q[u], e);
+            T* const to = X + row[u] * ldx + col[u];
+            if (last >= 0) store_vec(to, from_floats<T>(v));
+            else store_vec_part(to, from_floats<T>(v), f);
         }
     }
 }

@@ -45,24 +45,18 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t most, float top) {
     return s < most_of_type ? s : most_of_type;
 }
 
-// x / s to the nearest whole number: the bits of 1.5 2^23 plus it, whose lowest byte is the code.  `inv`: 1 / s to a few 2^-24.  One correction of the product x inv makes a quotient that has few
+// x / s, between -127 and 127, to the nearest whole number: the bits of 1.5 2^23 plus it, whose lowest byte is the code.  `inv`: 1 / s to a few 2^-24.  One correction of the product x inv makes a quotient that has few
 // bits exact, so that the middle between two numbers, x = (c + 1/2) s, goes to the even one.  Other quotients are no nearer to a middle than 2^-9 (bf16 x) or 2^-12 (fp16) and the
 // correction is off by 2^-17 at most; fp32 numbers can be as near as 2^-25, so there the remainder, which is exact, decides.
 template <typename T>
 __device__ __forceinline__ uint32_t checkpoint_code(float x, float s, float inv) {
     const float q = x * inv;
-    float t = fmaf(fmaf(-q, s, x), inv, q);
-#if defined(__HIP_DEVICE_COMPILE__)
-    t = __builtin_amdgcn_fmed3f(t, -CHECKPOINT_TOP, CHECKPOINT_TOP);
-#endif
+    const float t = fmaf(fmaf(-q, s, x), inv, q);
     constexpr float MAGIC = 12582912.f;
     const float m = t + MAGIC;
     if (sizeof(T) == 4) {
         const float c = m - MAGIC, rest = fmaf(-c, s, x);
-        const float up = fabsf(rest) > 0.5f * s ? (rest > 0.f ? 1.f : -1.f) : 0.f;
-        float v = c + up;
-        v = v > CHECKPOINT_TOP ? CHECKPOINT_TOP : (v < -CHECKPOINT_TOP ? -CHECKPOINT_TOP : v);
-        return __builtin_bit_cast(uint32_t, v + MAGIC);
+        return __builtin_bit_cast(uint32_t, fabsf(rest) > 0.5f * s ? m + (rest > 0.f ? 1.f : -1.f) : m);
     }
     return __builtin_bit_cast(uint32_t, m);
 }
