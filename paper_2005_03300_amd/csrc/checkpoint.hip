@@ -64,13 +64,12 @@ struct Walk {
         }
     }
 };
-constexpr int PASS_AHEAD = 2;                                     // pieces of a lane that are on their way together
 
 // 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.  A piece that a row's end cuts is the row's last whole one instead, where that lies in the
 // same group: its codes are written twice, the same.  Bound by memory and, with 12 vector instructions an element, nearly as much by these: 232965 x 602 in bf16 PACK_US.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* C, int64_t ldc, uint16_t* S, int64_t lds) {
-    constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E, A = PASS_AHEAD;
+    constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E, A = 2;
     const int32_t per = (int32_t)groups_of(f, CHECKPOINT_GROUP) * L;          // lanes of a row
     const int32_t end = f % CHECKPOINT_GROUP, last = end == 0 || end >= E ? f - E : f;         // where the last whole piece of the last group begins
     Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, per, (int64_t)gridDim.x * 256);
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, c
 // A lane has 16 bytes of a row; those that its end cuts are the row's last whole ones, of which some lie in the group before.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f, const int8_t* C, int64_t ldc, const uint16_t* S, int64_t lds, T* X, int64_t ldx) {
-    constexpr int E = Elem<T>::E, A = PASS_AHEAD;
+    constexpr int E = Elem<T>::E, A = 4;
     const int32_t last = f - E;
     Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, (int32_t)groups_of(f, E), (int64_t)gridDim.x * 256);
     while (at.row < n) {
