@@ -48,8 +48,9 @@ static int linear_product(const TileArgs& a, hipStream_t s) {
     return launch_tile<T, 64, 64, 2, 2, LA, LB, GATED>(a, c.splits, s);
 }
 
+// `shares` > 0: shares of the sum over k, as many as it has steps at most.
 template <typename T, int C, int RT, bool GATED>
-static int launch_few(TileArgs a, hipStream_t s) {
+static int launch_few(TileArgs a, hipStream_t s, int64_t shares = 0) {
     constexpr int STEP = 4 * Elem<T>::E * FEW_WAVES;              // values of k that a workgroup takes at a time
     constexpr int WIDE = GATED ? 8 * C : 16 * C;
     const int strips = (a.N + WIDE - 1) / WIDE;
@@ -62,6 +63,7 @@ static int launch_few(TileArgs a, hipStream_t s) {
         if (splits > most) splits = most;
     }
     const int64_t steps = (a.K + STEP - 1) / STEP;
+    if (shares > 0) splits = shares < steps ? shares : steps;
     a.k_share = (steps + splits - 1) / splits * STEP;
     splits = (a.K + a.k_share - 1) / a.k_share;
     ScratchLease lease;
@@ -82,6 +84,17 @@ static int linear_forward_impl(const TileArgs& a, hipStream_t s) {
     // 4.3, 4096 x 4096 13.8 and 15.7 against 13.6 and 14.6; fp32 21.6 and 23.8 against 31.  Tiles are the faster for long sums over few columns (16384 x 1024 in bf16 13.8 us
     // against 40).
     if (a.M > 32) return linear_product<T, BY_K, BY_MN, GATED>(a, s);
+    // A gated block's strip has two halves, and memory gives 5.0 TB/s in pieces of 128 bytes, 3.6 in pieces of 64 and 2.3 in pieces of 32.  So strips are as wide as gives each half 128 bytes, and the
+    // sum over k is shared where they leave compute units without work.  Microseconds of one row in bf16 with the strips and shares of a linear layer and with these: 8192 x 2*14336 123 and 98, 4096 x 2*8192
+    // 36.9 and 34.4, 4096 x 2*4096 28.7 and 22.7, 2048 x 2*2048 14.8 and 13.1; but 1024 x 2*8192 12.1 and 14.5, where the
+    // second launch costs more, and 8192 x 2*100 12.9 and 17.5, where the steps are too few for half of the compute units.  (17 to 32 rows of 16 bits: a wavefront has registers for 64 bytes.)
+    if constexpr (GATED)
+    {
+        constexpr int WIDE = sizeof(T) == 2 ? 8 : 4, STEP = 4 * Elem<T>::E * FEW_WAVES;
+        const int64_t wide = 16 * (a.M <= 16 ? WIDE : 4), shares = cus * wide / N > 1 ? cus * wide / N : 1;
+        if (shares == 1 || (a.K >= 2048 && (N + wide - 1) / wide * ((a.K + STEP - 1) / STEP) >= cus / 2))
+            return a.M <= 16 ? launch_few<T, WIDE, 1, GATED>(a, s, shares) : launch_few<T, 4, 2, GATED>(a, s, shares);
+    }
     // the widest strips that are still one for every compute unit
     const int c = N >= 64 * cus ? 4 : N >= 32 * cus ? 2 : 1;
     if (a.M <= 16) return c == 4 ? launch_few<T, 4, 1, GATED>(a, s) : c == 2 ? launch_few<T, 2, 1, GATED>(a, s) : launch_few<T, 1, 1, GATED>(a, s);
