@@ -169,16 +169,20 @@ static int unpack_launch(int64_t n, int32_t f, const Kept& k, void* X, int64_t l
 int back_products(int type, const BackProducts& b, hipStream_t s) {
     return by_type(type, [&](auto t) -> int {
         using T = decltype(t);
-        TileArgs a;
         if (b.dX) {
+            TileArgs a;
             a.A = b.G; a.lda = b.ldg; a.B = b.W; a.ldb = b.ldw; a.M = b.n; a.N = b.f_in; a.K = b.cols; a.Y = b.dX; a.ldy = b.lddx;
             GCN_TRY(linear_dx_of<T>(a, s));
         }
         if (b.dW) {
+            TileArgs a;
             const void* X = b.X.p;
             int64_t ldx = b.X.ld;
             ScratchLease lease;
-            if (b.X.scales) {
+            if (b.X.scales && sizeof(T) == 4 && b.f_in % 4 == 0) {             // fp32 products split their operands on the way to LDS, and codes as well
+                a.a_scales = b.X.scales;
+                a.lda_scales = b.X.lds;
+            } else if (b.X.scales) {
                 void* p = nullptr;
                 ldx = groups_of(b.f_in, Elem<T>::E) * Elem<T>::E;
                 GCN_TRY(lease.get(&p, (size_t)b.n * ldx * sizeof(T), s));

@@ -112,7 +112,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT ==
     const uint16_t* const S = w.S + c;
     const int64_t m0 = (int64_t)blockIdx.z * (16 * RT);
     const T* const X = (const T*)a.A + m0 * a.lda;
+    const int64_t rows = a.M;
     a.M -= m0;
+    if (a.part) a.part += m0 * a.N * (GATED ? 2 : 1);
     a.Y = (T*)a.Y + m0 * a.ldy;
     if (a.R) a.R = (const T*)a.R + m0 * a.ldr;
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
@@ -164,7 +166,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 16 || (sizeof(T) == 2 && RT ==
     if (n0 + WIDE <= a.N)
         for (; k + BLOCK4 <= ke; k += WAVES * BLOCK4) block(k, std::true_type());
     for (; k < ke; k += WAVES * BLOCK4) block(k, std::false_type());
-    leave_few<T, C, RT, GATED, WAVES, true>(a, acc, lds, n0, 1.f / PLACE4<T>);
+    leave_few<T, C, RT, GATED, WAVES, true>(a, acc, lds, n0, rows, 1.f / PLACE4<T>);
 }
 
 // Many rows: 128 x 128 results of four wavefronts, 64 values of k at a time, through registers: words become 16-byte pieces of places on their way to LDS, where X and W lie by k alike (see Operand).
@@ -357,7 +359,7 @@ template <typename T, int C, int RT, bool GATED>
 static int launch_few4(TileArgs a, const Weights4& w, int64_t splits, hipStream_t s) {
     constexpr int WAVES = few4_waves(C, RT), WIDE = GATED ? 8 * C : 16 * C, ALL = BLOCK4 * WAVES, ROWS = 16 * RT;
     const int strips = (a.N + WIDE - 1) / WIDE;
-    if (a.M > ROWS) splits = 1;
+    if (a.M > 65535 * ROWS) splits = 1;                           // (more than one launch)
     const int64_t blocks = (a.K + ALL - 1) / ALL;
     a.k_share = (blocks + splits - 1) / splits * ALL;
     splits = (a.K + a.k_share - 1) / a.k_share;
@@ -367,7 +369,7 @@ static int launch_few4(TileArgs a, const Weights4& w, int64_t splits, hipStream_
         GCN_TRY(lease.get(&p, (size_t)splits * a.M * a.N * (GATED ? 8 : 4), s));
         a.part = (float*)p;
     }
-    for (int64_t m = 0; m < a.M; m += 65535 * ROWS) {             // (a launch has so many workgroups along a dimension; more than one take whole sums)
+    for (int64_t m = 0; m < a.M; m += 65535 * ROWS) {             // (a launch has so many workgroups along a dimension)
         TileArgs b = a;
         b.A = (const T*)a.A + m * a.lda;
         b.Y = (T*)a.Y + m * a.ldy;

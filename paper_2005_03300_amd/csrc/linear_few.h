@@ -14,9 +14,9 @@ template <int C, int RT, int WAVES = FEW_WAVES>
 constexpr size_t few_lds() { return (size_t)WAVES * RT * 16 * (16 * C + 4) * 4; }
 
 // The wavefronts' results, of lane (r, quarter) those of row r (of each 16) and columns (4 quarter + e) C + q of the strip from n0 on (TURNED: of rows 4 quarter + e and columns r C + q), added in
-// order in LDS, times `times`, and what the layer does with them.
+// order in LDS, times `times`, and what the layer does with them.  part_rows: of a share's partial results.
 template <typename T, int C, int RT, bool GATED, int WAVES = FEW_WAVES, bool TURNED = false>
-__device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT][C], char* lds, int n0, float times = 1.f) {
+__device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT][C], char* lds, int n0, int64_t part_rows, float times = 1.f) {
     constexpr int E = Elem<T>::E, ROW = 16 * C + 4, WIDE = GATED ? 8 * C : 16 * C;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
     float* const mine = (float*)lds + wave * (RT * 16 * ROW);
@@ -47,7 +47,7 @@ __device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT
 #pragma unroll
                 for (int e = 0; e < E; ++e) d[h][e] = ((const float*)lds)[row * ROW + h * WIDE + c + e];
                 if (a.part) {
-                    float* const p = a.part + (((int64_t)blockIdx.y * a.M + row) * (GATED ? 2 : 1) + h) * a.N + n0 + c;
+                    float* const p = a.part + (((int64_t)blockIdx.y * part_rows + row) * (GATED ? 2 : 1) + h) * a.N + n0 + c;
 #pragma unroll
                     for (int e = 0; e < E; ++e)
                         if (e < count) p[e] = d[h][e];
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(TileArgs a, int s
             for (int u = 0; u < AHEAD; ++u) products(s[u]);
         }
     for (; k < ke; k += ALL) products(load(k, std::false_type()));
-    leave_few<T, C, RT, GATED>(a, acc, lds, n0);
+    leave_few<T, C, RT, GATED>(a, acc, lds, n0, a.M);
 }
 
 }  // namespace gcn

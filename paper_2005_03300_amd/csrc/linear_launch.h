@@ -26,7 +26,12 @@ static int launch_tile(TileArgs a, int splits, hipStream_t s) {
     }
     const dim3 grid((unsigned)(tm * tn), (unsigned)splits);
     if constexpr (sizeof(T) == 4) {
-        hipLaunchKernelGGL((k_linear_thirds<BM, BN, WM, WN, LA, LB, GATED>), grid, dim3(WM * WN * 64), 0, s, a);
+        bool held = false;
+        if constexpr (LA == BY_MN && LB == BY_MN) {
+            held = a.a_scales != nullptr;
+            if (held) hipLaunchKernelGGL((k_linear_thirds<BM, BN, WM, WN, LA, LB, GATED, true>), grid, dim3(WM * WN * 64), 0, s, a);
+        }
+        if (!held) hipLaunchKernelGGL((k_linear_thirds<BM, BN, WM, WN, LA, LB, GATED>), grid, dim3(WM * WN * 64), 0, s, a);
     } else {
         if (whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N))
             hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, true, GATED>), grid, dim3(WM * WN * 64), 0, s, a);

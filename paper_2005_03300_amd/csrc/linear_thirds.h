@@ -7,6 +7,7 @@
 // numbers whose h are rounded up can become infinite.  A workgroup that has results that are not finite computes its tile again on the fp32 units, and takes these
 // results from there (and no other, so that none depends on another row's numbers).  Numbers below 2^-100 lose bits of m and l below the smallest bf16 number, 2^-133.
 #pragma once
+#include "held.h"
 #include "linear_tile.h"
 
 namespace gcn {
@@ -15,20 +16,21 @@ namespace gcn {
 // One operand of a stage: 32 values of k of R rows (of A) or columns (of B), as three planes of bf16.
 //   BY_K   64 bytes per row; its four pieces of 8 k are moved about by bits of the row
 //   BY_MN  one row per k of R elements, whose blocks of 16 are moved about as in Operand
-template <int R, int LIES, int THREADS, int HALF = 0>
+template <int R, int LIES, int THREADS, int HALF = 0, class P = Operand<float, R, LIES, THREADS, HALF>>
 struct Thirds {
-    using Plain = Operand<float, R, LIES, THREADS, HALF>;
+    using Plain = P;
     static constexpr int PLANE = R * 64, PER = Plain::PER;
     static constexpr int BLOCKS = R / 16 < 8 ? R / 16 : 8;
     __device__ static int twist(int k) { return ((k & 3) | ((k >> 3 & 1) << 2)) & (BLOCKS - 1); }
-    __device__ static void put(const Vec<float> (&v)[PER], char* lds, int tid) {
+    __device__ static void put(const typename Plain::Piece (&pieces)[PER], char* lds, int tid) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             int row, piece;
             Plain::at(i * THREADS + tid, row, piece);
+            const Vec<float> v = Plain::elements(pieces[i]);
             const int at = LIES == BY_K ? row * 64 + (((piece >> 1) ^ ((row >> 2) & 3)) << 4) + (piece & 1) * 8
                                         : row * (R * 2) + (((piece >> 2) ^ twist(row)) << 5) + (piece & 3) * 8;
-            float x[4] = {v[i][0], v[i][1], v[i][2], v[i][3]};
+            float x[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
                 uint2 words;
@@ -64,15 +66,79 @@ struct Thirds {
     }
 };
 
+// The operand of dW = X^T dZ whose X is a checkpoint, BY_MN: pieces are four codes and their scale until they are split.  For rows of whole pieces, which are in one group each.
+template <int R, int THREADS>
+struct HeldOperand : Operand<float, R, BY_MN, THREADS> {
+    using Base = Operand<float, R, BY_MN, THREADS>;
+    static constexpr int PER = Base::PER;
+    struct Piece {
+        uint32_t codes;
+        uint32_t scale;
+    };
+    __device__ static Vec<float> elements(const Piece& p) {
+        const float s = scale_value(p.scale);
+        const Codes<4> c{{p.codes}};
+        return Vec<float>{s * code_value<4>(c, 0), s * code_value<4>(c, 1), s * code_value<4>(c, 2), s * code_value<4>(c, 3)};
+    }
+    struct Source {
+        const int8_t* src[PER];
+        const uint16_t* scales[PER];
+        int64_t lds;
+    };
+    __device__ static int64_t along(int64_t r0, int piece, int64_t rows) { return Base::piece_at(r0 + piece * 4, rows); }
+    __device__ static Source source(const TileArgs& a, int64_t r0, int64_t k0, int tid) {
+        Source s;
+        s.lds = a.lda_scales;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            int row, piece;
+            Base::at(i * THREADS + tid, row, piece);
+            const int64_t c = along(r0, piece, a.M);
+            s.src[i] = (const int8_t*)a.A + (k0 + row) * a.lda + c;
+            s.scales[i] = a.a_scales + (k0 + row) * a.lda_scales + c / CHECKPOINT_GROUP;
+        }
+        return s;
+    }
+    __device__ static void fetch(Source& s, int64_t ld, Piece (&v)[PER]) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            v[i].codes = reinterpret_cast<const LooseCodes<4>*>(s.src[i])->w[0];
+            v[i].scale = *s.scales[i];
+            s.src[i] += Base::BK * ld;
+            s.scales[i] += Base::BK * s.lds;
+        }
+    }
+    __device__ static void fetch_end(const TileArgs& a, int64_t r0, int64_t k0, int64_t K, Piece (&v)[PER], int tid) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            int row, piece;
+            Base::at(i * THREADS + tid, row, piece);
+            const int64_t c = along(r0, piece, a.M), k = k0 + row;
+            v[i] = Piece{0, 0};
+            if (k < K) {
+                v[i].codes = reinterpret_cast<const LooseCodes<4>*>((const int8_t*)a.A + k * a.lda + c)->w[0];
+                v[i].scale = a.a_scales[k * a.lda_scales + c / CHECKPOINT_GROUP];
+            }
+        }
+    }
+    __device__ static void put(const Piece (&p)[PER], char* lds, int tid) {
+        Vec<float> v[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = elements(p[i]);
+        Base::put(v, lds, tid);
+    }
+};
+
 // As k_linear_tile through registers, for any alignment; one stage in LDS (three planes of 32 k: 48 KB of a 128 x 128 tile), the next one in registers, and another
 // workgroup on the compute unit meanwhile.  Of the compute units' cycles the matrix units are busy in 40 % at 232965 x 602 x 128 (96 products of 16 cycles a stage and wavefront), and
 // vector instructions are issued in 40 %: 22 split four numbers.  (A look at every number for infinities made them as many as the products take: 180 TFLOP/s.)  The second set of
 // results for those that are not finite costs 16 and 18 spilled registers of the 128 x 128 forms whose B lies along n.
-template <int BM, int BN, int WM, int WN, int LA, int LB, bool GATED>
+// HELD: A is a checkpoint.
+template <int BM, int BN, int WM, int WN, int LA, int LB, bool GATED, bool HELD = false>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, BK = 32, E = 4;
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-    using OpA = Thirds<BM, LA, THREADS>;
+    using OpA = Thirds<BM, LA, THREADS, 0, std::conditional_t<HELD, HeldOperand<BM, THREADS>, Operand<float, BM, LA, THREADS>>>;
     using OpB = Thirds<BN, LB, THREADS, GATED ? BN / WN / 2 : 0>;
     using PlainA = typename OpA::Plain;
     using PlainB = typename OpB::Plain;
@@ -91,13 +157,15 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     v4f acc[FM][FN] = {};
     // put(va, vb) and products() for all stages
     auto run = [&](auto put, auto products) {
-        Vec<float> va[OpA::PER], vb[OpB::PER];
+        typename PlainA::Piece va[OpA::PER];
+        Vec<float> vb[OpB::PER];
         int64_t k = kb;
         const int64_t end = (LA == BY_MN && a.M < E) || (LB == BY_MN && a.N < E) ? k : k + (ke - k) / BK * BK;
         typename PlainA::Source sa;
         typename PlainB::Source sb;
         if (k < end) {
-            sa = PlainA::source(A, a.lda, m0, a.M, k, tid);
+            if constexpr (HELD) sa = PlainA::source(a, m0, k, tid);
+            else sa = PlainA::source(A, a.lda, m0, a.M, k, tid);
             sb = PlainB::source(B, a.ldb, n0, a.N, k, tid);
         }
         auto next = [&]() {
@@ -105,7 +173,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
                 PlainA::fetch(sa, a.lda, va);
                 PlainB::fetch(sb, a.ldb, vb);
             } else {
-                PlainA::fetch_end(A, a.lda, m0, a.M, k, ke, va, tid);
+                if constexpr (HELD) PlainA::fetch_end(a, m0, k, ke, va, tid);
+                else PlainA::fetch_end(A, a.lda, m0, a.M, k, ke, va, tid);
                 PlainB::fetch_end(B, a.ldb, n0, a.N, k, ke, vb, tid);
             }
         };
@@ -120,7 +189,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
             if (k >= ke) break;
         }
     };
-    run([&](const Vec<float>(&va)[OpA::PER], const Vec<float>(&vb)[OpB::PER]) {
+    run([&](const typename PlainA::Piece(&va)[OpA::PER], const Vec<float>(&vb)[OpB::PER]) {
             OpA::put(va, stage, tid);
             OpB::put(vb, stage_b, tid);
         },
@@ -153,7 +222,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
             for (int e = 0; e < 4; ++e) lost |= !(fabsf(acc[i][j][e]) < INFINITY);
     if (__syncthreads_or(lost)) {
         v4f plain[FM][FN] = {};
-        run([&](const Vec<float>(&va)[OpA::PER], const Vec<float>(&vb)[OpB::PER]) {
+        run([&](const typename PlainA::Piece(&va)[OpA::PER], const Vec<float>(&vb)[OpB::PER]) {
                 PlainA::put(va, stage, tid);
                 PlainB::put(vb, stage + BM * 128, tid);
             },

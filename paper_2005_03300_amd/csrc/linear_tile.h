@@ -21,6 +21,8 @@ struct TileArgs {
     int32_t N = 0;
     int32_t tiles_m = 0, tiles_n = 0;
     float* part = nullptr;        // partial results, one M x N (gated: M x 2 N) each split; NULL: the epilogue runs here
+    const uint16_t* a_scales = nullptr;          // A is a checkpoint, these its scales
+    int64_t lda_scales = 0;
     // D' = rho R + act(D + 1 bias^T); the argument of act is Z.  Gated: D and Z have 2 N columns, D' = act(Z's first N) (Hadamard) the others
     const float* bias = nullptr;
     const void* R = nullptr;
@@ -185,6 +187,8 @@ struct Operand {
     }
     // Any alignment and any k: through registers.  What lies beyond the matrix along the other dimension is, as with `direct`, something else of it; a piece that its
     // end cuts is the last whole one (see `piece_at`).
+    using Piece = Vec<T>;                                         // of the next stage, in registers, and its elements
+    __device__ static Vec<T> elements(const Piece& p) { return p; }
     struct Source {                                               // where a thread's pieces of the next stage are
         const T* src[PER];
     };
