@@ -183,23 +183,24 @@ inline int splits_of_4(int64_t tiles, int64_t results, int64_t K, bool fp32, int
 //  - The rows of X are read again for every strip, 128 bytes of 64 rows for each 32 of codes that a strip of 64 columns has.  So from 17 rows on, and from 9 on where strips would be 16 columns wide and
 //    k is long, strips are 64 wide and the sum is shared instead, 64 rows and 4096 columns, k of 4096 and 14336, 20 and 59 -> 18 and 31, 16 rows and k of 14336 19 -> 15; with fewer rows the second
 //    launch costs more (1 row 11.6 -> 13.5).
-//  - 64 rows as tiles took 25 and 39 there, 57 with 14336 columns and k of 8192 (so 42), and in fp32, 4096 columns and k of 4096, 42 (so FP32_US).
+//  - Up to 64 rows, and more while strips of 64 columns and blocks of rows give no compute unit a second one: tiles took 25 and 39 for these 64 rows, 57 with 14336 columns and k of 8192 (so 42), and for 128
+//    rows, k and columns 4096, 27 (so 22); in fp32 42 and 46 for 64 and 128 rows (so 20 and 26).
 struct Few4 {
     int rows, columns;
     int64_t splits;
 };
 constexpr int few4_waves(int columns, int rows) { return columns == 1 && rows == 1 ? 16 : 8; }
 inline Few4 few4_choice(int64_t M, int64_t cols, int64_t K, bool fp32, int64_t cus) {
-    Few4 f{M <= 16 ? 1 : M <= 32 ? 2 : 4, 1, 1};
-    if (fp32 && M > 32) f.rows = 2;                               // (registers for no more: twice over the codes)
-    if (M > 64) f.rows = 0;
+    Few4 f{M <= 16 ? 1 : M <= 32 || fp32 ? 2 : 4, 1, 1};          // (fp32: registers for no more than 32 rows, so more go over the codes again)
+    const int64_t blocks = (M + 16 * f.rows - 1) / (16 * f.rows);
+    if (M > 64 && blocks * ((cols + 63) / 64) > cus) return Few4{0, 0, 0};
     const int widest = f.rows == 1 || (f.rows == 2 && !fp32) ? 8 : 4;
-    const bool shared = ((f.rows != 1 && K >= 4096) || (M > 8 && K >= 8192 && cols <= 16 * cus)) && cols <= 64 * cus;
+    const bool shared = (M > 64 || (M > 16 && K >= 4096) || (M > 8 && K >= 8192 && cols <= 16 * cus)) && cols <= 64 * cus;
     if (shared) f.columns = 4;
     else
         while (f.columns < widest && cols > 16 * f.columns * cus) f.columns *= 2;
     const int64_t strips = (cols + 16 * f.columns - 1) / (16 * f.columns), all = 128 * few4_waves(f.columns, f.rows), most = (K + all - 1) / all;
-    if (shared) f.splits = cus / (strips * (f.rows ? (M + 16 * f.rows - 1) / (16 * f.rows) : 1));
+    if (shared) f.splits = cus / (strips * blocks);
     else if (strips < 48) f.splits = 128 / strips;                // as k_linear_few
     f.splits = f.splits < 1 ? 1 : f.splits > most ? most : f.splits;
     return f;
