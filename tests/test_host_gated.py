@@ -148,3 +148,37 @@ def test_binding_looks_at_shapes():
         g.gcn_checkpoint_pack(x, torch.zeros(4, 100, dtype=torch.int8), torch.zeros(4, 2, dtype=torch.bfloat16))
     with pytest.raises(AssertionError):
         g.gcn_linear4_pack(x, torch.zeros(1, 100, dtype=torch.int32), torch.zeros(1, 100, dtype=torch.bfloat16), group=0)
+
+
+def test_sizes_take_the_kernels_that_they_stand_for(tmp_path):
+    """The lists that the GPU tests go through hold every kernel, and their sizes choose it."""
+    from gated_tiles import FEW4, GATED, TILES4
+    from test_host_parts import run_cpp
+    calls = "".join(f"gated({M}, {2 * N}, {K}, {int(t == 'f32')}, {int(w)});" for t, w, _, _, M, N, K in GATED)
+    calls += "".join(f"few({M}, {N}, {K}, {int(t == 'f32')});" for t, _, _, _, M, N, K in FEW4)
+    calls += "".join(f"tiles({M}, {N}, {K}, {int(t == 'f32')});" for t, _, M, N, K in TILES4)
+    r = run_cpp(tmp_path, """
+        #include <cstdio>
+        #include "launch_rules.h"
+        using namespace gcn;
+        void gated(int64_t M, int64_t N, int64_t K, int fp32, int direct) {
+            const TileChoice c = choose_tiles(M, N, K, fp32, direct, 256);
+            printf("%%d %%d\\n", c.edge, c.splits);
+        }
+        void few(int64_t M, int64_t N, int64_t K, int fp32) {
+            const Few4 f = few4_choice(M, N, K, fp32, 256);
+            printf("%%d %%d %%d\\n", f.rows, f.columns, (int)f.splits);
+        }
+        void tiles(int64_t M, int64_t N, int64_t K, int fp32) {
+            printf("%%d %%d\\n", few4_choice(M, N, K, fp32, 256).rows, splits_of_4((M + 127) / 128 * ((N + 127) / 128), M * N, K, fp32, 256));
+        }
+        int main() { %s }
+    """ % calls)
+    got = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
+    want = [p[2:4] for p in GATED] + [p[1:4] for p in FEW4] + [(0, p[1]) for p in TILES4]
+    assert got == want, [(g_, w_) for g_, w_ in zip(got, want) if g_ != w_]
+    assert {(p[0], p[1], p[2], p[3] > 1) for p in GATED} == {("16", w, e, s) for w in (False, True) for e in (256, 128, 64) for s in (False, True)} | {
+        ("f32", False, e, s) for e in (128, 64) for s in (False, True)}
+    assert {(p[0], p[1], p[2]) for p in FEW4} == {("16", r, c) for r in (1, 2, 4) for c in (1, 2, 4, 8) if (r, c) != (4, 8)} | {("f32", 1, c) for c in (1, 4, 8)} | {
+        ("f32", 2, c) for c in (1, 2, 4)}
+    assert {p[0] for p in FEW4 if p[3] > 1} == {p[0] for p in TILES4 if p[1] > 1} == {"16", "f32"}
