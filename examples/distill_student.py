@@ -9,7 +9,10 @@ once) pass through residual blocks
 and a last linear layer; its loss is gcn_distill against the teacher's k largest logits per vertex and the labels.  Answering for a
 vertex afterwards needs neither the graph nor the teacher.
 
-    python examples/distill_student.py [--type bf16|f16|f32] [--blocks 2] [--width 128] [--steps 200]
+With --gated the blocks' first layer is a gated one, act(H Wg + bg) * (H Wu + bu); between the forward and the backward pass its argument and
+input are kept in 8 bits, and its output is computed again.  Such a student also answers from weights held in 4 bits.
+
+    python examples/distill_student.py [--type bf16|f16|f32] [--blocks 2] [--width 128] [--steps 200] [--gated]
 """
 from __future__ import annotations
 
@@ -64,17 +67,18 @@ def teacher(steps: int = 600, lr: float = 30.0):
 class Student:
     """Weights in the element type with fp32 copies that the steps are taken on; buffers for one training step over n rows."""
 
-    def __init__(self, n: int, f_in: int, width: int, classes: int, blocks: int, dtype, seed: int = 0):
+    def __init__(self, n: int, f_in: int, width: int, classes: int, blocks: int, dtype, seed: int = 0, gated: bool = False):
         gen = torch.Generator(device="cuda").manual_seed(seed)
-        self.dtype, self.blocks, self.n = dtype, blocks, n
+        self.dtype, self.blocks, self.n, self.gated = dtype, blocks, n, gated
+        inner = 4 * width if gated else 2 * width                 # columns of a block's first layer: of the gate and of what it opens
 
         def glorot(i, o):
             return torch.randn(i, o, generator=gen, device="cuda") * (2.0 / (i + o)) ** 0.5
         self.master = {"in": glorot(f_in, width), "out": glorot(width, classes)}
         self.vec = {"in.b": torch.zeros(width, device="cuda"), "norm0": torch.ones(width, device="cuda")}
         for l in range(blocks):
-            self.master.update({f"{l}.W1": glorot(width, 2 * width), f"{l}.W2": glorot(2 * width, width), f"{l}.G": glorot(width, width)})
-            self.vec.update({f"{l}.b1": torch.zeros(2 * width, device="cuda"), f"{l}.b2": torch.zeros(width, device="cuda"),
+            self.master.update({f"{l}.W1": glorot(width, inner), f"{l}.W2": glorot(2 * width, width), f"{l}.G": glorot(width, width)})
+            self.vec.update({f"{l}.b1": torch.zeros(inner, device="cuda"), f"{l}.b2": torch.zeros(width, device="cuda"),
                              f"{l}.scale": torch.full((width,), 0.5, device="cuda"), f"{l}.post": torch.ones(width, device="cuda"),
                              f"norm{l + 1}": torch.ones(width, device="cuda")})
         self.W = {k: v.to(dtype) for k, v in self.master.items()}
@@ -83,11 +87,17 @@ class Student:
         e = lambda cols: torch.empty(n, cols, dtype=dtype, device="cuda")
         rows = lambda: torch.empty(n, 4, device="cuda")
         self.X, self.H, self.st = [e(width) for _ in range(blocks + 1)], [e(width) for _ in range(blocks + 1)], [rows() for _ in range(blocks + 1)]
-        self.Z1, self.Y1 = [e(2 * width) for _ in range(blocks)], [e(2 * width) for _ in range(blocks)]
+        if gated:                                                 # one block's at a time; what is kept of each are checkpoints
+            self.Z1, self.Y1 = [e(inner)] * blocks, [e(2 * width)] * blocks
+            held = lambda cols: (torch.empty(n, cols, dtype=torch.int8, device="cuda"),
+                                 torch.empty(n, -(-cols // g.CHECKPOINT_GROUP), dtype=torch.bfloat16, device="cuda"))
+            self.H8, self.Z8 = [held(width) for _ in range(blocks)], [held(inner) for _ in range(blocks)]
+        else:
+            self.Z1, self.Y1 = [e(inner) for _ in range(blocks)], [e(inner) for _ in range(blocks)]
         self.U, self.A = [e(width) for _ in range(blocks)], [e(width) for _ in range(blocks)]
         self.logits, self.G = e(classes), e(classes)
         self.dX, self.dH, self.dH2, self.dU, self.dA = (e(width) for _ in range(5))
-        self.dY1, self.dZ1 = e(2 * width), e(2 * width)
+        self.dY1, self.dZ1 = e(2 * width), e(inner)
         self.loss = torch.empty(1, device="cuda")
         self.momentum = {}
 
@@ -97,7 +107,12 @@ class Student:
         g.gcn_block_norm_forward(self.X[0], H=self.H[0], w_pre=v["norm0"], stats=self.st[0])
         for l in range(self.blocks):
             H = self.H[l]
-            g.gcn_linear_forward(H, W[f"{l}.W1"], self.Y1[l], bias=v[f"{l}.b1"], act=g.ACT_GELU, Z=self.Z1[l])
+            if self.gated:
+                g.gcn_gated_forward(H, W[f"{l}.W1"], self.Y1[l], bias=v[f"{l}.b1"], Z=self.Z1[l])
+                g.gcn_checkpoint_pack(self.Z1[l], *self.Z8[l])
+                g.gcn_checkpoint_pack(H, *self.H8[l])
+            else:
+                g.gcn_linear_forward(H, W[f"{l}.W1"], self.Y1[l], bias=v[f"{l}.b1"], act=g.ACT_GELU, Z=self.Z1[l])
             g.gcn_linear_forward(self.Y1[l], W[f"{l}.W2"], self.U[l], bias=v[f"{l}.b2"])
             g.gcn_linear_forward(H, W[f"{l}.G"], self.A[l])
             g.gcn_block_norm_forward(self.X[l], self.U[l], self.X[l + 1], self.H[l + 1], w_pre=v[f"norm{l + 1}"], A=self.A[l],
@@ -119,9 +134,15 @@ class Student:
                                       A=self.A[l], dA=self.dA, scale=v[f"{l}.scale"], w_post=v[f"{l}.post"], dscale=dv[f"{l}.scale"],
                                       dw_post=dv[f"{l}.post"], dw_pre=dv[f"norm{l + 1}"])
             dXout = self.dX
-            g.gcn_linear_backward(self.Y1[l], W[f"{l}.W2"], None, self.dU, dX=self.dY1, dW=dW[f"{l}.W2"], dbias=dv[f"{l}.b2"])
-            g.gcn_linear_backward(self.H[l], W[f"{l}.W1"], self.Z1[l], self.dY1, self.dZ1, dX=self.dH, dW=dW[f"{l}.W1"],
-                                  dbias=dv[f"{l}.b1"], act=g.ACT_GELU)
+            if self.gated:
+                g.gcn_linear_backward(None, W[f"{l}.W2"], None, self.dU, dX=self.dY1, dbias=dv[f"{l}.b2"])
+                g.gcn_gated_backward(self.H8[l], W[f"{l}.W1"], self.Z8[l], self.dY1, self.dZ1, dX=self.dH, dW=dW[f"{l}.W1"],
+                                     dbias=dv[f"{l}.b1"], H=self.Y1[l])
+                g.gcn_linear_backward(self.Y1[l], None, None, self.dU, dW=dW[f"{l}.W2"])
+            else:
+                g.gcn_linear_backward(self.Y1[l], W[f"{l}.W2"], None, self.dU, dX=self.dY1, dW=dW[f"{l}.W2"], dbias=dv[f"{l}.b2"])
+                g.gcn_linear_backward(self.H[l], W[f"{l}.W1"], self.Z1[l], self.dY1, self.dZ1, dX=self.dH, dW=dW[f"{l}.W1"],
+                                      dbias=dv[f"{l}.b1"], act=g.ACT_GELU)
             g.gcn_linear_backward(self.H[l], W[f"{l}.G"], None, self.dA, dX=self.dH2, dW=dW[f"{l}.G"])
             self.dH += self.dH2
         g.gcn_block_norm_backward(None, self.X[0], self.st[0], dXout, self.dH, self.dX, w_pre=v["norm0"], dw_pre=dv["norm0"])
@@ -140,13 +161,39 @@ class Student:
         return lr * b
 
 
-def train(dtype: str = "bf16", blocks: int = 2, width: int = 128, steps: int = 200, k: int = 4, lr: float = 0.1, say=print):
+class FourBits:
+    """A gated student's weights in 4 bits, and its answers from them."""
+
+    def __init__(self, student: Student, group: int = 32):
+        self.s, self.group, self.W = student, group, {}
+        for k, m in student.master.items():
+            rows, cols = m.shape
+            self.W[k] = (torch.empty(-(-rows // 8), cols, dtype=torch.int32, device="cuda"),
+                         torch.empty(-(-rows // group), cols, dtype=torch.bfloat16, device="cuda"))
+            g.gcn_linear4_pack(m, *self.W[k], group=group)
+
+    def answer(self, P):
+        s, v = self.s, self.s.vec
+        rows = lambda k, gated=False: torch.empty(P.shape[0], self.W[k][0].shape[1] // (2 if gated else 1), dtype=s.dtype, device="cuda")
+
+        def layer(X, k, **how):
+            return g.gcn_linear4_forward(X, *self.W[k], rows(k, how.get("gated", False)), group=self.group, **how)
+        X = layer(P, "in", bias=v["in.b"])
+        H = torch.empty_like(X)
+        g.gcn_block_norm_forward(X, H=H, w_pre=v["norm0"])
+        for l in range(s.blocks):
+            U = layer(layer(H, f"{l}.W1", bias=v[f"{l}.b1"], act=g.ACT_SILU, gated=True), f"{l}.W2", bias=v[f"{l}.b2"])
+            g.gcn_block_norm_forward(X, U, X, H, w_pre=v[f"norm{l + 1}"], A=layer(H, f"{l}.G"), scale=v[f"{l}.scale"], w_post=v[f"{l}.post"])
+        return layer(H, "out")
+
+
+def train(dtype: str = "bf16", blocks: int = 2, width: int = 128, steps: int = 200, k: int = 4, lr: float = 0.1, say=print, gated: bool = False):
     """Trains a student; returns (first loss, last loss, share of vertices on which it agrees with the teacher)."""
     logits, labels, P = teacher()
     dt = TYPES[dtype]
     t, top = logits.topk(k, dim=1)
     t, top, P = t.to(dt).contiguous(), top.int().contiguous(), ((P - P.mean(0)) / P.std(0)).to(dt)
-    s = Student(P.shape[0], P.shape[1], width, logits.shape[1], blocks, dt)
+    s = Student(P.shape[0], P.shape[1], width, logits.shape[1], blocks, dt, gated=gated)
     first = None
     for i in range(steps):
         loss = s.step(P, top, t, labels, lr * (1.0 - i / steps))
@@ -155,10 +202,15 @@ def train(dtype: str = "bf16", blocks: int = 2, width: int = 128, steps: int = 2
         first = loss.item() if first is None else first
     agree = (s.forward(P).argmax(1) == logits.argmax(1)).float().mean().item()
     one = torch.empty(1, logits.shape[1], dtype=dt, device="cuda")         # a single vertex, as in serving
-    alone = Student(1, P.shape[1], width, logits.shape[1], blocks, dt)
+    alone = Student(1, P.shape[1], width, logits.shape[1], blocks, dt, gated=gated)
     alone.W, alone.vec = s.W, s.vec
     one.copy_(alone.forward(P[:1].contiguous()))
     say(f"agrees with the teacher on {100 * agree:.1f} % of the vertices; vertex 0 alone: class {one.argmax().item()}")
+    if gated:
+        four = FourBits(s)
+        same = (four.answer(P).argmax(1) == logits.argmax(1)).float().mean().item()
+        one = four.answer(P[:1].contiguous())
+        say(f"from weights in 4 bits it agrees on {100 * same:.1f} %; vertex 0 alone: class {one.argmax().item()}")
     return first, s.loss.item(), agree
 
 
@@ -168,5 +220,6 @@ if __name__ == "__main__":
     ap.add_argument("--blocks", type=int, default=2)
     ap.add_argument("--width", type=int, default=128)
     ap.add_argument("--steps", type=int, default=200)
+    ap.add_argument("--gated", action="store_true")
     args = ap.parse_args()
-    train(args.type, args.blocks, args.width, args.steps)
+    train(args.type, args.blocks, args.width, args.steps, gated=args.gated)
