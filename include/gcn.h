@@ -315,7 +315,8 @@ int gcn_gated_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const v
  * codes: int8, n x f, ldc >= f apart; scales: bf16, n x ceil(f / GCN_CHECKPOINT_GROUP), lds apart; X: n x f elements; any alignment; widths up to 2^27 (RANGE).
  * pack writes codes and scales, unpack X; no output may overlap an input or another output.
  * gcn_checkpoint_linear_backward: gcn_linear_backward from checkpoints.  x_scales, z_scales: NULL, or X (Z) is a checkpoint, X the codes (int8, ldx apart) and x_scales their scales; the rest as
- * there, except that dZ may not be the codes.
+ * there, except that dZ may not be the codes.  Scratch of it and of gcn_gated_backward, where X is a checkpoint and dW wanted: the n x f_in elements that it stands for (rows rounded up to 16 bytes); none
+ * with fp32 elements and f_in a multiple of 4.
  * ----------------------------------------------------------------------------------------- */
 int gcn_checkpoint_pack(int64_t n, int32_t f, int type, const void* X, int64_t ldx, int8_t* codes, int64_t ldc, uint16_t* scales, int64_t lds,
                         void* stream);
@@ -335,7 +336,8 @@ int gcn_checkpoint_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int t
  * Q: words, ceil(f_in / 8) x cols, ldq apart; word (j, c) holds the codes of W[8 j .. 8 j + 7, c], the first in its lowest bits; those beyond f_in are 0.  S: bf16, ceil(f_in / group) x cols, lds
  * apart.  cols: the columns of W, f_out or, gated, 2 f_out; a block of columns of Q and S at the same leading dimensions holds that block of columns of W.
  * pack: W, f_in x cols of element type `type`, to Q and S; unpack: back, each weight rounded to the type; no output may overlap an input or another output.
- * forward: the weights enter the products as they are held, without a rounding: sums over a group in fp32, times the scale, added in fp32 in a fixed order.  bias: fp32[cols] or NULL; R may be
+ * forward: the weights enter the products as they are held, without a rounding (and of fp32 elements all bits): sums over a group in fp32, times the scale, added in fp32 in a fixed order; bf16 and fp32 numbers
+ * of X below 2^-100 lose bits below 2^-133.  The elements may be of another type than the weights were packed from.  bias: fp32[cols] or NULL; R may be
  * NULL; Y may be R (same address and leading dimension) and may overlap no other input.  Roundings, activations and alignment as gcn_linear_forward; f_in and cols up to 2^27 (RANGE).
  * ----------------------------------------------------------------------------------------- */
 int gcn_linear4_pack(int32_t f_in, int32_t cols, int type, const void* W, int64_t ldw, int group, uint32_t* Q, int64_t ldq, uint16_t* S,

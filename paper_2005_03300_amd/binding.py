@@ -388,7 +388,7 @@ def gcn_linear_backward(X, W, Z, dY, dZ=None, dX=None, dW=None, dbias=None, act:
 def _kept(t, shape, dtype):
     """Address and leading dimension of a matrix that was kept, and of its scales: of a tensor (no scales), or of a checkpoint, the pair of its codes
     and scales."""
-    if not isinstance(t, tuple):
+    if not isinstance(t, (tuple, list)):
         return *_mat(t, shape, dtype), 0, 0
     codes, scales = t
     return *_mat(codes, shape, _i8), *_mat(scales, (shape[0], -(-shape[1] // CHECKPOINT_GROUP)), _bf16)
@@ -415,7 +415,7 @@ def gcn_gated_backward(X, W, Z, dH, dZ=None, dX=None, dW=None, dbias=None, act: 
     dt, out = dH.dtype, dH.shape
     n, m = out
     both = (n, 2 * m)
-    f_in = (X[0] if isinstance(X, tuple) else X).shape[1] if X is not None else W.shape[0] if W is not None else 1
+    f_in = (X[0] if isinstance(X, (tuple, list)) else X).shape[1] if X is not None else W.shape[0] if W is not None else 1
     rows, weights = (n, f_in), (f_in, 2 * m)
     rc = L.gcn_gated_backward(n, f_in, m, _type_of(dt), *_kept(X, rows, dt), *_mat(W, weights, dt), *_kept(Z, both, dt), *_mat(dH, out, dt), act,
                               *_mat(dZ, both, dt), *_mat(dX, rows, dt), *_mat(dW, weights, dt), _vec(dbias, (2 * m,)), *_mat(H, out, dt),
@@ -451,7 +451,7 @@ def gcn_checkpoint_linear_backward(X, W, Z, dY, dZ=None, dX=None, dW=None, dbias
     L = _lib or lib()
     dt, out = dY.dtype, dY.shape
     n, f_out = out
-    f_in = (X[0] if isinstance(X, tuple) else X).shape[1] if X is not None else W.shape[0] if W is not None else 1
+    f_in = (X[0] if isinstance(X, (tuple, list)) else X).shape[1] if X is not None else W.shape[0] if W is not None else 1
     rows, weights = (n, f_in), (f_in, f_out)
     rc = L.gcn_checkpoint_linear_backward(n, f_in, f_out, _type_of(dt), *_kept(X, rows, dt), *_mat(W, weights, dt), *_kept(Z, out, dt),
                                           *_mat(dY, out, dt), act, rho, *_mat(dZ, out, dt), *_mat(dX, rows, dt), *_mat(dW, weights, dt),

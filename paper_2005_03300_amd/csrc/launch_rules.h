@@ -193,7 +193,7 @@ constexpr int few4_waves(int columns, int rows) { return columns == 1 && rows ==
 inline Few4 few4_choice(int64_t M, int64_t cols, int64_t K, bool fp32, int64_t cus) {
     Few4 f{M <= 16 ? 1 : M <= 32 || fp32 ? 2 : 4, 1, 1};          // (fp32: registers for no more than 32 rows, so more go over the codes again)
     const int64_t blocks = (M + 16 * f.rows - 1) / (16 * f.rows);
-    if (M > 64 && blocks * ((cols + 63) / 64) > cus) return Few4{0, 0, 0};
+    if (M > 64 && blocks * ((cols + 63) / 64) > cus && K >= (fp32 ? 4 : 8)) return Few4{0, 0, 0};          // (tiles take rows of 16 bytes and more)
     const int widest = f.rows == 1 || (f.rows == 2 && !fp32) ? 8 : 4;
     const bool shared = (M > 64 || (M > 16 && K >= 4096) || (M > 8 && K >= 8192 && cols <= 16 * cus)) && cols <= 64 * cus;
     if (shared) f.columns = 4;

@@ -413,7 +413,7 @@ template <typename T, bool GATED>
 static int linear4_impl(const TileArgs& a, const Weights4& w, hipStream_t s) {
     constexpr bool FP32 = sizeof(T) == 4;
     const Few4 f = few4_choice(a.M, GATED ? 2 * (int64_t)a.N : a.N, a.K, FP32, device_info().cus);
-    if (f.rows == 0 && a.K >= Elem<T>::E) return launch_tile4<T, GATED>(a, w, s);
+    if (f.rows == 0) return launch_tile4<T, GATED>(a, w, s);
     auto by_columns = [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
         if constexpr (RT == 1 || (RT == 2 && !FP32))

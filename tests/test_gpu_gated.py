@@ -437,7 +437,7 @@ def test_checkpoint_that_stands_for_nan():
 LINEAR4 = [(1, 1, 1, 32, 0, 0), (1, 64, 64, 64, 0, 0), (1, 1000, 300, 128, 0, 0), (1, 4096, 48, 32, 8, 0), (2, 4096, 40, 128, 8, 0), (3, 5, 7, 32, 0, 1), (16, 512, 1024, 64, 0, 0), (17, 33, 65, 32, 3, 0),
            (32, 160, 96, 64, 0, 8), (33, 160, 96, 128, 0, 8), (64, 64, 64, 32, 0, 0), (65, 128, 129, 64, 0, 0), (130, 602, 41, 128, 0, 0), (257, 96, 304, 32, 16, 0), (1000, 37, 8, 64, 0, 0),
            (2049, 72, 808, 32, 0, 0), (2049, 71, 801, 64, 1, 1), (1027, 520, 2048, 128, 0, 0), (20001, 48, 24, 64, 0, 0), (9, 3000, 17, 32, 0, 0), (8, 24, 20000, 64, 0, 0),
-           (5, 20000, 24, 128, 0, 0), (40, 8200, 72, 64, 0, 0), (100, 3, 50, 32, 0, 0), (70, 7, 200, 128, 0, 1), (301, 1, 9, 64, 2, 0)]
+           (5, 20000, 24, 128, 0, 0), (40, 8200, 72, 64, 0, 0), (100, 3, 50, 32, 0, 0), (70, 7, 200, 128, 0, 1), (301, 1, 9, 64, 2, 0), (20000, 3, 300, 32, 0, 0), (70001, 2, 5, 64, 0, 0)]
 
 
 @pytest.mark.parametrize("gated", [False, True])

@@ -181,4 +181,21 @@ def test_sizes_take_the_kernels_that_they_stand_for(tmp_path):
         ("f32", False, e, s) for e in (128, 64) for s in (False, True)}
     assert {(p[0], p[1], p[2]) for p in FEW4} == {("16", r, c) for r in (1, 2, 4) for c in (1, 2, 4, 8) if (r, c) != (4, 8)} | {("f32", 1, c) for c in (1, 4, 8)} | {
         ("f32", 2, c) for c in (1, 2, 4)}
+    # k shorter than 16 bytes, which tiles do not take: any number of rows goes the other way
+    r = run_cpp(tmp_path, """
+        #include <cstdio>
+        #include <initializer_list>
+        #include "launch_rules.h"
+        int main() {
+            for (int64_t M : {1, 65, 20000, 100000000})
+                for (int64_t cols : {1, 300, 1 << 27})
+                    for (int64_t K : {1, 3, 7, 8, 100, 1 << 27})
+                        for (int fp32 : {0, 1}) {
+                            const gcn::Few4 f = gcn::few4_choice(M, cols, K, fp32, 256);
+                            const bool tiles = K >= (fp32 ? 4 : 8);
+                            if (f.rows == 0 ? !tiles : f.columns < 1 || f.splits < 1) return printf("%lld %lld %lld\\n", (long long)M, (long long)cols, (long long)K), 1;
+                        }
+        }
+    """)
+    assert r.returncode == 0, r.stdout
     assert {p[0] for p in FEW4 if p[3] > 1} == {p[0] for p in TILES4 if p[1] > 1} == {"16", "f32"}
