@@ -49,15 +49,21 @@ __device__ __forceinline__ uint32_t lowest_bytes(uint32_t a, uint32_t b, uint32_
 #endif
 }
 
-// The pieces of a matrix, `per` of each row, that a lane comes to: from number t on every `step`th.
+// The pieces of a matrix, `per` of each row, that a lane comes to: the lane's own and then as many further on as there are lanes, which are `rows` rows and `pieces` pieces.
 struct Walk {
     int64_t row;
-    int32_t piece, per, step_pieces;
-    int64_t step_rows;
-    __device__ Walk(int64_t t, int32_t per, int64_t step) : row(t / per), piece((int32_t)(t % per)), per(per), step_pieces((int32_t)(step % per)), step_rows(step / per) {}
+    int32_t piece, per, pieces;
+    int64_t rows;
+    __device__ Walk(int32_t per, int32_t lanes) : per(per) {
+        const uint32_t t = blockIdx.x * 256 + threadIdx.x;       // (a launch has up to 2^20 lanes)
+        row = t / (uint32_t)per;
+        piece = (int32_t)(t % (uint32_t)per);
+        rows = lanes / per;
+        pieces = lanes % per;
+    }
     __device__ void next() {
-        row += step_rows;
-        piece += step_pieces;
+        row += rows;
+        piece += pieces;
         if (piece >= per) {
             piece -= per;
             ++row;
@@ -72,7 +78,7 @@ __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, c
     constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E, A = 2;
     const int32_t per = (int32_t)groups_of(f, CHECKPOINT_GROUP) * L;          // lanes of a row
     const int32_t end = f % CHECKPOINT_GROUP, last = end == 0 || end >= E ? f - E : f;         // where the last whole piece of the last group begins
-    Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, per, (int64_t)gridDim.x * 256);
+    Walk at(per, gridDim.x * 256);
     while (at.row < n) {                                          // (a group's lanes go together)
         Vec<T> x[A];
         int64_t row[A];
@@ -122,7 +128,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f, const int8_t* C, int64_t ldc, const uint16_t* S, int64_t lds, T* X, int64_t ldx) {
     constexpr int E = Elem<T>::E, A = 4;
     const int32_t last = f - E;
-    Walk at((int64_t)blockIdx.x * 256 + threadIdx.x, (int32_t)groups_of(f, E), (int64_t)gridDim.x * 256);
+    Walk at((int32_t)groups_of(f, E), gridDim.x * 256);
     while (at.row < n) {
         Codes<E> q[A];
         uint16_t s[A][2];
@@ -154,8 +160,8 @@ __global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f,
     }
 }
 
-static unsigned passes(int64_t lanes) {                           // workgroups of a pass over matrices
-    const int64_t blocks = (lanes + 255) / 256, most = 16 * (int64_t)device_info().cus;
+static unsigned passes(int64_t pieces) {                          // workgroups of a pass over matrices: two pieces for each lane, and more
+    const int64_t blocks = (pieces + 511) / 512, most = 16 * (int64_t)device_info().cus;
     return (unsigned)(blocks < most ? blocks : most);
 }
 

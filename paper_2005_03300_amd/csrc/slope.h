@@ -26,22 +26,26 @@ struct SlopeArgs {
     void* also = nullptr;             // H of a gated block, dR of a linear layer; or NULL
     int64_t lddy = 0, lddz = 0, ldalso = 0;
     int act = GCN_ACT_NONE;
+    int lanes = 64;                   // of a wavefront for a row
     float rho = 1;
     float* part = nullptr;            // sums of each share of the rows, or NULL
 };
 
 // One pass over the matrices, bound by memory (a linear layer's 8192 x 4096 in fp16 with SiLU: 201 MB in 45 us, 4.5 TB/s).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two
-// such sets on their way, and a share of the rows; the four row sets are added in order.
+// or four such sets on their way, and a share of the rows; the four row sets are added in order.  Of gated blocks and of checkpoints a wavefront has several rows where they are short, `lanes`
+// of it for each, a power of two, and folds their sums first (56450 x 20 of a gated block in fp16: all 64 lanes for a row 106 us, four 18).
 // dZ is rounded to the element type here: both products take it from memory, and 16-bit matrix units take no more.  As the sum of two 16-bit numbers it would lose
 // nothing that counts, and both products would be twice as long (8192 x 1024 x 4096 in fp16: 160 us more on 210).  So dX and dW are off by what the roundings of dZ come to, about as much as by their own
 // (2.9e-4 of their norm in fp16 where the sum of an unrounded dZ has 2.1e-4, 2.3e-3 and 1.7e-3 in bf16); the bias's gradient is the sum of what was not rounded.
 template <typename T, bool GATED, bool HELD>
 __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
-    constexpr int E = Elem<T>::E, SETS = 4, AHEAD = GATED ? 2 : 4, HALVES = GATED ? 2 : 1;
-    __shared__ float sums[SETS][64][HALVES * E + 1];
-    const int lane = threadIdx.x & 63, set = threadIdx.x >> 6;
+    constexpr int E = Elem<T>::E, WAVES = 4, AHEAD = GATED ? 2 : 4, HALVES = GATED ? 2 : 1;
+    constexpr bool NARROW = GATED || HELD;                        // (linear layers keep the order of their sums)
+    __shared__ float sums[WAVES][64][HALVES * E + 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lanes = NARROW ? a.lanes : 64, SETS = WAVES * (64 / lanes), set = (int)threadIdx.x / lanes;
     const int32_t N = a.N;
-    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * E, width = (int64_t)HALVES * N;
+    const int64_t c = ((int64_t)blockIdx.x * lanes + (lane & (lanes - 1))) * E, width = (int64_t)HALVES * N;
     const int64_t rb = (int64_t)blockIdx.y * a.rows_per_block, re = rb + a.rows_per_block < a.n ? rb + a.rows_per_block : a.n;
     const int count = c >= N ? 0 : N - c < E ? (int)(N - c) : E;
     const bool apart = GATED && N % E != 0;                       // a piece of the second half can lie in two groups
@@ -124,21 +128,30 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
                 if (i + u * SETS < re) row(i + u * SETS, p[u]);
         }
     };
-    // a workgroup whose columns are not all whole pieces goes the other way with all of them: two ways one after the other took twice as long (4099 x 1001 WAYS_US)
-    if (((int64_t)blockIdx.x + 1) * 64 * E <= N) rows(std::true_type());
-    else if (count > 0) rows(std::false_type());
+    // a workgroup whose columns are not all whole pieces goes the other way with all of them: two ways one after the other took twice as long (4099 x 1001 of a gated block from a checkpoint in bf16: 22 us, 32)
+    if (((int64_t)blockIdx.x + 1) * lanes * E <= N || N % E == 0) {
+        if (count > 0) rows(std::true_type());
+    } else if (count > 0) {
+        rows(std::false_type());
+    }
     if (!a.part) return;
+    if constexpr (NARROW)
+        for (int d = 32; d >= lanes; d >>= 1)                     // the rows of a wavefront
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[h][e] += __shfl_xor(sum[h][e], d);
 #pragma unroll
     for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-        for (int e = 0; e < E; ++e) sums[set][lane][h * E + e] = sum[h][e];
+        for (int e = 0; e < E; ++e) sums[wave][lane][h * E + e] = sum[h][e];
     __syncthreads();
-    if (set) return;
+    if (wave || lane >= lanes) return;
 #pragma unroll
     for (int h = 0; h < HALVES; ++h)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            for (int w = 1; w < SETS; ++w) sum[h][e] += sums[w][lane][h * E + e];
+            for (int w = 1; w < WAVES; ++w) sum[h][e] += sums[w][lane][h * E + e];
             if (e < count) a.part[(int64_t)blockIdx.y * width + (int64_t)h * N + c + e] = sum[h][e];
         }
 }
@@ -148,9 +161,12 @@ int launch_column_sums(const float* part, int parts, int32_t count, float* out, 
 
 template <typename T, bool GATED, bool HELD>
 static int launch_slope(SlopeArgs a, float* dbias, hipStream_t s) {
-    const int64_t wide = 64 * Elem<T>::E, across = (a.N + wide - 1) / wide, width = (int64_t)a.N * (GATED ? 2 : 1);
-    const RowShares shares = row_shares(a.n, across, device_info().cus);
-    a.rows_per_block = shares.rows;
+    if (GATED || HELD)
+        for (; a.lanes > 1 && a.lanes / 2 * Elem<T>::E >= a.N; a.lanes /= 2) {}
+    const int64_t wide = a.lanes * Elem<T>::E, across = (a.N + wide - 1) / wide, width = (int64_t)a.N * (GATED ? 2 : 1), together = 64 / a.lanes;
+    RowShares shares = row_shares((a.n + together - 1) / together, across, device_info().cus);       // of as many rows as a wavefront has together
+    a.rows_per_block = shares.rows *= together;
+    shares.count = (a.n + shares.rows - 1) / shares.rows;
     ScratchLease lease;
     void* part = dbias;                                           // the sums of a single share of the rows are the result
     if (dbias && shares.count > 1) GCN_TRY(lease.get(&part, (size_t)shares.count * width * 4, s));
