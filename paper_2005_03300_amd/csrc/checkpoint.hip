@@ -188,13 +188,14 @@ int back_products(int type, const BackProducts& b, hipStream_t s) {
             if (b.X.scales && sizeof(T) == 4 && b.f_in % 4 == 0) {             // fp32 products split their operands on the way to LDS, and codes as well
                 a.a_scales = b.X.scales;
                 a.lda_scales = b.X.lds;
-            } else if (b.X.scales) {
+            } else if (b.X.scales) {                              // into rows of whole pieces, which the tiles take straight to LDS (dW of 25809 x 2271 x 800 in fp16 127 us, 166 in rows of 2271)
                 void* p = nullptr;
                 ldx = groups_of(b.f_in, Elem<T>::E) * Elem<T>::E;
                 GCN_TRY(lease.get(&p, (size_t)b.n * ldx * sizeof(T), s));
                 GCN_TRY(unpack_launch<T>(b.n, b.f_in, b.X, p, ldx, s));
                 X = p;
             }
+            a.a_wide = X == b.X.p ? 0 : ldx;
             a.A = X; a.lda = ldx; a.B = b.G; a.ldb = b.ldg; a.M = b.f_in; a.N = b.cols; a.K = b.n; a.Y = b.dW; a.ldy = b.lddw;
             GCN_TRY(linear_dw_of<T>(a, s));
         }

@@ -33,7 +33,7 @@ static int launch_tile(TileArgs a, int splits, hipStream_t s) {
         }
         if (!held) hipLaunchKernelGGL((k_linear_thirds<BM, BN, WM, WN, LA, LB, GATED>), grid, dim3(WM * WN * 64), 0, s, a);
     } else {
-        if (whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N))
+        if (whole_pieces<T, LA>(a.A, a.lda, a.wide_a()) && whole_pieces<T, LB>(a.B, a.ldb, a.N))
             hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, true, GATED>), grid, dim3(WM * WN * 64), 0, s, a);
         else
             hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, LA, LB, false, GATED>), grid, dim3(WM * WN * 64), 0, s, a);
@@ -45,7 +45,7 @@ static int launch_tile(TileArgs a, int splits, hipStream_t s) {
 
 template <typename T, int LA, int LB, bool GATED = false>
 static int linear_product(const TileArgs& a, hipStream_t s) {
-    const bool direct = whole_pieces<T, LA>(a.A, a.lda, a.M) && whole_pieces<T, LB>(a.B, a.ldb, a.N);
+    const bool direct = whole_pieces<T, LA>(a.A, a.lda, a.wide_a()) && whole_pieces<T, LB>(a.B, a.ldb, a.N);
     const TileChoice c = choose_tiles(a.M, GATED ? 2 * (int64_t)a.N : a.N, a.K, sizeof(T) == 4, sizeof(T) == 2 && direct, device_info().cus);
     if constexpr (sizeof(T) == 2)
         if (c.edge == 256) return launch_tile<T, 256, 256, 2, 4, LA, LB, GATED>(a, c.splits, s);

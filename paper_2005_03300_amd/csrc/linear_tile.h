@@ -23,6 +23,8 @@ struct TileArgs {
     float* part = nullptr;        // partial results, one M x N (gated: M x 2 N) each split; NULL: the epilogue runs here
     const uint16_t* a_scales = nullptr;          // A is a checkpoint, these its scales
     int64_t lda_scales = 0;
+    int64_t a_wide = 0;           // elements that rows of A have, where that is more than M (A by m): the others are anything, as their results are not stored
+    __host__ __device__ int64_t wide_a() const { return a_wide ? a_wide : M; }
     // D' = rho R + act(D + 1 bias^T); the argument of act is Z.  Gated: D and Z have 2 N columns, D' = act(Z's first N) (Hadamard) the others
     const float* bias = nullptr;
     const void* R = nullptr;
@@ -492,6 +494,7 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
     const int64_t kb = (int64_t)blockIdx.y * a.k_share, ke = kb + a.k_share < a.K ? kb + a.k_share : a.K;
     const T* const A = (const T*)a.A;
     const T* const B = (const T*)a.B;
+    const int64_t wide = DIRECT && LA == BY_MN ? a.wide_a() : a.M;
     const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
     v4f acc[FM][FN] = {};
 
@@ -512,7 +515,7 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
     const int64_t whole = DIRECT ? (ke - kb) / BK : 0;
     if (DIRECT && whole > 0) {
         auto send = [&](char* stage, int64_t t) {
-            OpA::direct(A, a.lda, m0, a.M, kb + t * BK, stage, tid);
+            OpA::direct(A, a.lda, m0, wide, kb + t * BK, stage, tid);
             OpB::direct(B, a.ldb, n0, a.N, kb + t * BK, stage + BM * 128, tid);
         };
         auto arrived = []() {
@@ -547,7 +550,7 @@ __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(T
                 OpA::fetch(sa, a.lda, va);
                 OpB::fetch(sb, a.ldb, vb);
             } else {
-                OpA::fetch_end(A, a.lda, m0, a.M, k, ke, va, tid);
+                OpA::fetch_end(A, a.lda, m0, wide, k, ke, va, tid);
                 OpB::fetch_end(B, a.ldb, n0, a.N, k, ke, vb, tid);
             }
         };
