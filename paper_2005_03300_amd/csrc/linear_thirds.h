@@ -133,7 +133,8 @@ struct HeldOperand : Operand<float, R, BY_MN, THREADS> {
 // workgroup on the compute unit meanwhile.  Of the compute units' cycles the matrix units are busy in 40 % at 232965 x 602 x 128 (96 products of 16 cycles a stage and wavefront), and
 // vector instructions are issued in 40 %: 22 split four numbers.  (A look at every number for infinities made them as many as the products take: 180 TFLOP/s.)  The second set of
 // results for those that are not finite costs 16 and 18 spilled registers of the 128 x 128 forms whose B lies along n.
-// HELD: A is a checkpoint.
+// HELD: A is a checkpoint (dW of 232965 x 128 x 256 from codes 109 us; unpacked first 112 and a pass of 43).
+// GATED, 232965 x 128 x 2*256 with GELU 299 us: a tile has four stages only, whose splitting makes vector instructions issue in 60 % of the cycles; matrix units are busy in 26 %.
 template <int BM, int BN, int WM, int WN, int LA, int LB, bool GATED, bool HELD = false>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, BK = 32, E = 4;
