@@ -33,7 +33,8 @@ struct SlopeArgs {
 
 // One pass over the matrices, bound by memory (a linear layer's 8192 x 4096 in fp16 with SiLU: 201 MB in 45 us, 4.5 TB/s).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two
 // or four such sets on their way, and a share of the rows; the four row sets are added in order.  Of gated blocks and of checkpoints a wavefront has several rows where they are short, `lanes`
-// of it for each, a power of two, and folds their sums first (56450 x 20 of a gated block in fp16: all 64 lanes for a row 106 us, four 18).
+// of it for each, a power of two, and folds their sums first (56450 x 20 of a gated block in fp16: all 64 lanes for a row 106 us, four 18);
+// rows that would leave an eighth of the lanes idle are cut into strips of 32 or 16 (16384 x 720 in fp16 41 us with 64, 37 with 32; 16508 x 300 in bf16 from a checkpoint 39 and, with 16, 34).
 // dZ is rounded to the element type here: both products take it from memory, and 16-bit matrix units take no more.  As the sum of two 16-bit numbers it would lose
 // nothing that counts, and both products would be twice as long (8192 x 1024 x 4096 in fp16: 160 us more on 210).  So dX and dW are off by what the roundings of dZ come to, about as much as by their own
 // (2.9e-4 of their norm in fp16 where the sum of an unrounded dZ has 2.1e-4, 2.3e-3 and 1.7e-3 in bf16); the bias's gradient is the sum of what was not rounded.
@@ -161,8 +162,13 @@ int launch_column_sums(const float* part, int parts, int32_t count, float* out, 
 
 template <typename T, bool GATED, bool HELD>
 static int launch_slope(SlopeArgs a, float* dbias, hipStream_t s) {
-    if (GATED || HELD)
-        for (; a.lanes > 1 && a.lanes / 2 * Elem<T>::E >= a.N; a.lanes /= 2) {}
+    if (GATED || HELD) {
+        constexpr int E = Elem<T>::E;
+        auto taken = [&](int lanes) { return (a.N + lanes * E - 1) / (lanes * E) * lanes; };       // lanes for a row, idle ones among them
+        for (; a.lanes > 1 && a.lanes / 2 * E >= a.N; a.lanes /= 2) {}
+        for (int lanes = a.lanes / 2; lanes >= 16; lanes /= 2)
+            if (8 * taken(lanes) <= 7 * taken(a.lanes)) a.lanes = lanes;
+    }
     const int64_t wide = a.lanes * Elem<T>::E, across = (a.N + wide - 1) / wide, width = (int64_t)a.N * (GATED ? 2 : 1), together = 64 / a.lanes;
     RowShares shares = row_shares((a.n + together - 1) / together, across, device_info().cus);       // of as many rows as a wavefront has together
     a.rows_per_block = shares.rows *= together;

@@ -214,7 +214,7 @@ def test_weights_of_ties_and_at_the_ends(type_):
 GATED = [(1, 1, 1, 0, 0), (1, 64, 64, 0, 0), (1, 1000, 300, 0, 0), (2, 4096, 40, 8, 0), (3, 5, 7, 0, 1), (16, 512, 1024, 0, 0), (17, 33, 65, 3, 0), (32, 160, 96, 0, 8), (33, 160, 96, 0, 8),
          (64, 64, 64, 0, 0), (65, 128, 129, 0, 0), (130, 602, 41, 0, 0), (257, 96, 304, 16, 0), (1000, 37, 8, 0, 0), (2049, 72, 808, 0, 0), (2049, 71, 801, 1, 1),
          (4099, 136, 2048, 0, 0), (20001, 48, 24, 0, 0), (9, 3000, 17, 0, 0), (8, 24, 20000, 0, 0), (5003, 9, 5, 0, 0), (3001, 16, 1, 2, 1), (700, 30, 200, 0, 0),
-         (1201, 8, 513, 0, 0)]
+         (1201, 8, 513, 0, 0), (515, 8, 300, 0, 0), (260, 24, 720, 4, 1)]
 
 
 def product_off(x, w, b):
