@@ -125,3 +125,28 @@ def test_weights_gradient_from_a_checkpoint(type_, p):
         again = torch.empty_like(dW.t)
         g.gcn_checkpoint_linear_backward(bx.pair(), None, None, dY.t, dW=again)
         assert torch.equal(again, dW.t), "the same call gives other bits"
+
+
+PADDED = [("bf16", p) for p in PRODUCTS if p[0] == "16" and p[1]]
+
+
+@pytest.mark.parametrize("type_,p", PADDED, ids=names(PADDED))
+def test_weights_gradient_of_padded_rows(type_, p):
+    """dW of X a checkpoint of f_in columns that do not fill 16 bytes: its restored rows do, and what lies behind them, here NaN of a call before, is no part of a result."""
+    g = lib()
+    _, _, _, _, M, N, K = p
+    gen = gen_of("padded dW", type_, M, N, K)
+    dY = matrix(K, N, type_, True, normal(gen, (K, N), type_))
+    codes = torch.ones(K, M, dtype=torch.int8, device="cuda")
+    scales = torch.full((K, -(-M // g.CHECKPOINT_GROUP)), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lost = torch.empty(M, N, dtype=dY.t.dtype, device="cuda")
+    g.gcn_checkpoint_linear_backward((codes, scales), None, None, dY.t, dW=lost)
+    assert torch.isnan(lost).all()
+    for f_in in (M - 1, M - 7):
+        bx, x = kept(normal(gen, (K, f_in), type_), type_, 3, 1)
+        dW = matrix(f_in, N, type_, False)
+        g.gcn_checkpoint_linear_backward(bx.pair(), None, None, dY.t, dW=dW.t)
+        x, dy = x.cuda(), dY.t.double()
+        ref, off = x.t() @ dy, (K + 2) * EPS * (x.abs().t() @ dy.abs())
+        check(dW.t, ref.cpu(), (off + UNIT[type_] * (ref.abs() + off) + TINY[type_]).cpu(), "dW")
+        assert dW.outside_is_untouched()
