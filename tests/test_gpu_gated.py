@@ -309,6 +309,27 @@ def test_gated_backward(type_, at, which):
         assert torch.equal(alone, got[one]), one
 
 
+@pytest.mark.parametrize("type_", ALL)
+@pytest.mark.parametrize("at", range(len(GATED)))
+def test_backward_in_place(type_, at):
+    """dZ in the place of Z, H in that of dH (dR in that of dY): the same bits, whatever lies beside a row's end in its rows."""
+    g = lib()
+    n, _, N, pad, skip = GATED[at]
+    act = ACTS[at % 4]
+    gen = gen_of("in place", type_, at)
+    z, dh = normal(gen, (n, 2 * N), type_), normal(gen, (n, N), type_)
+    Z, dH, dZ, H = Strided(n, 2 * N, type_, pad, skip, z), Strided(n, N, type_, pad, skip, dh), out(n, 2 * N, type_, pad, skip), out(n, N, type_, pad, skip)
+    db, again = torch.empty(2, 2 * N, device="cuda")
+    g.gcn_gated_backward(None, None, Z.t, dH.t, dZ.t, dbias=db, act=code(g, act), H=H.t)
+    g.gcn_gated_backward(None, None, Z.t, dH.t, Z.t, dbias=again, act=code(g, act), H=dH.t)
+    assert torch.equal(Z.t, dZ.t) and torch.equal(dH.t, H.t) and torch.equal(db, again)
+    bz, _ = kept(z, type_, pad, skip)
+    dY, dZ, dR = Strided(n, 2 * N, type_, pad, skip, normal(gen, (n, 2 * N), type_)), out(n, 2 * N, type_, pad, skip), out(n, 2 * N, type_, pad, skip)
+    g.gcn_checkpoint_linear_backward(None, None, bz.pair(), dY.t, dZ.t, dbias=db, act=g.ACT_SILU, dR=dR.t, rho=0.5)
+    g.gcn_checkpoint_linear_backward(None, None, bz.pair(), dY.t, dY.t, dbias=again, act=g.ACT_SILU)
+    assert torch.equal(dY.t, dZ.t) and torch.equal(db, again)
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_gated_gradient_against_differences(act):
     """Along a random direction of all inputs, against the quotient of differences of the plain form in 64 bits (step 1e-6, so that no ReLU's corner lies
