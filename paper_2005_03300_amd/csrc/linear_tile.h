@@ -22,10 +22,6 @@ struct TileArgs {
     int32_t N = 0;
     int32_t tiles_m = 0, tiles_n = 0;
     float* part = nullptr;        // partial results, one M x N (gated: M x 2 N) each split; NULL: the epilogue runs here
-    const uint16_t* a_scales = nullptr;          // A is a checkpoint, these its scales
-    int64_t lda_scales = 0;
-    int64_t a_wide = 0;           // elements that rows of A have, where that is more than M (A by m): the others are anything, as their results are not stored
-    __host__ __device__ int64_t wide_a() const { return a_wide ? a_wide : M; }
     // D' = rho R + act(D + 1 bias^T); the argument of act is Z.  Gated: D and Z have 2 N columns, D' = act(Z's first N) (Hadamard) the others
     const float* bias = nullptr;
     const void* R = nullptr;
@@ -34,6 +30,12 @@ struct TileArgs {
     int64_t ldr = 0, ldz = 0, ldy = 0;
     float rho = 0;
     int act = GCN_ACT_NONE;
+    // Fields of few kernels come last: in front of `bias` these moved the others' places, and the 256 x 256 tile through registers spilled 30 registers forward in place of 19 (bf16 23): 8191 x 2047 x
+    // 4095 with a kept Z 274 us in place of 206 in fp16, 270 in place of 248 in bf16.
+    const uint16_t* a_scales = nullptr;          // A is a checkpoint, these its scales
+    int64_t lda_scales = 0;
+    int64_t a_wide = 0;           // elements that rows of A have, where that is more than M (A by m): the others are anything, as their results are not stored
+    __host__ __device__ int64_t wide_a() const { return a_wide ? a_wide : M; }
 };
 
 // The normal distribution function Phi(z) and its density.  For 16-bit elements erfc by Abramowitz and Stegun's formula 7.1.26, off by 1.5e-7 at most, whose
@@ -474,8 +476,8 @@ __device__ __forceinline__ void leave_gated(const TileArgs& a, const v4f (&acc)[
 // each operand half as often from L2 as 128 x 128 and LDS as often per product as its wavefronts' 128 x 64 results ask for (the units take 2048 cycles of a stage, LDS
 // 1536); 128 x 128 has two workgroups on a compute unit, so that one's end overlaps the other's products (1.05 PFLOP/s), and 64 x 64 is for results too small to fill
 // the chip otherwise.  128 bytes of k are a cache line of a row, and one barrier for 64 (256 x 256) products of a wavefront.
-// DIRECT: rows of both operands at 16-byte addresses in whole pieces: memory to LDS without registers.  (Through registers the 256 x 256 tile spills 23 of them forward and
-// 60 for dW.)
+// DIRECT: rows of both operands at 16-byte addresses in whole pieces: memory to LDS without registers.  (Through registers the 256 x 256 tile spills 23 of them forward, 29 of a gated block, and
+// 60 for dW; in fp16 19, 29 and 76.)
 template <typename T, int BM, int BN, int WM, int WN, int LA, int LB, bool DIRECT, bool GATED>
 __global__ __launch_bounds__(WM* WN * 64, BM == 64 ? 4 : 2) void k_linear_tile(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, E = Elem<T>::E, BK = 8 * E;

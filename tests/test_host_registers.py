@@ -1,0 +1,35 @@
+"""Registers of the linear layers' kernels as the compiler gave them: what a change beside a kernel takes from it shows here, and not in its results.  Read from the built library, so without a GPU."""
+import os
+import re
+
+import pytest
+
+pytest.importorskip("msgpack")
+
+import kernel_registers
+from paper_2005_03300_amd import build
+
+TYPES = {"DF16b": "bf16", "DF16_": "f16"}
+WAYS = {(0, 1): "forward", (0, 0): "dX", (1, 1): "dW"}
+
+
+@pytest.fixture(scope="module")
+def kernels():
+    if not os.path.exists(build.LIB):
+        build.build()
+    return kernel_registers.kernels(build.LIB)
+
+
+def test_spilled_registers_of_linear_layers(kernels):
+    """The 256 x 256 tile through registers holds all there are and spills some; no other tile of 16-bit elements spills a vector register."""
+    most = {("bf16", "forward"): (23, 18), ("f16", "forward"): (19, 18), ("bf16", "dX"): (0, 0), ("f16", "dX"): (0, 0), ("bf16", "dW"): (60, 0), ("f16", "dW"): (78, 0)}
+    seen = 0
+    for name, k in kernels.items():
+        m = re.match(r"_ZN3gcn13k_linear_tileI(DF16b|DF16_)Li(\d+)ELi\d+ELi\d+ELi\d+ELi(\d)ELi(\d)ELb(\d)ELb0EEE", name)
+        if not m:
+            continue
+        seen += 1
+        type_, edge, way, direct = TYPES[m[1]], int(m[2]), WAYS[int(m[3]), int(m[4])], m[5] == "1"
+        vector, scalar = most[type_, way] if edge == 256 and not direct else (0, 28)
+        assert k[".vgpr_spill_count"] <= vector and k[".sgpr_spill_count"] <= scalar, (name, k[".vgpr_spill_count"], k[".sgpr_spill_count"])
+    assert seen == 36
