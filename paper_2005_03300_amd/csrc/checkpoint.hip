@@ -272,10 +272,7 @@ extern "C" int gcn_checkpoint_linear_backward(int64_t n, int32_t f_in, int32_t f
         SlopeArgs a;
         a.n = n; a.N = f_out; a.Z = z; a.dY = dY; a.lddy = lddy; a.dZ = dZ; a.lddz = lddz; a.also = dR; a.ldalso = lddr; a.rho = rho;
         a.act = dbias || dZ ? act : GCN_ACT_NONE;
-        GCN_TRY(by_type(type, [&](auto t) {
-            using T = decltype(t);
-            return z.scales ? launch_slope<T, false, true>(a, dbias, s) : launch_slope<T, false, false>(a, dbias, s);
-        }));
+        GCN_TRY(z.scales ? by_type(type, [&](auto t) { return launch_slope<decltype(t), false, true>(a, dbias, s); }) : launch_linear_slope(type, a, dbias, s));
     }
     BackProducts p;
     p.n = n; p.f_in = f_in; p.cols = f_out; p.X = x; p.W = W; p.ldw = ldw; p.G = curved ? dZ : dY; p.ldg = curved ? lddz : lddy;

@@ -114,6 +114,16 @@ inline RowShares row_shares(int64_t n, int64_t across, int64_t cus) {
     return {rows, (n + rows - 1) / rows};
 }
 
+// Rows of a set that the elementwise pass of a linear layer's backward pass has on their way (k_linear_slope): four where a share has 32 rows and more, else two, which take fewer registers and so
+// have more wavefronts on a compute unit, and less to begin and to end.  Nor four where rows of 16 KB and multiples stand in shares that begin a multiple of 2 MB apart: all workgroups then walk over the
+// same channels of the memory at the same time, and with more of the rows in flight more of them meet.  Microseconds of dZ with SiLU with two and with four, bf16: 4099 x 1024 7.9 and 8.3, 4099 x 4096 (shares of
+// 20 rows) 19.6 and 23.4, 65536 x 1024 89 and 83, 232965 x 128 91 and 78, 16384 x 8192 181 and 196; fp32: 4099 x 512 6.8 and 7.1, 16384 x 1024 42 and 41, 232965 x 128 91 and 80, 4099 x 8192 78 and
+// 76, 16384 x 4096 165 and 184.  Rows that are no whole pieces likewise: 16384 x 1001 in bf16 (shares of 16 rows) 23.7 and 26.1, 232965 x 301 in fp32 268 and 216 (but in bf16 117 and 129).
+inline int slope_rows_ahead(int64_t rows_of_share, int64_t row_bytes) {
+    if (row_bytes % (16 << 10) == 0 && rows_of_share * row_bytes % (2 << 20) == 0) return 2;
+    return rows_of_share >= 32 ? 4 : 2;
+}
+
 // The tiles of a product: their edge, and in how many shares the sum over k is cut.
 struct TileChoice {
     int edge, splits;

@@ -1,6 +1,6 @@
 // The elementwise part of a backward pass: what the gradient of a layer's output becomes in front of its products.  Of a gated block, whose Z = [Zg Zu] has 2 N columns,
 //   dZg = dH Zu act'(Zg),  dZu = dH act(Zg),  H = act(Zg) Zu again,
-// and of a linear layer from a checkpoint of Z, dZ = dY act'(Z), dR = rho dY.  With the column sums of dZ, of the products before they are rounded.
+// and of a linear layer, dZ = dY act'(Z), dR = rho dY.  With the column sums of dZ, of the products before they are rounded.
 #pragma once
 #include "held.h"
 #include "launch_rules.h"
@@ -31,8 +31,8 @@ struct SlopeArgs {
     float* part = nullptr;            // sums of each share of the rows, or NULL
 };
 
-// One pass over the matrices, bound by memory (a linear layer's 8192 x 4096 in fp16 with SiLU: 201 MB in 45 us, 4.5 TB/s).  A workgroup has 64 lanes of 16 bytes by four rows at a time, two
-// or four such sets on their way, and a share of the rows; the four row sets are added in order.  Of gated blocks and of checkpoints a wavefront has several rows where they are short, `lanes`
+// Of gated blocks, and of linear layers from a checkpoint of Z (from elements see k_linear_slope): one pass over the matrices, bound by memory.  A workgroup has 64 lanes of 16 bytes by four rows at a time, two
+// or four such sets on their way, and a share of the rows; the four row sets are added in order.  A wavefront has several rows where they are short, `lanes`
 // of it for each, a power of two, and folds their sums first (56450 x 20 of a gated block in fp16: all 64 lanes for a row 106 us, four 18);
 // rows that would leave an eighth of the lanes idle are cut into strips of 32 or 16 (16384 x 720 in fp16 41 us with 64, 37 with 32; 16508 x 300 in bf16 from a checkpoint 39 and, with 16, 34).
 // dZ is rounded to the element type here: both products take it from memory, and 16-bit matrix units take no more.  As the sum of two 16-bit numbers it would lose
@@ -41,10 +41,10 @@ struct SlopeArgs {
 template <typename T, bool GATED, bool HELD>
 __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
     constexpr int E = Elem<T>::E, WAVES = 4, AHEAD = GATED ? 2 : 4, HALVES = GATED ? 2 : 1;
-    constexpr bool NARROW = GATED || HELD;                        // (linear layers keep the order of their sums)
+    static_assert(GATED || HELD, "linear layers from elements have k_linear_slope");
     __shared__ float sums[WAVES][64][HALVES * E + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int lanes = NARROW ? a.lanes : 64, SETS = WAVES * (64 / lanes), set = (int)threadIdx.x / lanes;
+    const int lanes = a.lanes, SETS = WAVES * (64 / lanes), set = (int)threadIdx.x / lanes;
     const int32_t N = a.N;
     const int64_t c = ((int64_t)blockIdx.x * lanes + (lane & (lanes - 1))) * E, width = (int64_t)HALVES * N;
     const int64_t rb = (int64_t)blockIdx.y * a.rows_per_block, re = rb + a.rows_per_block < a.n ? rb + a.rows_per_block : a.n;
@@ -136,12 +136,11 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
         rows(std::false_type());
     }
     if (!a.part) return;
-    if constexpr (NARROW)
-        for (int d = 32; d >= lanes; d >>= 1)                     // the rows of a wavefront
+    for (int d = 32; d >= lanes; d >>= 1)                         // the rows of a wavefront
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h)
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum[h][e] += __shfl_xor(sum[h][e], d);
+            for (int e = 0; e < E; ++e) sum[h][e] += __shfl_xor(sum[h][e], d);
 #pragma unroll
     for (int h = 0; h < HALVES; ++h)
 #pragma unroll
@@ -159,17 +158,17 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a) {
 
 // The sums of the shares of the rows, added in order: 64 columns for each workgroup.
 int launch_column_sums(const float* part, int parts, int32_t count, float* out, hipStream_t s);
+// The elementwise part of a linear layer whose Z is elements.
+int launch_linear_slope(int type, SlopeArgs a, float* dbias, hipStream_t s);
 
 template <typename T, bool GATED, bool HELD>
 static int launch_slope(SlopeArgs a, float* dbias, hipStream_t s) {
-    if (GATED || HELD) {
-        constexpr int E = Elem<T>::E;
-        auto taken = [&](int lanes) { return (a.N + lanes * E - 1) / (lanes * E) * lanes; };       // lanes for a row, idle ones among them
-        for (; a.lanes > 1 && a.lanes / 2 * E >= a.N; a.lanes /= 2) {}
-        for (int lanes = a.lanes / 2; lanes >= 16; lanes /= 2)
-            if (8 * taken(lanes) <= 7 * taken(a.lanes)) a.lanes = lanes;
-    }
-    const int64_t wide = a.lanes * Elem<T>::E, across = (a.N + wide - 1) / wide, width = (int64_t)a.N * (GATED ? 2 : 1), together = 64 / a.lanes;
+    constexpr int E = Elem<T>::E;
+    auto taken = [&](int lanes) { return (a.N + lanes * E - 1) / (lanes * E) * lanes; };           // lanes for a row, idle ones among them
+    for (; a.lanes > 1 && a.lanes / 2 * E >= a.N; a.lanes /= 2) {}
+    for (int lanes = a.lanes / 2; lanes >= 16; lanes /= 2)
+        if (8 * taken(lanes) <= 7 * taken(a.lanes)) a.lanes = lanes;
+    const int64_t wide = a.lanes * E, across = (a.N + wide - 1) / wide, width = (int64_t)a.N * (GATED ? 2 : 1), together = 64 / a.lanes;
     RowShares shares = row_shares((a.n + together - 1) / together, across, device_info().cus);       // of as many rows as a wavefront has together
     a.rows_per_block = shares.rows *= together;
     shares.count = (a.n + shares.rows - 1) / shares.rows;

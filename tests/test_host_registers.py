@@ -33,3 +33,30 @@ def test_spilled_registers_of_linear_layers(kernels):
         vector, scalar = most[type_, way] if edge == 256 and not direct else (0, 28)
         assert k[".vgpr_spill_count"] <= vector and k[".sgpr_spill_count"] <= scalar, (name, k[".vgpr_spill_count"], k[".sgpr_spill_count"])
     assert seen == 36
+
+
+def test_registers_of_linear_slopes(kernels):
+    """The elementwise pass with two rows ahead leaves room for eight wavefronts on a SIMD (16-bit elements: seven); nothing of it is spilled."""
+    most = {"f": 64, "DF16b": 72, "DF16_": 72}
+    seen = 0
+    for name, k in kernels.items():
+        m = re.match(r"_ZN3gcn14k_linear_slopeI(f|DF16b|DF16_)Li(\d)ELb(\d)EEE", name)
+        if not m:
+            continue
+        seen += 1
+        assert k[".vgpr_spill_count"] == k[".sgpr_spill_count"] == 0, name
+        if m[2] == "2" and m[3] == "1":
+            assert k[".vgpr_count"] <= most[m[1]], (name, k[".vgpr_count"])
+    assert seen == 12
+
+
+def test_rows_ahead(tmp_path):
+    """Two rows ahead for short shares, and for rows of 16 KB whose shares begin 2 MB apart."""
+    from test_host_parts import run_cpp
+    cases = [(4, 2048, 2), (16, 2048, 2), (20, 8192, 2), (28, 602, 2), (32, 4096, 4), (64, 1024, 4), (228, 256, 4), (128, 16384, 2), (256, 32768, 2), (68, 16384, 4), (256, 8192, 4), (128, 16386, 4)]
+    r = run_cpp(tmp_path, '''
+        #include <cstdio>
+        #include "launch_rules.h"
+        int main() { %s }
+    ''' % "".join(f'printf("%d ", gcn::slope_rows_ahead({a}, {b}));' for a, b, _ in cases))
+    assert list(map(int, r.stdout.split())) == [w for _, _, w in cases]
