@@ -164,6 +164,56 @@ inline TileChoice choose_tiles(int64_t M, int64_t N, int64_t K, bool fp32, bool 
     return best;
 }
 
+// A gated block of up to 32 rows (k_linear_few): columns of a lane, and in how many shares the sum over k is cut.  A workgroup has a strip of 8 columns of H for each column of a lane, and with them as
+// many of either half of the weights.
+struct FewGated {
+    int columns, splits;
+};
+// The choice with the least estimated time, as choose_tiles.  A step of all wavefronts takes as long as its way from memory, little longer for wide strips than for narrow ones, and memory gives more in wide
+// pieces (rates below in bytes of a microsecond); so strips are the wider the more of them there are, and shares fill the compute units.  A second workgroup of a compute unit adds three quarters of the first one's
+// time, the whole of it where the registers and LDS have room for one only.  Shares cost partial results written and read again, and a launch.  Of 541 measured sizes (1 to 32
+// rows in bf16 and fp32, k of 64 to 16384, f_out of 100 to 30000) the choice takes 0.5 % longer than the fastest in the mean, 11 % at most.  (Rows at odd addresses take longer for a step, so that more
+// shares would pay: 3943 x 14583 in bf16 120 us with the choice, which is 8x1, and 73 with 8x3.)  Microseconds in bf16 of strips and shares of a row, columns of a lane x shares:
+//   f_in x f_out      1x1    2x1    4x1    8x1    8x2    8x3    8x4    others
+//   300 x 2048        5.2    5.3    5.5    6.0
+//   1024 x 4096      13.4   10.3   11.6   12.4   12.8
+//   1024 x 8192      23.1   17.1   12.6   13.4   15.5
+//   1024 x 8960      23.9   17.4   16.5   12.5   19.1
+//   4096 x 512       22.9   25.1   30.0   32.0   22.0   19.1   14.9   2x8 11.4
+//   4096 x 4096      40.2   28.5   34.5   36.6   26.2   24.6   23.7   4x4 24.5
+//   4096 x 8192      66.1   52.9   37.5   39.4   35.1   37.2   34.0
+//   4096 x 8960      71.5   52.8   49.9   35.5   42.1   37.0   38.9
+//   8192 x 8200     138.0  100.9   88.1   75.9   83.4   67.5   71.0
+//   8192 x 14336    223.0  150.9  124.5   99.1  102.4
+inline FewGated few_gated_choice(int64_t M, int64_t f_out, int64_t K, bool fp32, int64_t cus) {
+    static const double STEP16[4] = {2.2, 3.3, 3.8, 5.7}, RATE16[4] = {1.1e6, 2.3e6, 3.8e6, 4.7e6}, STEP16_32[4] = {2.8, 3.1, 4.0, 0}, RATE16_32[4] = {2.0e6, 2.2e6, 3.3e6, 0};
+    static const double STEP32[4] = {1.3, 2.2, 3.0, 0}, RATE32[4] = {2.0e6, 3.4e6, 4.4e6, 0}, STEP32_32[4] = {2.1, 2.4, 3.8, 0}, RATE32_32[4] = {1.8e6, 2.7e6, 3.6e6, 0};
+    const bool two = M > 16;                                      // fragments of 16 rows
+    const double* const step_us = fp32 ? (two ? STEP32_32 : STEP32) : two ? STEP16_32 : STEP16;
+    const double* const rate = fp32 ? (two ? RATE32_32 : RATE32) : two ? RATE16_32 : RATE16;
+    const int64_t bytes = fp32 ? 4 : 2, step = 16 * (64 / bytes), steps = (K + step - 1) / step;
+    FewGated best{1, 1};
+    double least = 1e300;
+    for (int i = 0; i < (fp32 || two ? 3 : 4); ++i) {
+        const int columns = 1 << i;
+        const int64_t strips = (f_out + 8 * columns - 1) / (8 * columns);
+        const bool alone = columns == 8 || (two && columns == 4);             // of a compute unit
+        for (int64_t splits = 1; splits <= 64 && splits <= steps; splits += splits < 4 ? 1 : (splits & (splits - 1)) ? splits / 3 : splits / 2) {
+            if (splits > 1 && strips * (splits - 1) > 2 * cus) break;
+            const int64_t share = (steps + splits - 1) / splits, each = (strips * splits + cus - 1) / cus;
+            const double rounds = alone ? each : 1 + 0.75 * (each - 1), way = (double)strips * 16 * columns * bytes * K / rate[i];
+            double us = rounds * share * step_us[i];
+            us = (us > way ? us : way) + 2.1 * rounds;
+            if (splits > 1) us += 4.8 + splits * (double)M * 2 * f_out * 8 / 4.3e6;
+            if (us < least) {
+                least = us;
+                best = {columns, (int)splits};
+            }
+        }
+    }
+    return best;
+}
+
 // In how many shares the sum over k of a product with weights held in 4 bits is cut, for tiles of 128 x 128: the least estimated time, as choose_tiles.  A share is a whole number of blocks of 128
 // values of k.
 inline int splits_of_4(int64_t tiles, int64_t results, int64_t K, bool fp32, int64_t cus) {

@@ -71,7 +71,7 @@ __device__ __forceinline__ void leave_few(const TileArgs& a, const v4f (&acc)[RT
 // lane loads C neighbouring columns of E rows of W and has with them C fragments of E values of k.  Up to 16 RT rows of X, whose fragments are 16
 // bytes of a row.  The wavefronts' results are added in order in LDS, and what the layer does with them follows.  Neighbouring strips run on the same XCD, since
 // a strip can be half of a cache line wide.
-// C is the widest that still leaves a strip for every compute unit: 4096 x 4096 in fp32 with 256 strips of 16 columns 14.5 us, with 128 of 32 18.8.
+// C is the widest that still leaves a strip for every compute unit (of a gated block see few_gated_choice): 4096 x 4096 in fp32 with 256 strips of 16 columns 14.5 us, with 128 of 32 18.8.
 // Few strips: the steps are also shared by gridDim.y workgroups, whose partial results k_linear_join adds.
 // GATED: half of a strip's columns are the gate's, the others those of the same 8 C columns of H (one row, 4096 x 2*8192 in bf16: 30 us, 4.5 TB/s, and 5 to join two shares).
 template <typename T, int C, int RT, bool GATED>

@@ -84,26 +84,25 @@ static int launch_few(TileArgs a, hipStream_t s, int64_t shares = 0) {
 
 template <typename T, bool GATED>
 static int linear_forward_impl(const TileArgs& a, hipStream_t s) {
-    const int64_t cus = device_info().cus, N = GATED ? 2 * (int64_t)a.N : a.N;
+    const int64_t cus = device_info().cus;
     // Two fragments of 16 rows are what k_linear_few holds.  17 and 32 rows there and as tiles of 64, bf16: 1024 x 4096 4.9 and 5.5 us against 9.1 and 10.0, 256 x 1024 3.7 and 3.8 against
     // 4.3, 4096 x 4096 13.8 and 15.7 against 13.6 and 14.6; fp32 21.6 and 23.8 against 31.  Tiles are the faster for long sums over few columns (16384 x 1024 in bf16 13.8 us
     // against 40).
     if (a.M > 32) return linear_product<T, BY_K, BY_MN, GATED>(a, s);
-    // A gated block's strip has two halves, and memory gives 5.0 TB/s in pieces of 128 bytes, 3.6 in pieces of 64 and 2.3 in pieces of 32.  So strips are as wide as gives each half 128 bytes, and the
-    // sum over k is shared where they leave compute units without work.  Microseconds of one row in bf16 with the strips and shares of a linear layer and with these: 8192 x 2*14336 123 and 98, 4096 x 2*8192
-    // 36.9 and 34.4, 4096 x 2*4096 28.7 and 22.7, 2048 x 2*2048 14.8 and 13.1; but 1024 x 2*8192 12.1 and 14.5, where the
-    // second launch costs more, and 8192 x 2*100 12.9 and 17.5, where the steps are too few for half of the compute units.  (17 to 32 rows of 16 bits: a wavefront has registers for 64 bytes.)
-    if constexpr (GATED)
-    {
-        constexpr int WIDE = sizeof(T) == 2 ? 8 : 4, STEP = 4 * Elem<T>::E * FEW_WAVES;
-        const int64_t wide = 16 * (a.M <= 16 ? WIDE : 4), shares = cus * wide / N > 1 ? cus * wide / N : 1;
-        if (shares == 1 || (a.K >= 2048 && (N + wide - 1) / wide * ((a.K + STEP - 1) / STEP) >= cus / 2))
-            return a.M <= 16 ? launch_few<T, WIDE, 1, GATED>(a, s, shares) : launch_few<T, 4, 2, GATED>(a, s, shares);
+    if constexpr (GATED) {
+        const FewGated f = few_gated_choice(a.M, a.N, a.K, sizeof(T) == 4, cus);
+        if (a.M <= 16) {
+            if constexpr (sizeof(T) == 2)
+                if (f.columns == 8) return launch_few<T, 8, 1, true>(a, s, f.splits);
+            return f.columns == 4 ? launch_few<T, 4, 1, true>(a, s, f.splits) : f.columns == 2 ? launch_few<T, 2, 1, true>(a, s, f.splits) : launch_few<T, 1, 1, true>(a, s, f.splits);
+        }
+        return f.columns == 4 ? launch_few<T, 4, 2, true>(a, s, f.splits) : f.columns == 2 ? launch_few<T, 2, 2, true>(a, s, f.splits) : launch_few<T, 1, 2, true>(a, s, f.splits);
+    } else {
+        // the widest strips that are still one for every compute unit
+        const int c = a.N >= 64 * cus ? 4 : a.N >= 32 * cus ? 2 : 1;
+        if (a.M <= 16) return c == 4 ? launch_few<T, 4, 1, false>(a, s) : c == 2 ? launch_few<T, 2, 1, false>(a, s) : launch_few<T, 1, 1, false>(a, s);
+        return c == 4 ? launch_few<T, 4, 2, false>(a, s) : c == 2 ? launch_few<T, 2, 2, false>(a, s) : launch_few<T, 1, 2, false>(a, s);
     }
-    // the widest strips that are still one for every compute unit
-    const int c = N >= 64 * cus ? 4 : N >= 32 * cus ? 2 : 1;
-    if (a.M <= 16) return c == 4 ? launch_few<T, 4, 1, GATED>(a, s) : c == 2 ? launch_few<T, 2, 1, GATED>(a, s) : launch_few<T, 1, 1, GATED>(a, s);
-    return c == 4 ? launch_few<T, 4, 2, GATED>(a, s) : c == 2 ? launch_few<T, 2, 2, GATED>(a, s) : launch_few<T, 1, 2, GATED>(a, s);
 }
 
 template <> int linear_forward_of<GCN_LINEAR_ELEM>(const TileArgs& a, hipStream_t s) { return linear_forward_impl<GCN_LINEAR_ELEM, false>(a, s); }
