@@ -10,7 +10,7 @@ and a last linear layer; its loss is gcn_distill against the teacher's k largest
 vertex afterwards needs neither the graph nor the teacher.
 
 With --gated the blocks' first layer is a gated one, act(H Wg + bg) * (H Wu + bu); between the forward and the backward pass its argument and
-input are kept in 8 bits, and its output is computed again.  Such a student also answers from weights held in 4 bits.
+the block's input are kept in 8 bits, and its output is computed again.  Such a student also answers from weights held in 4 bits.
 
     python examples/distill_student.py [--type bf16|f16|f32] [--blocks 2] [--width 128] [--steps 200] [--gated]
 """
@@ -86,14 +86,14 @@ class Student:
         self.dvec = {k: torch.empty_like(v) for k, v in self.vec.items()}
         e = lambda cols: torch.empty(n, cols, dtype=dtype, device="cuda")
         rows = lambda: torch.empty(n, 4, device="cuda")
-        self.X, self.H, self.st = [e(width) for _ in range(blocks + 1)], [e(width) for _ in range(blocks + 1)], [rows() for _ in range(blocks + 1)]
+        self.X, self.st = [e(width) for _ in range(blocks + 1)], [rows() for _ in range(blocks + 1)]
         if gated:                                                 # one block's at a time; what is kept of each are checkpoints
-            self.Z1, self.Y1 = [e(inner)] * blocks, [e(2 * width)] * blocks
+            self.H, self.Z1, self.Y1 = [e(width)] * (blocks + 1), [e(inner)] * blocks, [e(2 * width)] * blocks
             held = lambda cols: (torch.empty(n, cols, dtype=torch.int8, device="cuda"),
                                  torch.empty(n, -(-cols // g.CHECKPOINT_GROUP), dtype=torch.bfloat16, device="cuda"))
             self.H8, self.Z8 = [held(width) for _ in range(blocks)], [held(inner) for _ in range(blocks)]
         else:
-            self.Z1, self.Y1 = [e(inner) for _ in range(blocks)], [e(inner) for _ in range(blocks)]
+            self.H, self.Z1, self.Y1 = [e(width) for _ in range(blocks + 1)], [e(inner) for _ in range(blocks)], [e(inner) for _ in range(blocks)]
         self.U, self.A = [e(width) for _ in range(blocks)], [e(width) for _ in range(blocks)]
         self.logits, self.G = e(classes), e(classes)
         self.dX, self.dH, self.dH2, self.dU, self.dA = (e(width) for _ in range(5))
@@ -101,16 +101,18 @@ class Student:
         self.loss = torch.empty(1, device="cuda")
         self.momentum = {}
 
-    def forward(self, P):
+    def forward(self, P, keep: bool = False):
+        """Logits; with `keep` a gated student's checkpoints as well, which only a backward pass needs."""
         W, v = self.W, self.vec
         g.gcn_linear_forward(P, W["in"], self.X[0], bias=v["in.b"])
         g.gcn_block_norm_forward(self.X[0], H=self.H[0], w_pre=v["norm0"], stats=self.st[0])
         for l in range(self.blocks):
             H = self.H[l]
             if self.gated:
-                g.gcn_gated_forward(H, W[f"{l}.W1"], self.Y1[l], bias=v[f"{l}.b1"], Z=self.Z1[l])
-                g.gcn_checkpoint_pack(self.Z1[l], *self.Z8[l])
-                g.gcn_checkpoint_pack(H, *self.H8[l])
+                g.gcn_gated_forward(H, W[f"{l}.W1"], self.Y1[l], bias=v[f"{l}.b1"], Z=self.Z1[l] if keep else None)
+                if keep:
+                    g.gcn_checkpoint_pack(self.Z1[l], *self.Z8[l])
+                    g.gcn_checkpoint_pack(H, *self.H8[l])
             else:
                 g.gcn_linear_forward(H, W[f"{l}.W1"], self.Y1[l], bias=v[f"{l}.b1"], act=g.ACT_GELU, Z=self.Z1[l])
             g.gcn_linear_forward(self.Y1[l], W[f"{l}.W2"], self.U[l], bias=v[f"{l}.b2"])
@@ -123,7 +125,7 @@ class Student:
     def step(self, P, top, t, labels, lr: float, temperature: float = 2.0):
         """One step of gradient descent over all rows; returns the loss (on the device)."""
         W, dW, v, dv = self.W, self.dW, self.vec, self.dvec
-        self.forward(P)
+        self.forward(P, keep=True)
         # half-precision gradients of a mean over many rows would be lost below the type's smallest numbers: they are carried n times as large
         g.gcn_distill(self.logits, top, t, self.loss, self.G, labels=labels, temperature=temperature, w_teacher=0.7, w_label=0.3,
                       grad_scale=float(self.n))
@@ -139,11 +141,12 @@ class Student:
                 g.gcn_gated_backward(self.H8[l], W[f"{l}.W1"], self.Z8[l], self.dY1, self.dZ1, dX=self.dH, dW=dW[f"{l}.W1"],
                                      dbias=dv[f"{l}.b1"], H=self.Y1[l])
                 g.gcn_linear_backward(self.Y1[l], None, None, self.dU, dW=dW[f"{l}.W2"])
+                g.gcn_checkpoint_linear_backward(self.H8[l], W[f"{l}.G"], None, self.dA, dX=self.dH2, dW=dW[f"{l}.G"])
             else:
                 g.gcn_linear_backward(self.Y1[l], W[f"{l}.W2"], None, self.dU, dX=self.dY1, dW=dW[f"{l}.W2"], dbias=dv[f"{l}.b2"])
                 g.gcn_linear_backward(self.H[l], W[f"{l}.W1"], self.Z1[l], self.dY1, self.dZ1, dX=self.dH, dW=dW[f"{l}.W1"],
                                       dbias=dv[f"{l}.b1"], act=g.ACT_GELU)
-            g.gcn_linear_backward(self.H[l], W[f"{l}.G"], None, self.dA, dX=self.dH2, dW=dW[f"{l}.G"])
+                g.gcn_linear_backward(self.H[l], W[f"{l}.G"], None, self.dA, dX=self.dH2, dW=dW[f"{l}.G"])
             self.dH += self.dH2
         g.gcn_block_norm_backward(None, self.X[0], self.st[0], dXout, self.dH, self.dX, w_pre=v["norm0"], dw_pre=dv["norm0"])
         g.gcn_linear_backward(P, None, None, self.dX, dW=dW["in"], dbias=dv["in.b"])
