@@ -295,7 +295,8 @@ int gcn_linear_backward(int64_t n, int32_t f_in, int32_t f_out, int type, const 
  * and reproducibility as gcn_linear_forward; f_in up to 2^27, f_out up to 2^26 (RANGE).  No output may overlap an input or another output.
  * backward, with dL/dH given as dH:
  *   dZ = [dH (Hadamard) Z[:, f_out:] (Hadamard) act'(Z[:, :f_out]),  dH (Hadamard) act(Z[:, :f_out])],  dX = dZ W^T,  dW = X^T dZ,
- *   dbias = column sums of dZ (before it is rounded),  H as above (which then need not be kept for the next layer's dW)
+ *   dbias = column sums of dZ (before it is rounded),  H as above, so that it need not be kept for the next layer's dW: from Z as it is given, where forward
+ *   had its sums in fp32; so with 16-bit elements, or from a checkpoint, it is near forward's H and not the same bits
  * Any of dX, dW, dbias, H may be NULL, and is then not computed; X is read for dW and W for dX only.  dZ (n x 2 f_out) is workspace that the call fills, needed for dX and dW; it is rounded
  * to the element type, as in gcn_linear_backward.  dZ may be Z, and H may be dH (same address and leading dimension).
  * x_scales, z_scales: NULL, or X (Z) is a checkpoint, X the codes (int8, ldx apart) and x_scales their scales (see below; Z's groups are of its rows of 2 f_out).

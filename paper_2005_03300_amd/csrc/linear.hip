@@ -4,7 +4,7 @@
 namespace gcn {
 
 // dZ = dY * act'(Z), dR = rho dY, and the column sums of dZ (the bias gradient, of the unrounded products) of a linear layer whose Z is elements: one pass over the matrices for the elementwise
-// part, bound by memory (8192 x 4096 in fp16 with SiLU: 201 MB in 45 us, 4.5 TB/s).  A workgroup has 64 lanes of 16 bytes by four rows at a time, AHEAD such sets on their way (see
+// part, bound by memory (8192 x 4096 in fp16 with SiLU: 205 MB in 42 us, 4.9 TB/s).  A workgroup has 64 lanes of 16 bytes by four rows at a time, AHEAD such sets on their way (see
 // slope_rows_ahead), and a share of the rows; the four row sets are added in order.  How dZ is rounded, and what that costs: see k_slope.
 // WHOLE: rows of whole pieces.  Else a workgroup whose columns are not all whole pieces goes the other way with all of them: two ways one after the other took twice as long (4099 x 1001 in bf16
 // with SiLU 12.8 and 8.8 us).  In a kernel of its own, since with both ways in one the first has 78 registers of bf16 and not 70, and so a wavefront less on every SIMD (4099 x 4096 22.8 us in place of 20).

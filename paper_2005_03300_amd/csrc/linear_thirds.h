@@ -132,9 +132,11 @@ struct HeldOperand : Operand<float, R, BY_MN, THREADS> {
 // As k_linear_tile through registers, for any alignment; one stage in LDS (three planes of 32 k: 48 KB of a 128 x 128 tile), the next one in registers, and another
 // workgroup on the compute unit meanwhile.  Of the compute units' cycles the matrix units are busy in 40 % at 232965 x 602 x 128 (96 products of 16 cycles a stage and wavefront), and
 // vector instructions are issued in 40 %: 22 split four numbers.  (A look at every number for infinities made them as many as the products take: 180 TFLOP/s.)  The second set of
-// results for those that are not finite costs 16 and 18 spilled registers of the 128 x 128 forms whose B lies along n.
+// results for those that are not finite costs 17 and 18 spilled registers of the 128 x 128 forms whose B lies along n (21 of a gated block, 12 from codes) and 108 to 134 scalar ones, which are stored
+// in every workgroup: 232965 x 602 x 128 takes 266 us, and 252 with that part left out.
 // HELD: A is a checkpoint (dW of 232965 x 128 x 256 from codes 109 us; unpacked first 112 and a pass of 43).
-// GATED, 232965 x 128 x 2*256 with GELU 299 us: a tile has four stages only, whose splitting makes vector instructions issue in 60 % of the cycles; matrix units are busy in 26 %.
+// GATED, 232965 x 128 x 2*256 with GELU 301 us: a tile has four stages only, and what is beside them counts: GELU 42 us, the spilled registers, 0.16 GB of the 0.40 written, 29.  Vector instructions are
+// issued in 60 % of the cycles, of which splitting W, half of all that is split, is 2 % of the time; matrix units are busy in 25 %.
 template <int BM, int BN, int WM, int WN, int LA, int LB, bool GATED, bool HELD = false>
 __global__ __launch_bounds__(WM* WN * 64, 2) void k_linear_thirds(TileArgs a) {
     constexpr int THREADS = WM * WN * 64, BK = 32, E = 4;
