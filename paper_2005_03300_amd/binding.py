@@ -391,6 +391,7 @@ def _kept(t, shape, dtype):
     if not isinstance(t, (tuple, list)):
         return *_mat(t, shape, dtype), 0, 0
     codes, scales = t
+    assert codes is not None and scales is not None, "a checkpoint has codes and scales"        # (codes without scales would be taken for elements, which are longer)
     return *_mat(codes, shape, _i8), *_mat(scales, (shape[0], -(-shape[1] // CHECKPOINT_GROUP)), _bf16)
 
 
