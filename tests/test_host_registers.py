@@ -60,3 +60,20 @@ def test_rows_ahead(tmp_path):
         int main() { %s }
     ''' % "".join(f'printf("%d ", gcn::slope_rows_ahead({a}, {b}));' for a, b, _ in cases))
     assert list(map(int, r.stdout.split())) == [w for _, _, w in cases]
+
+
+def test_sizes_take_the_slopes_that_they_stand_for(tmp_path):
+    from linear_slopes import SLOPES
+    from test_host_parts import run_cpp
+    r = run_cpp(tmp_path, '''
+        #include <cstdio>
+        #include "launch_rules.h"
+        static void size(int64_t n, int64_t N, int64_t bytes) {
+            const int64_t wide = 64 * (16 / bytes), across = (N + wide - 1) / wide;
+            printf("%%d %%d\\n", gcn::slope_rows_ahead(gcn::row_shares(n, across, 256).rows, N * bytes), N %% (16 / bytes) == 0);
+        }
+        int main() { %s }
+    ''' % "".join(f"size({n}, {N}, {4 if t == 'f32' else 2});" for t, _, _, n, N in SLOPES))
+    got = [(int(a), b == "1") for a, b in map(str.split, r.stdout.splitlines())]
+    assert got == [p[1:3] for p in SLOPES], [(p, q) for p, q in zip(SLOPES, got) if p[1:3] != q]
+    assert {p[:3] for p in SLOPES} == {(t, a, w) for t in ("16", "f32") for a in (2, 4) for w in (False, True)}
